@@ -45,7 +45,8 @@ typedef enum fiona_status {
   FIONA_ERR_ARG = -1,          /* null pointer, zero or inconsistent size */
   FIONA_ERR_PLAN = -2,         /* layer description inconsistent (index out of range, bad CSR) */
   FIONA_ERR_UNSUPPORTED = -3,  /* N, L or a modulus outside the supported range */
-  FIONA_ERR_ALIGN = -4,        /* a device pointer is not 8-byte aligned (rotation keys: 16-byte) */
+  FIONA_ERR_ALIGN = -4,        /* a device pointer is not 8-byte aligned (rotation keys: 16-byte; the key
+                                  holder's operators: their elements' size) */
   FIONA_ERR_ALIAS = -5,        /* the output buffer overlaps an input buffer */
   FIONA_ERR_HIP = -6,          /* a HIP runtime call failed (device allocation, copy, launch) */
   FIONA_ERR_NOMEM = -7,        /* host allocation failed */
@@ -411,6 +412,189 @@ int fiona_rotation_key_layout(const fiona_rotator *rotator, uint32_t galois, con
                               uint64_t *key_out, hipStream_t stream);
 int fiona_hoisted_rotate(const fiona_rotator *rotator, const uint64_t *ct, uint32_t n_rot, const uint32_t *galois,
                          const uint64_t *keys, uint64_t *out_cts, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The key holder's operators.
+ *
+ * Between two encrypted projections of a transformer stand steps that residues
+ * have no exact form for (a softmax, its maximum, a division).  A program that
+ * runs them at the key holder has the decrypted rows of a projection on its
+ * own GPU: it adds its private adapters' part to them (fiona_adapter_linear),
+ * appends the keys and values to its cache (fiona_kv_append), attends
+ * (fiona_paged_attention) and encrypts the result for the next projection.
+ * The adapters are trained there too (fiona_adapter_backward).
+ *
+ * Elements are IEEE binary32, binary16 or bfloat16.  Whatever the type, every
+ * product is summed in 32 bits, softmax statistics are held in 32 bits, and a
+ * result is rounded to its type once.  Strides count elements; the last axis
+ * of every array is contiguous.  Device pointers need the alignment of their
+ * elements; where pointers and strides are multiples of 16 bytes and rows are
+ * multiples of 8 elements the kernels read and write 16 bytes per lane.
+ * ------------------------------------------------------------------------ */
+typedef enum fiona_type { FIONA_F32 = 0, FIONA_F16 = 1, FIONA_BF16 = 2 } fiona_type;
+
+#define FIONA_MAX_HEAD_DIM 256u
+#define FIONA_MAX_RANK 128u
+
+/*
+ * A paged cache: key (and value) row `head` of the token in place `at` of page
+ * `page` starts at element page * k_page + at * k_token + head * k_head of k.
+ * Rows of different (page, place, head) must not overlap, nor k with v.
+ */
+typedef struct fiona_kv_cache {
+  uint32_t type;       /* fiona_type of both arrays */
+  uint32_t n_pages, page_size, n_kv, head_dim;   /* head_dim <= FIONA_MAX_HEAD_DIM; n_pages * page_size < 2^31 */
+  void *k, *v;         /* device */
+  uint64_t k_page, k_token, k_head;
+  uint64_t v_page, v_token, v_head;
+} fiona_kv_cache;
+
+/*
+ * fiona_kv_append: rotate the new tokens' keys (and queries) by their
+ * positions and write keys and values into the cache.
+ *
+ * Pair i < rot_dim / 2 of a row, elements (i, i + rot_dim / 2), or
+ * (2 i, 2 i + 1) with interleaved, becomes
+ *     (a cos[p][i] - b sin[p][i],  a sin[p][i] + b cos[p][i])
+ * at the token's position p; elements from rot_dim on are copied.
+ *   rows_type   fiona_type of k, v and q
+ *   k, v        device, [n_tok][n_kv][head_dim]
+ *   q, q_out    device, [n_tok][n_head][head_dim], or NULL with n_head 0;
+ *               q_out has the cache's type; it may be q itself (same type and strides)
+ *   slots       device, [n_tok]: page * page_size + place of each token; a token
+ *               whose slot lies outside the cache is not written (padding: -1).
+ *               Slots of one call are distinct, or which token is kept is unspecified
+ *   positions   device, [n_tok], with rot_dim > 0
+ *   cos, sin    device, [n_pos][rot_dim / 2]; a token whose position lies
+ *               outside [0, n_pos) gets NaN in its rotated elements
+ * Asynchronous on stream; one kernel launch, allocates nothing.  Errors
+ * (nothing is launched): FIONA_ERR_ARG, FIONA_ERR_UNSUPPORTED (a type or size
+ * outside its range), FIONA_ERR_ALIGN, FIONA_ERR_ALIAS (an output overlaps an
+ * input or another output; cache rows that overlap each other), FIONA_ERR_HIP.
+ */
+typedef struct fiona_append_args {
+  uint32_t n_tok, n_head, rows_type, rot_dim, n_pos, interleaved;
+  const void *k, *v, *q;
+  void *q_out;
+  uint64_t k_tok, k_head, v_tok, v_head, q_tok, q_head, q_out_tok, q_out_head;
+  const int64_t *slots;
+  const int32_t *positions;
+  const float *cos, *sin;
+} fiona_append_args;
+
+int fiona_kv_append(const fiona_kv_cache *cache, const fiona_append_args *args, hipStream_t stream);
+
+/*
+ * fiona_attention_create: the workspace of fiona_paged_attention (the parts of
+ * a long cache's softmax that are joined), for up to max_seq sequences of up
+ * to max_length tokens.  n_head is a multiple of n_kv: query head h reads key
+ * head h / (n_head / n_kv).  Errors: FIONA_ERR_ARG, FIONA_ERR_UNSUPPORTED
+ * (a type or size outside its range), FIONA_ERR_NOMEM, FIONA_ERR_HIP.
+ */
+typedef struct fiona_attention_desc {
+  uint32_t type, n_head, n_kv, head_dim, page_size, max_seq, max_length;
+} fiona_attention_desc;
+
+typedef struct fiona_attention fiona_attention;
+int fiona_attention_create(const fiona_attention_desc *desc, fiona_attention **out);
+void fiona_attention_destroy(fiona_attention *att);
+
+/*
+ * fiona_paged_attention: one new token of each sequence attends to its cache.
+ * With n the sequence's length (the new token included), first = n - window
+ * (0 without a window, or below it), and key j in page page_table[j / page_size]
+ * at place j mod page_size,
+ *     s_j = scale q . k_j,  or softcap tanh(s_j / softcap) with a softcap,
+ *     out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   first <= j < n
+ *     lse = m + log sum_j exp(s_j - m),                    m = max_j s_j.
+ *   n_seq       at most the handle's max_seq
+ *   q, out      device, [n_seq][n_head][head_dim], of the handle's type
+ *   lse         device, [n_seq][n_head] float32, or NULL
+ *   page_table  device, [n_seq] rows of table_width entries, table_stride
+ *               apart.  A key whose entry lies outside [0, n_pages) is left
+ *               out, as if it were masked
+ *   lengths     device, [n_seq]; clamped to [0, min(max_length,
+ *               table_width * page_size)]
+ *   scale > 0; window 0: none; softcap 0: none, else > 0
+ * A sequence with no key gets out = 0 and lse = -inf.  Cache places past a
+ * sequence's length are never used, whatever they hold.
+ * Asynchronous on stream; one or two kernel launches, allocates nothing.  The
+ * workspace is shared by the handle's calls: one handle must not be used by
+ * two streams at the same time.  Errors (nothing is launched): FIONA_ERR_ARG
+ * (also a cache that does not match the handle), FIONA_ERR_UNSUPPORTED,
+ * FIONA_ERR_ALIGN, FIONA_ERR_ALIAS, FIONA_ERR_HIP.
+ */
+typedef struct fiona_attention_args {
+  uint32_t n_seq, table_width, window;
+  float scale, softcap;
+  const void *q;
+  void *out;
+  float *lse;
+  uint64_t q_seq, q_head, out_seq, out_head, table_stride;
+  const int32_t *page_table;
+  const int32_t *lengths;
+} fiona_attention_args;
+
+int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cache, const fiona_attention_args *args,
+                          hipStream_t stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared projection.  Token t has
+ * adapter a = ids[t] (any order; an id outside [0, n_adapter): none) of rank
+ * r = ranks[a] (clamped to [0, max_rank]; NULL: max_rank) and scaling
+ * c = scaling[a] (NULL: 1):
+ *     h_t = A_a x_t,   y_t = base_t + c B_a h_t.
+ *
+ * fiona_adapters_create: the workspace of calls of up to max_tokens tokens.
+ * Errors: FIONA_ERR_ARG, FIONA_ERR_UNSUPPORTED (a type, a rank over
+ * FIONA_MAX_RANK, a size outside its range), FIONA_ERR_NOMEM, FIONA_ERR_HIP.
+ *
+ * fiona_adapter_linear:
+ *   x     device, [n_tok][d_in]            A  device, [n_adapter][max_rank][d_in]
+ *   base  device, [n_tok][d_out], or NULL  B  device, [n_adapter][d_out][max_rank]
+ *         (zero); it may be y itself       y  device, [n_tok][d_out]
+ * Rows of A and columns of B from the adapter's rank on are not used.  A token
+ * without an adapter gets y_t = base_t.
+ *
+ * fiona_adapter_backward: from dy, the gradient of y,
+ *     g_t = c B_a^T dy_t,   dx_t = dx_base_t + A_a^T g_t,
+ *     dA_a = sum over its tokens of g_t x_t^T,   dB_a = c sum dy_t h_t^T
+ * dx_base may be NULL (zero) or dx itself (the gradient through the shared
+ * projection); dA and dB are overwritten whole, with zeros for adapters no
+ * token has and from an adapter's rank on.  The gradient of base is dy.
+ * Sums run in a fixed order: the same call gives the same bits.
+ *
+ * Both: asynchronous on stream, kernel launches only, allocate nothing.  The
+ * workspace is shared by the handle's calls: one handle must not be used by
+ * two streams at the same time.  Errors (nothing is launched): FIONA_ERR_ARG,
+ * FIONA_ERR_ALIGN, FIONA_ERR_ALIAS, FIONA_ERR_HIP.
+ */
+typedef struct fiona_adapters_desc {
+  uint32_t type, n_adapter, max_rank, d_in, d_out, max_tokens;
+} fiona_adapters_desc;
+
+typedef struct fiona_adapter_args {
+  uint32_t n_tok;
+  const void *x, *A, *B;
+  const int32_t *ids;
+  const int32_t *ranks;    /* [n_adapter] or NULL */
+  const float *scaling;    /* [n_adapter] or NULL */
+  uint64_t x_row;
+  /* fiona_adapter_linear */
+  const void *base;
+  void *y;
+  uint64_t base_row, y_row;
+  /* fiona_adapter_backward */
+  const void *dy, *dx_base;
+  void *dx, *dA, *dB;
+  uint64_t dy_row, dx_base_row, dx_row;
+} fiona_adapter_args;
+
+typedef struct fiona_adapters fiona_adapters;
+int fiona_adapters_create(const fiona_adapters_desc *desc, fiona_adapters **out);
+void fiona_adapters_destroy(fiona_adapters *adapters);
+int fiona_adapter_linear(const fiona_adapters *adapters, const fiona_adapter_args *args, hipStream_t stream);
+int fiona_adapter_backward(const fiona_adapters *adapters, const fiona_adapter_args *args, hipStream_t stream);
 
 /*
  * Measurement helper (not part of the weighted sum): the register-only rate
