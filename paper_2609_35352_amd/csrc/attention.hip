@@ -6,6 +6,7 @@
 #include <cstdint>
 #include <new>
 
+#include "attention_kernel.hpp"
 #include "fiona.h"
 #include "rows.hpp"
 
@@ -14,71 +15,36 @@ using namespace fiona_host;
 struct fiona_attention {
   fiona_attention_desc desc{};
   int device = -1;
+  float *part = nullptr;      // the parts of split sequences
+  uint64_t part_cap = 0;      // (sequence, split) pairs that fit, n_head heads each
 };
 
-namespace fiona {
+namespace {
 
-struct AttendParams {
-  const void *q, *kc, *vc;
-  void *out;
-  float *lse;
-  const int32_t *table, *lengths;
-  uint64_t q_seq, q_head, out_seq, out_head, table_stride;
-  uint64_t k_page, k_token, k_head, v_page, v_token, v_head;
-  uint32_t n_head, group, d, page_size, n_pages, window, max_length;
-  float scale, softcap;
-};
+constexpr uint32_t kMinChunk = 512, kMaxChunk = 1024, kMaxSplits = 128, kWorkgroups = 1024;
 
-// A workgroup of four wavefronts per (sequence, query head).  Wavefront w
-// takes keys w, w + 4, ... with a running maximum and sum, each lane holding
-// up to four elements of the head; the four are joined at the end.
-template <typename T>
-__global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
-  __shared__ float sm[4], sl[4], so[4][FIONA_MAX_HEAD_DIM];
-  const uint32_t h = blockIdx.x, s = blockIdx.y, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int32_t n = P.lengths[s];
-  n = n < 0 ? 0 : (uint32_t)n > P.max_length ? (int32_t)P.max_length : n;
-  const int32_t first = P.window && (uint32_t)n > P.window ? n - (int32_t)P.window : 0;
-  const T *q = (const T *)P.q + s * P.q_seq + h * P.q_head;
-  float qv[4], o[4] = {0, 0, 0, 0}, m = -INFINITY, l = 0;
-  for (int e = 0; e < 4; ++e) qv[e] = lane + 64 * e < P.d ? (float)q[lane + 64 * e] : 0.f;
-  for (int32_t j = first + (int32_t)w; j < n; j += 4) {
-    const int32_t page = P.table[s * P.table_stride + (uint32_t)j / P.page_size];
-    if (page < 0 || (uint32_t)page >= P.n_pages) continue;
-    const uint64_t at = (uint32_t)j % P.page_size, kh = h / P.group;
-    const T *k = (const T *)P.kc + page * P.k_page + at * P.k_token + kh * P.k_head;
-    const T *v = (const T *)P.vc + page * P.v_page + at * P.v_token + kh * P.v_head;
-    float dot = 0, vv[4];
-    for (int e = 0; e < 4; ++e) {
-      const bool in = lane + 64 * e < P.d;
-      dot += in ? qv[e] * (float)k[lane + 64 * e] : 0.f;
-      vv[e] = in ? (float)v[lane + 64 * e] : 0.f;
-    }
-    for (int x = 32; x; x >>= 1) dot += __shfl_xor(dot, x);
-    dot *= P.scale;
-    if (P.softcap > 0) dot = P.softcap * tanhf(dot / P.softcap);
-    const float mn = fmaxf(m, dot), ms = mn == -INFINITY ? 0.f : mn;
-    const float keep = expf(m - ms), p = expf(dot - ms);
-    l = l * keep + p;
-    for (int e = 0; e < 4; ++e) o[e] = o[e] * keep + p * vv[e];
-    m = mn;
-  }
-  if (lane == 0) sm[w] = m, sl[w] = l;
-  for (int e = 0; e < 4; ++e) so[w][lane + 64 * e] = o[e];
-  __syncthreads();
-  const float mt = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])), ms = mt == -INFINITY ? 0.f : mt;
-  float lt = 0, ot = 0;
-  const uint32_t e = threadIdx.x;
-  for (int i = 0; i < 4; ++i) {
-    const float f = expf(sm[i] - ms);
-    lt += sl[i] * f;
-    ot += so[i][e] * f;
-  }
-  if (e < P.d) ((T *)P.out)[s * P.out_seq + h * P.out_head + e] = (T)(lt == 0 ? 0.f : ot / lt);
-  if (e == 0 && P.lse) P.lse[(uint64_t)s * P.n_head + h] = lt == 0 ? -INFINITY : ms + logf(lt);
+// Keys of one workgroup's chunk for calls over up to `keys` keys: few enough
+// that the sequences and key heads fill the GPU, at most kMaxChunk so that
+// ragged lengths even out, and at most kMaxSplits parts to join.
+uint32_t chunk_of(uint64_t keys, uint64_t units) {
+  uint64_t c = (keys * units + kWorkgroups - 1) / kWorkgroups;
+  c = std::max<uint64_t>(kMinChunk, std::min<uint64_t>(c, kMaxChunk));
+  c = std::max<uint64_t>(c, (keys + kMaxSplits - 1) / kMaxSplits);
+  return (uint32_t)((c + 127) / 128 * 128);
 }
 
-}  // namespace fiona
+uint32_t splits_of(uint64_t keys, uint32_t chunk) { return keys ? (uint32_t)((keys + chunk - 1) / chunk) : 1; }
+
+uint32_t head_blocks(const fiona_attention_desc &D) { return (D.n_head / D.n_kv + 15) / 16; }
+
+template <typename T, int HD>
+void launch_split(const fiona::AttendParams &P, bool vec, bool span, dim3 grid, hipStream_t stream) {
+  if (vec && span) hipLaunchKernelGGL((fiona::attend_kernel<T, HD, true, true>), grid, dim3(256), 0, stream, P);
+  else if (vec) hipLaunchKernelGGL((fiona::attend_kernel<T, HD, true, false>), grid, dim3(256), 0, stream, P);
+  else hipLaunchKernelGGL((fiona::attend_kernel<T, HD, false, false>), grid, dim3(256), 0, stream, P);
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -100,11 +66,25 @@ int fiona_attention_create(const fiona_attention_desc *desc, fiona_attention **o
     delete H;
     return FIONA_ERR_HIP;
   }
+  for (uint64_t n = 1; n <= D.max_seq; ++n) {
+    const uint32_t splits = splits_of(D.max_length, chunk_of(D.max_length, n * D.n_kv * head_blocks(D)));
+    if (splits > 1) H->part_cap = std::max<uint64_t>(H->part_cap, n * splits);
+  }
+  const uint64_t bytes = H->part_cap * D.n_head * (D.head_dim + 2) * sizeof(float);
+  if (bytes && hipMalloc((void **)&H->part, bytes) != hipSuccess) {
+    (void)hipGetLastError();
+    delete H;
+    return FIONA_ERR_NOMEM;
+  }
   *out = H;
   return FIONA_OK;
 }
 
-void fiona_attention_destroy(fiona_attention *att) { delete att; }
+void fiona_attention_destroy(fiona_attention *att) {
+  if (!att) return;
+  if (att->part) (void)hipFree(att->part);
+  delete att;
+}
 
 int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cache, const fiona_attention_args *args,
                           hipStream_t stream) {
@@ -149,11 +129,30 @@ int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cach
   P.q_seq = A.q_seq, P.q_head = A.q_head, P.out_seq = A.out_seq, P.out_head = A.out_head, P.table_stride = A.table_stride;
   P.k_page = K.k_page, P.k_token = K.k_token, P.k_head = K.k_head;
   P.v_page = K.v_page, P.v_token = K.v_token, P.v_head = K.v_head;
-  P.n_head = D.n_head, P.group = D.n_head / D.n_kv, P.d = D.head_dim, P.page_size = D.page_size, P.n_pages = K.n_pages;
-  P.window = A.window, P.scale = A.scale, P.softcap = A.softcap;
+  P.n_head = D.n_head, P.group = D.n_head / D.n_kv, P.head_blocks = head_blocks(D), P.d = D.head_dim;
+  P.page_size = D.page_size, P.n_pages = K.n_pages, P.window = A.window, P.scale = A.scale, P.softcap = A.softcap;
+  if (D.page_size > 1) {
+    const uint32_t s = 32 - __builtin_clz(D.page_size - 1);   // 2^(s - 1) < page_size <= 2^s
+    P.page_mul = (uint32_t)((((uint64_t)1 << (31 + s)) + D.page_size - 1) / D.page_size);
+    P.page_shift = s - 1;
+  }
   P.max_length = (uint32_t)std::min<uint64_t>(D.max_length, (uint64_t)A.table_width * D.page_size);
+  // A window's keys start anywhere in a tile.
+  const uint64_t keys = A.window ? std::min<uint64_t>(P.max_length, (uint64_t)A.window + 32) : P.max_length;
+  P.chunk = chunk_of(keys, n * D.n_kv * P.head_blocks);
+  P.splits = splits_of(keys, P.chunk);
+  while (P.splits > 1 && n * P.splits > att->part_cap) P.chunk *= 2, P.splits = splits_of(keys, P.chunk);
+  P.part = att->part;
+  const dim3 grid(P.splits, D.n_kv * P.head_blocks, A.n_seq);
   with_type(D.type, [&](auto t) {
-    hipLaunchKernelGGL((fiona::attend_kernel<decltype(t)>), dim3(D.n_head, A.n_seq), dim3(256), 0, stream, P);
+    using T = decltype(t);
+    const bool vec = D.head_dim % fiona::kLaneElems<T> == 0 && rows_aligned16(in[0]) && rows_aligned16(in[1]) && rows_aligned16(in[2]);
+    const bool span = D.page_size % (uint32_t)fiona::kSpan<T> == 0;
+    if (D.head_dim <= 64) launch_split<T, 64>(P, vec, span, grid, stream);
+    else if (D.head_dim <= 128) launch_split<T, 128>(P, vec, span, grid, stream);
+    else launch_split<T, 256>(P, vec, span, grid, stream);
+    if (P.splits > 1)
+      hipLaunchKernelGGL(fiona::attend_join_kernel<T>, dim3(D.n_head, A.n_seq), dim3(256), 0, stream, P);
   });
   return hipGetLastError() == hipSuccess ? FIONA_OK : FIONA_ERR_HIP;
 }

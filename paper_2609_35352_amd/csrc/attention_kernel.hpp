@@ -1,0 +1,326 @@
+// Kernels of fiona_paged_attention.
+//
+// Softmax over a long axis in parts: a part with keys J has
+//     m_J = max s_j,  l_J = sum exp(s_j - m_J),  o_J = sum exp(s_j - m_J) v_j,
+// and two parts join as m = max(m_1, m_2), l = sum_i l_i exp(m_i - m), o alike;
+// so every key and value is read once, by whichever wavefront holds its part.
+// Exponentials are to base 2, with log2(e) in the scale.
+//
+// A workgroup takes one chunk of one sequence's keys for one key head and up
+// to 16 of the query heads that share it; its four wavefronts take tiles of
+// the chunk in turn.  Per tile of 32 keys (16 in 32 bits) a wavefront computes
+//     S^T = K Q^T     keys x heads: K's rows come from memory as fragments
+//     O^T += V^T P^T  dims x heads: P^T stays in the registers S^T came in
+// Key `row` of S^T's tile s stands for token (row / 4) * kSpan + 4 s + row % 4
+// of the tile, so that the kSpan tokens whose weights a lane ends up with are
+// consecutive, and are the tokens whose values the same lane loads, 16 bytes of
+// 16 lanes to a row: V^T's fragments are picked from the tokens' words in
+// registers (a lane's dims u of each token), and neither K, V nor P passes
+// through LDS.  Softmax weights are rounded to the values' type (at most 1, so
+// an error of at most half a unit of the sum); their sum l uses them unrounded.
+//
+// What bounds it: the cache is read once, and 2 or 4 operations per byte and
+// query head are far below the matrix cores' rate.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "mma.hpp"
+
+namespace fiona {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct AttendParams {
+  const void *q, *kc, *vc;
+  void *out;
+  float *lse;
+  const int32_t *table, *lengths;
+  float *part;                                  // [n_seq][n_head][splits][d + 2]: o, then m and l
+  uint64_t q_seq, q_head, out_seq, out_head, table_stride;
+  uint64_t k_page, k_token, k_head, v_page, v_token, v_head;
+  uint32_t n_head, group, head_blocks, d, page_size, n_pages, window, max_length;
+  uint32_t page_mul, page_shift;                // token / page_size (see page_of)
+  uint32_t chunk, splits;
+  float scale, softcap;
+};
+
+// token / page_size for token < 2^31: (token * page_mul) >> (32 + page_shift)
+// with page_mul = ceil(2^(32 + page_shift) / page_size), 2^page_shift <=
+// page_size / 2 < 2^(page_shift + 1); pages of one token have page_mul 0.
+__device__ __forceinline__ uint32_t page_of(const AttendParams &P, uint32_t token) {
+  return P.page_mul ? __umulhi(token, P.page_mul) >> P.page_shift : token;
+}
+
+// The tokens sequence s attends to, [first, n).
+__device__ __forceinline__ void key_range(const AttendParams &P, uint32_t s, int32_t &first, int32_t &n) {
+  n = P.lengths[s];
+  n = n < 0 ? 0 : (uint32_t)n > P.max_length ? (int32_t)P.max_length : n;
+  first = P.window && (uint32_t)n > P.window ? n - (int32_t)P.window : 0;
+}
+
+template <typename T>
+constexpr int32_t kTileKeys = sizeof(T) == 2 ? 32 : 16;
+template <typename T>
+constexpr int32_t kTiles = kTileKeys<T> / 16;     // score tiles of 16 keys
+template <typename T>
+constexpr int32_t kSpan = 4 * kTiles<T>;          // consecutive tokens of a lane
+
+// D: head size rounded up.  VEC: rows in 16-byte pieces.  SPAN: pages are
+// multiples of kSpan tokens, so that a span lies in one page.
+template <typename T, int D, bool VEC, bool SPAN>
+__global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
+  constexpr int TK = kTileKeys<T>, RT = kTiles<T>, SP = kSpan<T>;
+  constexpr int E = kLaneElems<T>, KF = D / kFragElems<T>;            // K and Q fragments of a row
+  constexpr int VW = D / 16 < E ? D / 16 : E, VL = D / (16 * VW);     // a lane's dims of a value row, and pieces
+  constexpr int VN = VW * sizeof(T) / 4, OT = D / 16;
+  constexpr int DC = D < 128 ? D : 128;                               // columns joined at a time
+  __shared__ float sm[4][16], sl[4][16], so[4][16][DC + 4];
+
+  const uint32_t split = blockIdx.x, kv = blockIdx.y / P.head_blocks, hb = blockIdx.y % P.head_blocks, seq = blockIdx.z;
+  const uint32_t lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+  int32_t first, n;
+  key_range(P, seq, first, n);
+  const int32_t start = first / TK * TK + (int32_t)(split * P.chunk);
+  const int32_t end = n - start < (int32_t)P.chunk ? n : start + (int32_t)P.chunk;
+  if (start >= n && split > 0) return;                                // (the join reads the parts below n only)
+
+  const uint32_t heads = P.group - hb * 16 < 16 ? P.group - hb * 16 : 16, head0 = kv * P.group + hb * 16;
+  const int d = (int)P.d;
+  u4 q[KF];
+  {
+    const T *qp = (const T *)P.q + seq * P.q_seq + (uint64_t)(head0 + col) * P.q_head;
+#pragma unroll
+    for (int f = 0; f < KF; ++f) {
+      uint32_t v[4];
+      const int at = f * (int)kFragElems<T> + (int)grp * E;
+      load_row<T, E, VEC>(qp + at, col < heads ? d - at : 0, v);
+      q[f] = (u4){v[0], v[1], v[2], v[3]};
+    }
+  }
+  f4 o[OT];
+#pragma unroll
+  for (int t = 0; t < OT; ++t) o[t] = (f4){0, 0, 0, 0};
+  float m = -INFINITY, l = 0;
+  const int32_t *table = P.table + seq * P.table_stride;
+  const T *kb = (const T *)P.kc + kv * P.k_head, *vb = (const T *)P.vc + kv * P.v_head;
+  const float scale2 = P.scale * kLog2e;
+
+  // The row of token `tok` in a cache, or null where there is none.
+  auto row_at = [&](const T *base, uint64_t page_stride, uint64_t token_stride, int32_t tok) -> const T * {
+    if (tok < first || tok >= end) return nullptr;
+    const uint32_t p = page_of(P, (uint32_t)tok);
+    const int32_t page = table[p];
+    if ((uint32_t)page >= P.n_pages) return nullptr;
+    return base + (uint64_t)(uint32_t)page * page_stride + ((uint32_t)tok - p * P.page_size) * token_stride;
+  };
+  // The page of the span that starts at token `tok`, and the place of tok in it.
+  auto span_at = [&](int32_t tok, int32_t &page, uint32_t &place) {
+    page = -1, place = 0;
+    if (tok + SP <= first || tok >= end) return;
+    const uint32_t p = page_of(P, (uint32_t)tok);
+    page = table[p];
+    place = (uint32_t)tok - p * P.page_size;
+  };
+
+  u4 k[RT][KF];
+  uint32_t v[SP][VL][VN];
+  int32_t kpage, vpage;
+  uint32_t kplace, vplace;
+  auto load_k = [&](int32_t base) {
+#pragma unroll
+    for (int s = 0; s < RT; ++s) {
+      const int32_t tok = base + (int32_t)(col / 4) * SP + 4 * s + (int32_t)(col % 4);
+      const T *row;
+      if constexpr (SPAN)
+        row = tok >= first && tok < end && (uint32_t)kpage < P.n_pages
+                  ? kb + (uint64_t)(uint32_t)kpage * P.k_page + (kplace + 4 * s + col % 4) * P.k_token
+                  : nullptr;
+      else
+        row = row_at(kb, P.k_page, P.k_token, tok);
+#pragma unroll
+      for (int f = 0; f < KF; ++f) {
+        uint32_t x[4];
+        const int at = f * (int)kFragElems<T> + (int)grp * E;
+        load_row<T, E, VEC>(row + at, row ? d - at : 0, x);
+        k[s][f] = (u4){x[0], x[1], x[2], x[3]};
+      }
+    }
+  };
+
+  const int32_t step = 4 * TK;
+  int32_t base = start + (int32_t)w * TK;
+  if (SPAN) {
+    span_at(base + (int32_t)(col / 4) * SP, kpage, kplace);
+    span_at(base + (int32_t)grp * SP, vpage, vplace);
+  }
+  if (base < end) load_k(base);
+  for (; base < end; base += step) {
+    // Values of this tile, and which of the lane's tokens count.
+    bool live[SP];
+#pragma unroll
+    for (int j = 0; j < SP; ++j) {
+      const int32_t tok = base + (int32_t)grp * SP + j;
+      const T *row;
+      if constexpr (SPAN) {
+        live[j] = tok >= first && tok < end && (uint32_t)vpage < P.n_pages;
+        row = vb + (uint64_t)(uint32_t)vpage * P.v_page + (vplace + j) * P.v_token;
+      } else {
+        row = row_at(vb, P.v_page, P.v_token, tok);
+        live[j] = row != nullptr;
+      }
+#pragma unroll
+      for (int x = 0; x < VL; ++x) {
+        const int at = x * 16 * VW + (int)col * VW;
+        load_row<T, VW, VEC>(row + at, live[j] ? d - at : 0, v[j][x]);
+      }
+    }
+    if (SPAN) {
+      span_at(base + step + (int32_t)(col / 4) * SP, kpage, kplace);
+      span_at(base + step + (int32_t)grp * SP, vpage, vplace);
+    }
+
+    float sc[SP];
+    float top = -INFINITY;
+#pragma unroll
+    for (int s = 0; s < RT; ++s) {
+      f4 acc = (f4){0, 0, 0, 0};
+#pragma unroll
+      for (int f = 0; f < KF; ++f) acc = mma<T>(k[s][f], q[f], acc);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x = acc[i] * scale2;
+        if (P.softcap > 0) {
+          // cap tanh(s / cap) = cap (1 - 2 / (exp(2 s / cap) + 1)), in units of log2(e)
+          const float e = __builtin_amdgcn_exp2f(2.f * kLog2e * (acc[i] * P.scale / P.softcap));
+          x = P.softcap * kLog2e * (1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f));
+        }
+        sc[4 * s + i] = live[4 * s + i] ? x : -INFINITY;
+        top = fmaxf(top, sc[4 * s + i]);
+      }
+    }
+    if (base + step < end) load_k(base + step);
+
+    const float mn = fmaxf(m, column_max(top)), ms = mn == -INFINITY ? 0.f : mn;
+    if (__any(mn > m)) {
+      const float keep = __builtin_amdgcn_exp2f(m - ms);
+      l *= keep;
+#pragma unroll
+      for (int t = 0; t < OT; ++t) o[t] *= keep;
+      m = mn;
+    }
+#pragma unroll
+    for (int j = 0; j < SP; ++j) {
+      sc[j] = __builtin_amdgcn_exp2f(sc[j] - ms);
+      l += sc[j];
+    }
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int x = 0; x < VL; ++x)
+#pragma unroll
+        for (int u = 0; u < VW; ++u)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            o[x * VW + u] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, v[j][x][u]), sc[j], o[x * VW + u], 0, 0, 0);
+    } else {
+      u4 p;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[j] = pack2<T>(sc[2 * j], sc[2 * j + 1]);
+#pragma unroll
+      for (int x = 0; x < VL; ++x)
+#pragma unroll
+        for (int u = 0; u < VW; ++u) {
+          u4 a;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            a[j] = u & 1 ? pair_high(v[2 * j][x][u / 2], v[2 * j + 1][x][u / 2]) : pair_low(v[2 * j][x][u / 2], v[2 * j + 1][x][u / 2]);
+          o[x * VW + u] = mma<T>(a, p, o[x * VW + u]);
+        }
+    }
+  }
+
+  // The four wavefronts' parts, joined DC columns at a time.
+  l = column_sum(l);
+  if (grp == 0) sm[w][col] = m, sl[w][col] = l;
+  const uint32_t oh = threadIdx.x >> 4, oc = threadIdx.x & 15;   // this thread's head, and its first column / (DC / 16)
+  const uint32_t head = head0 + oh;
+#pragma unroll
+  for (int c0 = 0; c0 < D; c0 += DC) {
+    if (c0) __syncthreads();
+#pragma unroll
+    for (int x = 0; x < VL; ++x) {
+      if (x * 16 * VW < c0 || x * 16 * VW >= c0 + DC) continue;
+#pragma unroll
+      for (int u = 0; u < VW; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) so[w][col][x * 16 * VW - c0 + (grp * 4 + i) * VW + u] = o[x * VW + u][i];
+    }
+    __syncthreads();
+    float f[4], mt = fmaxf(fmaxf(sm[0][oh], sm[1][oh]), fmaxf(sm[2][oh], sm[3][oh])), lt = 0;
+    const float ms = mt == -INFINITY ? 0.f : mt;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[i] = __builtin_amdgcn_exp2f(sm[i][oh] - ms);
+      lt += sl[i][oh] * f[i];
+    }
+    if (oh >= heads) continue;
+    const float inv = lt == 0 ? 0.f : 1.f / lt;
+    float *part = P.part + ((uint64_t)(seq * P.n_head + head) * P.splits + split) * (P.d + 2);
+    T *out = (T *)P.out + seq * P.out_seq + head * P.out_head;
+#pragma unroll
+    for (int e = 0; e < DC / 16; ++e) {
+      const uint32_t c = oc + 16 * e;
+      float x = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x += so[i][oh][c] * f[i];
+      if (c0 + c >= P.d) continue;
+      if (P.splits == 1) out[c0 + c] = (T)(lt == 0 ? 0.f : x * inv);
+      else part[c0 + c] = x;
+    }
+    if (oc == 0 && c0 == 0) {
+      if (P.splits > 1) part[P.d] = mt, part[P.d + 1] = lt;
+      else if (P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms + __builtin_amdgcn_logf(lt));
+    }
+  }
+}
+
+// The parts of one sequence and head: wavefront w takes parts w, w + 4, ...,
+// each lane up to four columns, and the four are joined as above.
+template <typename T>
+__global__ void __launch_bounds__(256) attend_join_kernel(AttendParams P) {
+  __shared__ float sm[4], sl[4], so[4][256];
+  const uint32_t head = blockIdx.x, seq = blockIdx.y, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int32_t first, n;
+  key_range(P, seq, first, n);
+  const int32_t start = first / kTileKeys<T> * kTileKeys<T>;
+  const uint32_t used = n > start ? ((uint32_t)(n - start) + P.chunk - 1) / P.chunk : 0;
+  const float *part = P.part + (uint64_t)(seq * P.n_head + head) * P.splits * (P.d + 2);
+  float m = -INFINITY, l = 0, o[4] = {0, 0, 0, 0};
+  for (uint32_t i = w; i < used; i += 4) {
+    const float *p = part + (uint64_t)i * (P.d + 2);
+    const float mi = p[P.d], li = p[P.d + 1];
+    const float mn = fmaxf(m, mi), ms = mn == -INFINITY ? 0.f : mn;
+    const float a = __builtin_amdgcn_exp2f(m - ms), b = __builtin_amdgcn_exp2f(mi - ms);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (lane + 64 * e < P.d) o[e] = o[e] * a + p[lane + 64 * e] * b;
+    l = l * a + li * b;
+    m = mn;
+  }
+  if (lane == 0) sm[w] = m, sl[w] = l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) so[w][lane + 64 * e] = o[e];
+  __syncthreads();
+  const float mt = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])), ms = mt == -INFINITY ? 0.f : mt;
+  float lt = 0, x = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float f = __builtin_amdgcn_exp2f(sm[i] - ms);
+    lt += sl[i] * f;
+    x += so[i][threadIdx.x] * f;
+  }
+  if (threadIdx.x < P.d) ((T *)P.out)[seq * P.out_seq + head * P.out_head + threadIdx.x] = (T)(lt == 0 ? 0.f : x / lt);
+  if (threadIdx.x == 0 && P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms + __builtin_amdgcn_logf(lt));
+}
+
+}  // namespace fiona
