@@ -130,7 +130,9 @@ int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cach
   P.k_page = K.k_page, P.k_token = K.k_token, P.k_head = K.k_head;
   P.v_page = K.v_page, P.v_token = K.v_token, P.v_head = K.v_head;
   P.n_head = D.n_head, P.group = D.n_head / D.n_kv, P.head_blocks = head_blocks(D), P.d = D.head_dim;
-  P.page_size = D.page_size, P.n_pages = K.n_pages, P.window = A.window, P.scale = A.scale, P.softcap = A.softcap;
+  P.page_size = D.page_size, P.n_pages = K.n_pages, P.window = A.window;
+  P.scale = A.scale * fiona::kLog2e;
+  if (A.softcap > 0) P.cap_in = 2.f * fiona::kLog2e * A.scale / A.softcap, P.cap_out = A.softcap * fiona::kLog2e;
   if (D.page_size > 1) {
     const uint32_t s = 32 - __builtin_clz(D.page_size - 1);   // 2^(s - 1) < page_size <= 2^s
     P.page_mul = (uint32_t)((((uint64_t)1 << (31 + s)) + D.page_size - 1) / D.page_size);

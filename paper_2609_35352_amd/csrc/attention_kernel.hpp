@@ -42,7 +42,8 @@ struct AttendParams {
   uint32_t n_head, group, head_blocks, d, page_size, n_pages, window, max_length;
   uint32_t page_mul, page_shift;                // token / page_size (see page_of)
   uint32_t chunk, splits;
-  float scale, softcap;
+  float scale;                                  // of a score, times log2(e)
+  float cap_in, cap_out;                        // 2 log2(e) scale / softcap, softcap log2(e); 0 without one
 };
 
 // token / page_size for token < 2^31: (token * page_mul) >> (32 + page_shift)
@@ -104,45 +105,44 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
   float m = -INFINITY, l = 0;
   const int32_t *table = P.table + seq * P.table_stride;
   const T *kb = (const T *)P.kc + kv * P.k_head, *vb = (const T *)P.vc + kv * P.v_head;
-  const float scale2 = P.scale * kLog2e;
 
-  // The row of token `tok` in a cache, or null where there is none.
-  auto row_at = [&](const T *base, uint64_t page_stride, uint64_t token_stride, int32_t tok) -> const T * {
-    if (tok < first || tok >= end) return nullptr;
-    const uint32_t p = page_of(P, (uint32_t)tok);
-    const int32_t page = table[p];
-    if ((uint32_t)page >= P.n_pages) return nullptr;
-    return base + (uint64_t)(uint32_t)page * page_stride + ((uint32_t)tok - p * P.page_size) * token_stride;
-  };
-  // The page of the span that starts at token `tok`, and the place of tok in it.
-  auto span_at = [&](int32_t tok, int32_t &page, uint32_t &place) {
-    page = -1, place = 0;
-    if (tok + SP <= first || tok >= end) return;
+  // Loads are issued without branches, so that the waits between them are for
+  // the data that is used next: where there is no row they read the query's.
+  const T *nowhere = (const T *)P.q + seq * P.q_seq + (uint64_t)head0 * P.q_head;
+  // The page and place of token `tok`, which lies in the table up to `end`.
+  auto locate = [&](int32_t tok, int32_t &page, uint32_t &place) {
+    tok = tok < end ? tok : end - 1;
     const uint32_t p = page_of(P, (uint32_t)tok);
     page = table[p];
     place = (uint32_t)tok - p * P.page_size;
   };
+  auto counts = [&](int32_t tok, int32_t page) {
+    return (bool)((int)(tok >= first) & (int)(tok < end) & (int)((uint32_t)page < P.n_pages));
+  };
+  auto row_of = [&](const T *base, uint64_t page_stride, uint64_t token_stride, int32_t page, uint32_t place, bool ok) {
+    const uint64_t row = (uint64_t)(base + (uint64_t)(uint32_t)page * page_stride + place * token_stride);
+    return (const T *)(ok ? row : (uint64_t)nowhere);
+  };
 
   u4 k[RT][KF];
   uint32_t v[SP][VL][VN];
-  int32_t kpage, vpage;
-  uint32_t kplace, vplace;
+  int32_t kpage = -1, vpage = -1;
+  uint32_t kplace = 0, vplace = 0;
   auto load_k = [&](int32_t base) {
 #pragma unroll
     for (int s = 0; s < RT; ++s) {
       const int32_t tok = base + (int32_t)(col / 4) * SP + 4 * s + (int32_t)(col % 4);
-      const T *row;
-      if constexpr (SPAN)
-        row = tok >= first && tok < end && (uint32_t)kpage < P.n_pages
-                  ? kb + (uint64_t)(uint32_t)kpage * P.k_page + (kplace + 4 * s + col % 4) * P.k_token
-                  : nullptr;
-      else
-        row = row_at(kb, P.k_page, P.k_token, tok);
+      int32_t page = kpage;
+      uint32_t place = kplace + 4 * s + col % 4;
+      if constexpr (!SPAN) locate(tok, page, place);
+      const bool ok = counts(tok, page);
+      const T *row = row_of(kb, P.k_page, P.k_token, page, place, ok);
 #pragma unroll
       for (int f = 0; f < KF; ++f) {
         uint32_t x[4];
         const int at = f * (int)kFragElems<T> + (int)grp * E;
-        load_row<T, E, VEC>(row + at, row ? d - at : 0, x);
+        if constexpr (VEC) load_row<T, E, true>(row + (at < d ? at : 0), 1, x);
+        else load_row<T, E, false>(row + at, ok ? d - at : 0, x);
         k[s][f] = (u4){x[0], x[1], x[2], x[3]};
       }
     }
@@ -150,56 +150,82 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
 
   const int32_t step = 4 * TK;
   int32_t base = start + (int32_t)w * TK;
-  if (SPAN) {
-    span_at(base + (int32_t)(col / 4) * SP, kpage, kplace);
-    span_at(base + (int32_t)grp * SP, vpage, vplace);
+  if (base < end) {
+    if (SPAN) {
+      locate(base + (int32_t)(col / 4) * SP, kpage, kplace);
+      locate(base + (int32_t)grp * SP, vpage, vplace);
+    }
+    load_k(base);
   }
-  if (base < end) load_k(base);
   for (; base < end; base += step) {
+    // The next tile's pages first: its keys are issued once they are there,
+    // without waiting for this tile's values, which come after them.
+    int32_t kpage_next = -1, vpage_next = -1;
+    uint32_t kplace_next = 0, vplace_next = 0;
+    if (SPAN) {
+      locate(base + step + (int32_t)(col / 4) * SP, kpage_next, kplace_next);
+      locate(base + step + (int32_t)grp * SP, vpage_next, vplace_next);
+    }
     // Values of this tile, and which of the lane's tokens count.
-    bool live[SP];
+    bool live[SP], whole = true;
 #pragma unroll
     for (int j = 0; j < SP; ++j) {
       const int32_t tok = base + (int32_t)grp * SP + j;
-      const T *row;
-      if constexpr (SPAN) {
-        live[j] = tok >= first && tok < end && (uint32_t)vpage < P.n_pages;
-        row = vb + (uint64_t)(uint32_t)vpage * P.v_page + (vplace + j) * P.v_token;
-      } else {
-        row = row_at(vb, P.v_page, P.v_token, tok);
-        live[j] = row != nullptr;
-      }
+      int32_t page = vpage;
+      uint32_t place = vplace + j;
+      if constexpr (!SPAN) locate(tok, page, place);
+      live[j] = counts(tok, page);
+      whole &= live[j];
+      const T *row = row_of(vb, P.v_page, P.v_token, page, place, live[j]);
 #pragma unroll
       for (int x = 0; x < VL; ++x) {
         const int at = x * 16 * VW + (int)col * VW;
-        load_row<T, VW, VEC>(row + at, live[j] ? d - at : 0, v[j][x]);
+        if constexpr (VEC) load_row<T, VW, true>(row + (at < d ? at : 0), 1, v[j][x]);
+        else load_row<T, VW, false>(row + at, live[j] ? d - at : 0, v[j][x]);
       }
     }
-    if (SPAN) {
-      span_at(base + step + (int32_t)(col / 4) * SP, kpage, kplace);
-      span_at(base + step + (int32_t)grp * SP, vpage, vplace);
-    }
+    whole = __all(whole);
+    kpage = kpage_next, kplace = kplace_next, vpage = vpage_next, vplace = vplace_next;
 
-    float sc[SP];
-    float top = -INFINITY;
+    // Dims from d on hold the row's first ones: their queries are zero, but not an infinite key times zero.
+    if (VEC && d < D) {
+#pragma unroll
+      for (int s = 0; s < RT; ++s)
+#pragma unroll
+        for (int f = 0; f < KF; ++f)
+          if (f * (int)kFragElems<T> + (int)grp * E >= d) k[s][f] = (u4){0, 0, 0, 0};
+    }
+    f4 acc[RT];
 #pragma unroll
     for (int s = 0; s < RT; ++s) {
-      f4 acc = (f4){0, 0, 0, 0};
+      acc[s] = (f4){0, 0, 0, 0};
 #pragma unroll
-      for (int f = 0; f < KF; ++f) acc = mma<T>(k[s][f], q[f], acc);
+      for (int f = 0; f < KF; ++f) acc[s] = mma<T>(k[s][f], q[f], acc[s]);
+    }
+    load_k(base + step);
+
+    float sc[SP];
+    if (P.cap_out > 0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float x = acc[i] * scale2;
-        if (P.softcap > 0) {
-          // cap tanh(s / cap) = cap (1 - 2 / (exp(2 s / cap) + 1)), in units of log2(e)
-          const float e = __builtin_amdgcn_exp2f(2.f * kLog2e * (acc[i] * P.scale / P.softcap));
-          x = P.softcap * kLog2e * (1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f));
-        }
-        sc[4 * s + i] = live[4 * s + i] ? x : -INFINITY;
-        top = fmaxf(top, sc[4 * s + i]);
+      for (int j = 0; j < SP; ++j)   // cap tanh(s / cap) = cap (1 - 2 / (exp(2 s / cap) + 1)), in units of log2(e)
+        sc[j] = P.cap_out * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(P.cap_in * acc[j / 4][j % 4]) + 1.f));
+    } else {
+#pragma unroll
+      for (int j = 0; j < SP; ++j) sc[j] = acc[j / 4][j % 4] * P.scale;
+    }
+    if (!whole) {   // places that do not count hold anything: no score, and no value that zero would not silence
+#pragma unroll
+      for (int j = 0; j < SP; ++j) {
+        sc[j] = live[j] ? sc[j] : -INFINITY;
+#pragma unroll
+        for (int x = 0; x < VL; ++x)
+#pragma unroll
+          for (int i = 0; i < VN; ++i) v[j][x][i] = live[j] ? v[j][x][i] : 0;
       }
     }
-    if (base + step < end) load_k(base + step);
+    float top = sc[0];
+#pragma unroll
+    for (int j = 1; j < SP; ++j) top = fmaxf(top, sc[j]);
 
     const float mn = fmaxf(m, column_max(top)), ms = mn == -INFINITY ? 0.f : mn;
     if (__any(mn > m)) {
