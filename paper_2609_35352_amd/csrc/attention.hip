@@ -145,7 +145,7 @@ int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cach
   P.splits = splits_of(keys, P.chunk);
   while (P.splits > 1 && n * P.splits > att->part_cap) P.chunk *= 2, P.splits = splits_of(keys, P.chunk);
   P.part = att->part;
-  const dim3 grid(P.splits, D.n_kv * P.head_blocks, A.n_seq);
+  const dim3 grid(D.n_kv * P.head_blocks, P.splits, A.n_seq);
   with_type(D.type, [&](auto t) {
     using T = decltype(t);
     const bool vec = D.head_dim % fiona::kLaneElems<T> == 0 && rows_aligned16(in[0]) && rows_aligned16(in[1]) && rows_aligned16(in[2]);

@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
   constexpr int DC = D < 128 ? D : 128;                               // columns joined at a time
   __shared__ float sm[4][16], sl[4][16], so[4][16][DC + 4];
 
-  const uint32_t split = blockIdx.x, kv = blockIdx.y / P.head_blocks, hb = blockIdx.y % P.head_blocks, seq = blockIdx.z;
+  const uint32_t split = blockIdx.y, kv = blockIdx.x / P.head_blocks, hb = blockIdx.x % P.head_blocks, seq = blockIdx.z;
   const uint32_t lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
   int32_t first, n;
   key_range(P, seq, first, n);
