@@ -21,7 +21,8 @@ struct fiona_attention {
 
 namespace {
 
-constexpr uint32_t kMinChunk = 512, kMaxChunk = 1024, kMaxSplits = 128, kWorkgroups = 1024;
+constexpr uint32_t kMinChunk = 512, kMaxChunk = 1024, kWorkgroups = 1024;
+using fiona::kMaxSplits;
 
 // Keys of one workgroup's chunk for calls over up to `keys` keys: few enough
 // that the sequences and key heads fill the GPU, at most kMaxChunk so that
@@ -139,12 +140,13 @@ int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cach
     P.page_shift = s - 1;
   }
   P.max_length = (uint32_t)std::min<uint64_t>(D.max_length, (uint64_t)A.table_width * D.page_size);
+  if (K.n_pages == 0) P.max_length = 0;
   // A window's keys start anywhere in a tile.
   const uint64_t keys = A.window ? std::min<uint64_t>(P.max_length, (uint64_t)A.window + 32) : P.max_length;
   P.chunk = chunk_of(keys, n * D.n_kv * P.head_blocks);
   P.splits = splits_of(keys, P.chunk);
   while (P.splits > 1 && n * P.splits > att->part_cap) P.chunk *= 2, P.splits = splits_of(keys, P.chunk);
-  P.part = att->part;
+  P.part_ml = att->part, P.part = att->part + 2 * att->part_cap * D.n_head;
   const dim3 grid(D.n_kv * P.head_blocks, P.splits, A.n_seq);
   with_type(D.type, [&](auto t) {
     using T = decltype(t);
@@ -153,8 +155,9 @@ int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cach
     if (D.head_dim <= 64) launch_split<T, 64>(P, vec, span, grid, stream);
     else if (D.head_dim <= 128) launch_split<T, 128>(P, vec, span, grid, stream);
     else launch_split<T, 256>(P, vec, span, grid, stream);
-    if (P.splits > 1)
-      hipLaunchKernelGGL(fiona::attend_join_kernel<T>, dim3(D.n_head, A.n_seq), dim3(256), 0, stream, P);
+    const dim3 rows(D.n_head, A.n_seq);
+    if (P.splits > 16) hipLaunchKernelGGL((fiona::attend_join_kernel<T, 4>), rows, dim3(1024), 0, stream, P);
+    else if (P.splits > 1) hipLaunchKernelGGL((fiona::attend_join_kernel<T, 1>), rows, dim3(256), 0, stream, P);
   });
   return hipGetLastError() == hipSuccess ? FIONA_OK : FIONA_ERR_HIP;
 }

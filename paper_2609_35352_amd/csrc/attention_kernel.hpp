@@ -9,15 +9,18 @@
 // A workgroup takes one chunk of one sequence's keys for one key head and up
 // to 16 of the query heads that share it; its four wavefronts take tiles of
 // the chunk in turn.  Per tile of 32 keys (16 in 32 bits) a wavefront computes
-//     S^T = K Q^T     keys x heads: K's rows come from memory as fragments
+//     S^T = K Q^T     keys x heads
 //     O^T += V^T P^T  dims x heads: P^T stays in the registers S^T came in
-// Key `row` of S^T's tile s stands for token (row / 4) * kSpan + 4 s + row % 4
-// of the tile, so that the kSpan tokens whose weights a lane ends up with are
-// consecutive, and are the tokens whose values the same lane loads, 16 bytes of
-// 16 lanes to a row: V^T's fragments are picked from the tokens' words in
-// registers (a lane's dims u of each token), and neither K, V nor P passes
-// through LDS.  Softmax weights are rounded to the values' type (at most 1, so
-// an error of at most half a unit of the sum); their sum l uses them unrounded.
+// Both caches are read whole rows at a time, 16 bytes of 16 lanes to a row.
+// K's rows pass through LDS, private to the wavefront, to become fragments:
+// read as fragments from memory (64 bytes of 16 rows per instruction) the same
+// bytes took 168 to 184 us where rows take 139 to 158 (944 MB of pages, loads alone,
+// nontemporal; a plain stream takes 135).  V^T's fragments are picked from the tokens'
+// words in registers.  Key `row` of S^T's tile s stands for token (row / 4) *
+// kSpan + 4 s + row % 4 of the tile, so that the kSpan tokens whose weights a
+// lane ends up with are consecutive, and are the tokens whose rows it loads.
+// Softmax weights are rounded to the values' type (at most 1, so an error of at
+// most half a unit of the sum); their sum l uses them unrounded.
 //
 // What bounds it: the cache is read once, and 2 or 4 operations per byte and
 // query head are far below the matrix cores' rate.
@@ -25,10 +28,12 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "fiona.h"
 #include "mma.hpp"
 
 namespace fiona {
 
+constexpr uint32_t kMaxSplits = 128;   // parts of one sequence
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttendParams {
@@ -36,7 +41,7 @@ struct AttendParams {
   void *out;
   float *lse;
   const int32_t *table, *lengths;
-  float *part;                                  // [n_seq][n_head][splits][d + 2]: o, then m and l
+  float *part, *part_ml;                        // [n_seq][n_head][splits][d]: o, and [..][2]: m and l
   uint64_t q_seq, q_head, out_seq, out_head, table_stride;
   uint64_t k_page, k_token, k_head, v_page, v_token, v_head;
   uint32_t n_head, group, head_blocks, d, page_size, n_pages, window, max_length;
@@ -70,13 +75,22 @@ constexpr int32_t kSpan = 4 * kTiles<T>;          // consecutive tokens of a lan
 // D: head size rounded up.  VEC: rows in 16-byte pieces.  SPAN: pages are
 // multiples of kSpan tokens, so that a span lies in one page.
 template <typename T, int D, bool VEC, bool SPAN>
-__global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
+__global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendParams P) {
   constexpr int TK = kTileKeys<T>, RT = kTiles<T>, SP = kSpan<T>;
   constexpr int E = kLaneElems<T>, KF = D / kFragElems<T>;            // K and Q fragments of a row
   constexpr int VW = D / 16 < E ? D / 16 : E, VL = D / (16 * VW);     // a lane's dims of a value row, and pieces
   constexpr int VN = VW * sizeof(T) / 4, OT = D / 16;
   constexpr int DC = D < 128 ? D : 128;                               // columns joined at a time
-  __shared__ float sm[4][16], sl[4][16], so[4][16][DC + 4];
+  // A wavefront's tile of K, rows 16 bytes apart from a multiple of the banks;
+  // later the four parts of O.
+  constexpr int LPR = D / E < 16 ? D / E : 16, PC = D / (E * LPR), KI = TK * LPR / 64;   // lanes of a key's row, pieces, rows of a lane
+  constexpr int KROW = D * (int)sizeof(T) + 16;
+  union alignas(16) Shared {
+    uint8_t k[4][TK][KROW];
+    float o[4][16][DC + 4];
+  };
+  __shared__ float sm[4][16], sl[4][16];
+  __shared__ Shared sh;
 
   const uint32_t split = blockIdx.y, kv = blockIdx.x / P.head_blocks, hb = blockIdx.x % P.head_blocks, seq = blockIdx.z;
   const uint32_t lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
@@ -107,8 +121,8 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
   const T *kb = (const T *)P.kc + kv * P.k_head, *vb = (const T *)P.vc + kv * P.v_head;
 
   // Loads are issued without branches, so that the waits between them are for
-  // the data that is used next: where there is no row they read the query's.
-  const T *nowhere = (const T *)P.q + seq * P.q_seq + (uint64_t)head0 * P.q_head;
+  // the data that is used next: a token that does not count is read from its
+  // page all the same, or from page 0 where the table has none.
   // The page and place of token `tok`, which lies in the table up to `end`.
   auto locate = [&](int32_t tok, int32_t &page, uint32_t &place) {
     tok = tok < end ? tok : end - 1;
@@ -116,34 +130,33 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
     page = table[p];
     place = (uint32_t)tok - p * P.page_size;
   };
-  auto counts = [&](int32_t tok, int32_t page) {
-    return (bool)((int)(tok >= first) & (int)(tok < end) & (int)((uint32_t)page < P.n_pages));
-  };
-  auto row_of = [&](const T *base, uint64_t page_stride, uint64_t token_stride, int32_t page, uint32_t place, bool ok) {
-    const uint64_t row = (uint64_t)(base + (uint64_t)(uint32_t)page * page_stride + place * token_stride);
-    return (const T *)(ok ? row : (uint64_t)nowhere);
+  auto row_of = [&](const T *base, uint64_t page_stride, uint64_t token_stride, int32_t page, uint32_t place) {
+    return base + ((uint32_t)page < P.n_pages ? (uint64_t)(uint32_t)page * page_stride : 0) + place * token_stride;
   };
 
-  u4 k[RT][KF];
+  u4 k[KI][PC];
   uint32_t v[SP][VL][VN];
-  int32_t kpage = -1, vpage = -1;
-  uint32_t kplace = 0, vplace = 0;
+  int32_t page = 0;          // (SPAN: of the lane's span in the tile whose keys are loaded)
+  uint32_t place = 0;
+  // Keys of the lane: token grp * SP + kfirst + i of the tile, dims from kat on in steps of 16 E.
+  const int kfirst = LPR < 16 ? (int)(lane / LPR % (16 / LPR)) * KI : 0, kat = (int)(lane % LPR) * E;
   auto load_k = [&](int32_t base) {
+    const T *row = row_of(kb, P.k_page, P.k_token, page, place + kfirst);
 #pragma unroll
-    for (int s = 0; s < RT; ++s) {
-      const int32_t tok = base + (int32_t)(col / 4) * SP + 4 * s + (int32_t)(col % 4);
-      int32_t page = kpage;
-      uint32_t place = kplace + 4 * s + col % 4;
-      if constexpr (!SPAN) locate(tok, page, place);
-      const bool ok = counts(tok, page);
-      const T *row = row_of(kb, P.k_page, P.k_token, page, place, ok);
+    for (int i = 0; i < KI; ++i) {
+      if constexpr (!SPAN) {
+        locate(base + (int32_t)grp * SP + kfirst + i, page, place);
+        row = row_of(kb, P.k_page, P.k_token, page, place);
+      } else if (i) {
+        row += P.k_token;
+      }
 #pragma unroll
-      for (int f = 0; f < KF; ++f) {
-        uint32_t x[4];
-        const int at = f * (int)kFragElems<T> + (int)grp * E;
-        if constexpr (VEC) load_row<T, E, true>(row + (at < d ? at : 0), 1, x);
-        else load_row<T, E, false>(row + at, ok ? d - at : 0, x);
-        k[s][f] = (u4){x[0], x[1], x[2], x[3]};
+      for (int x = 0; x < PC; ++x) {
+        uint32_t r[4];
+        const int at = x * 16 * E + kat;
+        if constexpr (VEC) load_row<T, E, true>(row + (at < d ? at : 0), 1, r);
+        else load_row<T, E, false>(row + at, d - at, r);
+        k[i][x] = (u4){r[0], r[1], r[2], r[3]};
       }
     }
   };
@@ -151,58 +164,59 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
   const int32_t step = 4 * TK;
   int32_t base = start + (int32_t)w * TK;
   if (base < end) {
-    if (SPAN) {
-      locate(base + (int32_t)(col / 4) * SP, kpage, kplace);
-      locate(base + (int32_t)grp * SP, vpage, vplace);
-    }
+    if (SPAN) locate(base + (int32_t)grp * SP, page, place);
     load_k(base);
   }
   for (; base < end; base += step) {
     // The next tile's pages first: its keys are issued once they are there,
     // without waiting for this tile's values, which come after them.
-    int32_t kpage_next = -1, vpage_next = -1;
-    uint32_t kplace_next = 0, vplace_next = 0;
-    if (SPAN) {
-      locate(base + step + (int32_t)(col / 4) * SP, kpage_next, kplace_next);
-      locate(base + step + (int32_t)grp * SP, vpage_next, vplace_next);
-    }
+    int32_t page_next = 0;
+    uint32_t place_next = 0;
+    if (SPAN) locate(base + step + (int32_t)grp * SP, page_next, place_next);
     // Values of this tile, and which of the lane's tokens count.
     bool live[SP], whole = true;
+    const T *row = row_of(vb, P.v_page, P.v_token, page, place);
 #pragma unroll
     for (int j = 0; j < SP; ++j) {
       const int32_t tok = base + (int32_t)grp * SP + j;
-      int32_t page = vpage;
-      uint32_t place = vplace + j;
-      if constexpr (!SPAN) locate(tok, page, place);
-      live[j] = counts(tok, page);
+      if constexpr (!SPAN) {
+        locate(tok, page, place);
+        row = row_of(vb, P.v_page, P.v_token, page, place);
+      } else if (j) {
+        row += P.v_token;
+      }
+      live[j] = (int)(tok >= first) & (int)(tok < end) & (int)((uint32_t)page < P.n_pages);
       whole &= live[j];
-      const T *row = row_of(vb, P.v_page, P.v_token, page, place, live[j]);
 #pragma unroll
       for (int x = 0; x < VL; ++x) {
         const int at = x * 16 * VW + (int)col * VW;
         if constexpr (VEC) load_row<T, VW, true>(row + (at < d ? at : 0), 1, v[j][x]);
-        else load_row<T, VW, false>(row + at, live[j] ? d - at : 0, v[j][x]);
+        else load_row<T, VW, false>(row + at, d - at, v[j][x]);
       }
     }
     whole = __all(whole);
-    kpage = kpage_next, kplace = kplace_next, vpage = vpage_next, vplace = vplace_next;
 
+    // The tile's keys into LDS: token grp * SP + r in row 16 (r / 4) + 4 grp + r % 4, tile and row of S^T.
     // Dims from d on hold the row's first ones: their queries are zero, but not an infinite key times zero.
-    if (VEC && d < D) {
 #pragma unroll
-      for (int s = 0; s < RT; ++s)
+    for (int i = 0; i < KI; ++i)
 #pragma unroll
-        for (int f = 0; f < KF; ++f)
-          if (f * (int)kFragElems<T> + (int)grp * E >= d) k[s][f] = (u4){0, 0, 0, 0};
-    }
+      for (int x = 0; x < PC; ++x) {
+        const int r = kfirst + i, at = x * 16 * E + kat;
+        u4 y = k[i][x];
+        if (VEC && d < D && at >= d) y = (u4){0, 0, 0, 0};
+        *(u4 *)&sh.k[w][16 * (r / 4) + 4 * grp + r % 4][at * sizeof(T)] = y;
+      }
+    page = page_next, place = place_next;
+    load_k(base + step);
+
     f4 acc[RT];
 #pragma unroll
     for (int s = 0; s < RT; ++s) {
       acc[s] = (f4){0, 0, 0, 0};
 #pragma unroll
-      for (int f = 0; f < KF; ++f) acc[s] = mma<T>(k[s][f], q[f], acc[s]);
+      for (int f = 0; f < KF; ++f) acc[s] = mma<T>(*(const u4 *)&sh.k[w][16 * s + col][(f * 4 + grp) * 16], q[f], acc[s]);
     }
-    load_k(base + step);
 
     float sc[SP];
     if (P.cap_out > 0) {
@@ -266,6 +280,7 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
   }
 
   // The four wavefronts' parts, joined DC columns at a time.
+  __syncthreads();
   l = column_sum(l);
   if (grp == 0) sm[w][col] = m, sl[w][col] = l;
   const uint32_t oh = threadIdx.x >> 4, oc = threadIdx.x & 15;   // this thread's head, and its first column / (DC / 16)
@@ -279,7 +294,7 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
 #pragma unroll
       for (int u = 0; u < VW; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) so[w][col][x * 16 * VW - c0 + (grp * 4 + i) * VW + u] = o[x * VW + u][i];
+        for (int i = 0; i < 4; ++i) sh.o[w][col][x * 16 * VW - c0 + (grp * 4 + i) * VW + u] = o[x * VW + u][i];
     }
     __syncthreads();
     float f[4], mt = fmaxf(fmaxf(sm[0][oh], sm[1][oh]), fmaxf(sm[2][oh], sm[3][oh])), lt = 0;
@@ -291,62 +306,71 @@ __global__ void __launch_bounds__(256) attend_kernel(AttendParams P) {
     }
     if (oh >= heads) continue;
     const float inv = lt == 0 ? 0.f : 1.f / lt;
-    float *part = P.part + ((uint64_t)(seq * P.n_head + head) * P.splits + split) * (P.d + 2);
+    const uint64_t at = (uint64_t)(seq * P.n_head + head) * P.splits + split;
+    float *part = P.part + at * P.d;
     T *out = (T *)P.out + seq * P.out_seq + head * P.out_head;
 #pragma unroll
     for (int e = 0; e < DC / 16; ++e) {
       const uint32_t c = oc + 16 * e;
       float x = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x += so[i][oh][c] * f[i];
+      for (int i = 0; i < 4; ++i) x += sh.o[i][oh][c] * f[i];
       if (c0 + c >= P.d) continue;
       if (P.splits == 1) out[c0 + c] = (T)(lt == 0 ? 0.f : x * inv);
       else part[c0 + c] = x;
     }
     if (oc == 0 && c0 == 0) {
-      if (P.splits > 1) part[P.d] = mt, part[P.d + 1] = lt;
+      if (P.splits > 1) P.part_ml[2 * at] = mt, P.part_ml[2 * at + 1] = lt;
       else if (P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms + __builtin_amdgcn_logf(lt));
     }
   }
 }
 
-// The parts of one sequence and head: wavefront w takes parts w, w + 4, ...,
-// each lane up to four columns, and the four are joined as above.
-template <typename T>
-__global__ void __launch_bounds__(256) attend_join_kernel(AttendParams P) {
-  __shared__ float sm[4], sl[4], so[4][256];
-  const uint32_t head = blockIdx.x, seq = blockIdx.y, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+// The parts of one sequence and head: every part's weight first, then the
+// threads of each of G groups sum a column each over every G-th part.
+template <typename T, int G>
+__global__ void __launch_bounds__(256 * G) attend_join_kernel(AttendParams P) {
+  __shared__ float sw[kMaxSplits], sm[2], sl[2], so[G][FIONA_MAX_HEAD_DIM];
+  const uint32_t head = blockIdx.x, seq = blockIdx.y, t = threadIdx.x;
   int32_t first, n;
   key_range(P, seq, first, n);
   const int32_t start = first / kTileKeys<T> * kTileKeys<T>;
   const uint32_t used = n > start ? ((uint32_t)(n - start) + P.chunk - 1) / P.chunk : 0;
-  const float *part = P.part + (uint64_t)(seq * P.n_head + head) * P.splits * (P.d + 2);
-  float m = -INFINITY, l = 0, o[4] = {0, 0, 0, 0};
-  for (uint32_t i = w; i < used; i += 4) {
-    const float *p = part + (uint64_t)i * (P.d + 2);
-    const float mi = p[P.d], li = p[P.d + 1];
-    const float mn = fmaxf(m, mi), ms = mn == -INFINITY ? 0.f : mn;
-    const float a = __builtin_amdgcn_exp2f(m - ms), b = __builtin_amdgcn_exp2f(mi - ms);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (lane + 64 * e < P.d) o[e] = o[e] * a + p[lane + 64 * e] * b;
-    l = l * a + li * b;
-    m = mn;
+  const uint64_t at = (uint64_t)(seq * P.n_head + head) * P.splits;
+  float m = -INFINITY, l = 0;
+  if (t < 128) {
+    if (t < used) m = P.part_ml[2 * (at + t)], l = P.part_ml[2 * (at + t) + 1];
+    float top = m;
+    for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    if (t % 64 == 0) sm[t / 64] = top;
   }
-  if (lane == 0) sm[w] = m, sl[w] = l;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) so[w][lane + 64 * e] = o[e];
   __syncthreads();
-  const float mt = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])), ms = mt == -INFINITY ? 0.f : mt;
-  float lt = 0, x = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float f = __builtin_amdgcn_exp2f(sm[i] - ms);
-    lt += sl[i] * f;
-    x += so[i][threadIdx.x] * f;
+  const float mt = fmaxf(sm[0], sm[1]), ms = mt == -INFINITY ? 0.f : mt;
+  if (t < 128) {
+    const float f = __builtin_amdgcn_exp2f(m - ms);
+    sw[t] = f;
+    l *= f;
+    for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
+    if (t % 64 == 0) sl[t / 64] = l;
   }
-  if (threadIdx.x < P.d) ((T *)P.out)[seq * P.out_seq + head * P.out_head + threadIdx.x] = (T)(lt == 0 ? 0.f : x / lt);
-  if (threadIdx.x == 0 && P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms + __builtin_amdgcn_logf(lt));
+  __syncthreads();
+  const float lt = sl[0] + sl[1];
+  const uint32_t c = t % 256, g = t / 256;
+  float x = 0;
+  if (c < P.d) {
+    const float *o = P.part + at * P.d + c;
+#pragma unroll 8
+    for (uint32_t i = g; i < used; i += G) x += o[(uint64_t)i * P.d] * sw[i];
+  }
+  if constexpr (G > 1) {
+    so[g][c] = x;
+    __syncthreads();
+  }
+  if (t >= P.d) return;
+#pragma unroll
+  for (int i = 1; i < G; ++i) x += so[i][t];
+  ((T *)P.out)[seq * P.out_seq + head * P.out_head + t] = (T)(lt == 0 ? 0.f : x / lt);
+  if (t == 0 && P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms + __builtin_amdgcn_logf(lt));
 }
 
 }  // namespace fiona

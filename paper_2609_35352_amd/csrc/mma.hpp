@@ -40,17 +40,18 @@ __device__ __forceinline__ f4 mma(u4 a, u4 b, f4 c) {
 
 // Words of W elements of T from p of which the first `valid` may be read, the
 // rest zero.  VEC: p is aligned to the W elements and valid is 0 or >= W.
+// Nontemporal: what these operators read once per call passes the caches by.
 template <typename T, int W, bool VEC>
 __device__ __forceinline__ void load_row(const T *p, int valid, uint32_t (&w)[W * sizeof(T) / 4]) {
   constexpr int N = W * sizeof(T) / 4;
   if constexpr (VEC) {
     if constexpr (N == 4) {
-      const u4 v = valid > 0 ? *(const u4 *)p : (u4){0, 0, 0, 0};
+      const u4 v = valid > 0 ? __builtin_nontemporal_load((const u4 *)p) : (u4){0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = v[i];
     } else {
       static_assert(N == 2, "8 or 16 bytes per lane");
-      const u2 v = valid > 0 ? *(const u2 *)p : (u2){0, 0};
+      const u2 v = valid > 0 ? __builtin_nontemporal_load((const u2 *)p) : (u2){0, 0};
       w[0] = v[0], w[1] = v[1];
     }
   } else if constexpr (sizeof(T) == 4) {
