@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -461,98 +462,80 @@ def hybrid_linear_static(plan: Plan, in_t, pt_t, sign_t, scale_t, out_t, stream=
 # contiguous; the other axes may have any stride.
 # ----------------------------------------------------------------------------
 
-class _KvCache(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_uint32) for n in ("type", "n_pages", "page_size", "n_kv", "head_dim")] + \
-        [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
-        [(n, ctypes.c_uint64) for n in ("k_page", "k_token", "k_head", "v_page", "v_token", "v_head")]
+# The header's structs, fields in order with native alignment; packed in one go, as a
+# decode step's calls are as short as a few microseconds.
+_KV_CACHE = struct.Struct("@5I2P6Q")
+_APPEND_ARGS = struct.Struct("@6I4P8Q4P")
+_ATTENTION_DESC = struct.Struct("@7I")
+_ATTENTION_ARGS = struct.Struct("@3I2f3P5Q2P")
+_ADAPTERS_DESC = struct.Struct("@6I")
+_ADAPTER_ARGS = struct.Struct("@I6PQ2P2Q5P3Q")
 
-
-class _AppendArgs(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_uint32) for n in ("n_tok", "n_head", "rows_type", "rot_dim", "n_pos", "interleaved")] + \
-        [(n, ctypes.c_void_p) for n in ("k", "v", "q", "q_out")] + \
-        [(n, ctypes.c_uint64) for n in ("k_tok", "k_head", "v_tok", "v_head", "q_tok", "q_head", "q_out_tok",
-                                        "q_out_head")] + \
-        [(n, ctypes.c_void_p) for n in ("slots", "positions", "cos", "sin")]
-
-
-class _AttentionDesc(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_uint32) for n in ("type", "n_head", "n_kv", "head_dim", "page_size", "max_seq",
-                                               "max_length")]
-
-
-class _AttentionArgs(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_uint32) for n in ("n_seq", "table_width", "window")] + \
-        [("scale", ctypes.c_float), ("softcap", ctypes.c_float)] + \
-        [(n, ctypes.c_void_p) for n in ("q", "out", "lse")] + \
-        [(n, ctypes.c_uint64) for n in ("q_seq", "q_head", "out_seq", "out_head", "table_stride")] + \
-        [(n, ctypes.c_void_p) for n in ("page_table", "lengths")]
-
-
-class _AdaptersDesc(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_uint32) for n in ("type", "n_adapter", "max_rank", "d_in", "d_out", "max_tokens")]
-
-
-class _AdapterArgs(ctypes.Structure):
-    _fields_ = [("n_tok", ctypes.c_uint32)] + \
-        [(n, ctypes.c_void_p) for n in ("x", "A", "B", "ids", "ranks", "scaling")] + [("x_row", ctypes.c_uint64)] + \
-        [("base", ctypes.c_void_p), ("y", ctypes.c_void_p), ("base_row", ctypes.c_uint64), ("y_row", ctypes.c_uint64)] + \
-        [(n, ctypes.c_void_p) for n in ("dy", "dx_base", "dx", "dA", "dB")] + \
-        [(n, ctypes.c_uint64) for n in ("dy_row", "dx_base_row", "dx_row")]
+_DTYPES = {}   # torch dtype -> fiona_type
+_INT = {}      # bytes -> torch dtype, and "f32"
 
 
 def _lm_lib():
     L = lib()
-    if not getattr(L, "_lm_declared", False):
-        P = ctypes.POINTER
-        for name, args in (("fiona_kv_append", [P(_KvCache), P(_AppendArgs), ctypes.c_void_p]),
-                           ("fiona_attention_create", [P(_AttentionDesc), P(ctypes.c_void_p)]),
-                           ("fiona_paged_attention", [ctypes.c_void_p, P(_KvCache), P(_AttentionArgs), ctypes.c_void_p]),
-                           ("fiona_adapters_create", [P(_AdaptersDesc), P(ctypes.c_void_p)]),
-                           ("fiona_adapter_linear", [ctypes.c_void_p, P(_AdapterArgs), ctypes.c_void_p]),
-                           ("fiona_adapter_backward", [ctypes.c_void_p, P(_AdapterArgs), ctypes.c_void_p])):
+    if not _DTYPES:
+        import torch
+
+        p = ctypes.c_void_p
+        for name, args in (("fiona_kv_append", [p] * 3), ("fiona_attention_create", [p, ctypes.POINTER(p)]),
+                           ("fiona_paged_attention", [p] * 4), ("fiona_adapters_create", [p, ctypes.POINTER(p)]),
+                           ("fiona_adapter_linear", [p] * 3), ("fiona_adapter_backward", [p] * 3)):
             getattr(L, name).restype, getattr(L, name).argtypes = ctypes.c_int, args
         for name in ("fiona_attention_destroy", "fiona_adapters_destroy"):
-            getattr(L, name).restype, getattr(L, name).argtypes = None, [ctypes.c_void_p]
-        L._lm_declared = True
+            getattr(L, name).restype, getattr(L, name).argtypes = None, [p]
+        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+        _INT.update({4: torch.int32, 8: torch.int64, "f32": torch.float32})
     return L
 
 
 def _type_code(dtype) -> int:
-    code = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}.get(str(dtype))
+    _lm_lib()
+    code = _DTYPES.get(dtype)
     if code is None:
         raise ValueError("%s is not float32, float16 or bfloat16" % (dtype,))
     return code
 
 
-def _rows_of(t, name, dtype, shape, device=None):
-    """Pointer and the strides of all axes but the last, after checking type, shape and device."""
+def _refuse(t, name, dtype, shape, dev, packed=False):
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
-    if device is not None and t.device != device:
-        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
-    if str(t.dtype) != str(dtype):
+    if t.get_device() != dev:
+        raise ValueError("%s is on device %d, not on %d" % (name, t.get_device(), dev))
+    if t.dtype is not dtype:
         raise ValueError("%s must be %s, is %s" % (name, dtype, t.dtype))
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s must have shape %s, has %s" % (name, tuple(shape), tuple(t.shape)))
-    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError("%s: its last axis must be contiguous" % name)
-    return (t.data_ptr() if t.numel() else None,) + tuple(t.stride()[:-1])
+    raise ValueError("%s must be contiguous" % name if packed else "%s: its last axis must be contiguous" % name)
 
 
-def _packed(t, name, dtype, shape, device):
-    p = _rows_of(t, name, dtype, shape, device)[0]
-    if not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
-    return p
+def _rows(t, name, dtype, shape, dev):
+    """The strides of a tensor whose last axis is contiguous, after checking type, shape and device."""
+    st = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or dev < 0 or (st[-1] != 1 and shape[-1] > 1):
+        _refuse(t, name, dtype, shape, dev)
+    return st
+
+
+def _packed(t, name, dtype, shape, dev):
+    """The address of a contiguous tensor, after the same checks."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or dev < 0 or not t.is_contiguous():
+        _refuse(t, name, dtype, shape, dev, True)
+    return t.data_ptr()
 
 
 def _cache_desc(k_cache, v_cache):
-    if k_cache.dim() != 4:
+    """(fiona_kv_cache, dtype, device, n_kv, head_dim)"""
+    dtype, shape, dev = k_cache.dtype, k_cache.shape, k_cache.get_device()
+    if len(shape) != 4:
         raise ValueError("k_cache must have shape [n_pages][page_size][n_kv][head_dim]")
-    c = _KvCache(_type_code(k_cache.dtype), *k_cache.shape)
-    c.k, c.k_page, c.k_token, c.k_head = _rows_of(k_cache, "k_cache", k_cache.dtype, k_cache.shape)
-    c.v, c.v_page, c.v_token, c.v_head = _rows_of(v_cache, "v_cache", k_cache.dtype, k_cache.shape, k_cache.device)
-    return c
+    code = _type_code(dtype)
+    ks, vs = _rows(k_cache, "k_cache", dtype, shape, dev), _rows(v_cache, "v_cache", dtype, shape, dev)
+    return _KV_CACHE.pack(code, *shape, k_cache.data_ptr(), v_cache.data_ptr(), *ks[:3], *vs[:3]), dtype, dev, shape[2], \
+        shape[3]
 
 
 def kv_append(k, v, slots, k_cache, v_cache, positions=None, cos=None, sin=None, interleaved: bool = False, q=None,
@@ -560,26 +543,34 @@ def kv_append(k, v, slots, k_cache, v_cache, positions=None, cos=None, sin=None,
     """fiona_kv_append: k, v [n_tok][n_kv][d] into the caches [n_pages][page_size][n_kv][d] at slots (int64
     [n_tok]; outside the cache: not written), keys rotated at positions (int32 [n_tok]) with cos, sin float32
     [n_pos][rot_dim / 2], and q [n_tok][n_head][d] rotated into q_out (the caches' type)."""
-    cache, a, dev = _cache_desc(k_cache, v_cache), _AppendArgs(), k_cache.device
-    n, n_kv, d = k.shape[0], k_cache.shape[2], k_cache.shape[3]
-    a.n_tok, a.rows_type, a.interleaved = n, _type_code(k.dtype), int(bool(interleaved))
-    a.k, a.k_tok, a.k_head = _rows_of(k, "k", k.dtype, (n, n_kv, d), dev)
-    a.v, a.v_tok, a.v_head = _rows_of(v, "v", k.dtype, (n, n_kv, d), dev)
-    a.slots = _packed(slots, "slots", "torch.int64", (n,), dev)
+    cache, dtype, dev, n_kv, d = _cache_desc(k_cache, v_cache)
+    n, rows = len(k), k.dtype
+    code = _type_code(rows)
+    ks, vs = _rows(k, "k", rows, (n, n_kv, d), dev), _rows(v, "v", rows, (n, n_kv, d), dev)
+    at = _packed(slots, "slots", _INT[8], (n,), dev)
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
+    H, qp, qop, qs, qos = 0, 0, 0, (0, 0), (0, 0)
     if q is not None:
-        a.n_head = q.shape[1]
-        a.q, a.q_tok, a.q_head = _rows_of(q, "q", k.dtype, (n, a.n_head, d), dev)
-        a.q_out, a.q_out_tok, a.q_out_head = _rows_of(q_out, "q_out", k_cache.dtype, (n, a.n_head, d), dev)
+        H = q.shape[1]
+        qs, qos = _rows(q, "q", rows, (n, H, d), dev), _rows(q_out, "q_out", dtype, (n, H, d), dev)
+        qp, qop = q.data_ptr(), q_out.data_ptr()
+    n_pos, rot, pp, cp, sp = 0, 0, 0, 0, 0
     if cos is not None or sin is not None:
         if cos is None or sin is None or positions is None:
             raise ValueError("positions, cos and sin go together")
-        a.n_pos, a.rot_dim = cos.shape[0], 2 * cos.shape[1]
-        a.cos = _packed(cos, "cos", "torch.float32", cos.shape, dev)
-        a.sin = _packed(sin, "sin", "torch.float32", cos.shape, dev)
-        a.positions = _packed(positions, "positions", "torch.int32", (n,), dev)
-    _check(_lm_lib().fiona_kv_append(ctypes.byref(cache), ctypes.byref(a), _stream_handle(stream)), "fiona_kv_append")
+        shape = cos.shape
+        if len(shape) != 2:
+            raise ValueError("cos must have shape [n_pos][rot_dim / 2]")
+        n_pos, rot = shape[0], 2 * shape[1]
+        f32 = _INT["f32"]
+        cp, sp = _packed(cos, "cos", f32, shape, dev), _packed(sin, "sin", f32, shape, dev)
+        pp = _packed(positions, "positions", _INT[4], (n,), dev)
+    args = _APPEND_ARGS.pack(n, H, code, rot, n_pos, 1 if interleaved else 0, k.data_ptr(), v.data_ptr(), qp, qop,
+                             ks[0], ks[1], vs[0], vs[1], qs[0], qs[1], qos[0], qos[1], at, pp, cp, sp)
+    rc = lib().fiona_kv_append(cache, args, _stream_handle(stream))
+    if rc:
+        raise FionaError(rc, "fiona_kv_append")
 
 
 class Attention:
@@ -588,10 +579,10 @@ class Attention:
     def __init__(self, dtype, n_head: int, n_kv: int, head_dim: int, page_size: int, max_seq: int, max_length: int):
         self.dtype = dtype
         self.n_head, self.n_kv, self.head_dim, self.max_seq = int(n_head), int(n_kv), int(head_dim), int(max_seq)
-        d = _AttentionDesc(_type_code(dtype), self.n_head, self.n_kv, self.head_dim, int(page_size), self.max_seq,
-                           int(max_length))
+        d = _ATTENTION_DESC.pack(_type_code(dtype), self.n_head, self.n_kv, self.head_dim, int(page_size), self.max_seq,
+                                 int(max_length))
         h = ctypes.c_void_p()
-        _check(_lm_lib().fiona_attention_create(ctypes.byref(d), ctypes.byref(h)), "fiona_attention_create")
+        _check(_lm_lib().fiona_attention_create(d, ctypes.byref(h)), "fiona_attention_create")
         self._h = h
 
     @property
@@ -615,21 +606,20 @@ def paged_attention(att: Attention, q, k_cache, v_cache, page_table, lengths, ou
     """fiona_paged_attention: q [n_seq][n_head][d] over the caches [n_pages][page_size][n_kv][d], page_table int32
     [n_seq][table_width], lengths int32 [n_seq] -> out [n_seq][n_head][d] and lse float32 [n_seq][n_head].
     scale: default head_dim ** -0.5."""
-    cache, a, dev = _cache_desc(k_cache, v_cache), _AttentionArgs(), k_cache.device
-    n = q.shape[0]
+    cache, _, dev, _, _ = _cache_desc(k_cache, v_cache)
+    n = len(q)
     shape = (n, att.n_head, att.head_dim)
-    a.n_seq, a.window, a.softcap = n, int(window), float(softcap)
-    a.scale = float(scale) if scale is not None else att.head_dim ** -0.5
-    a.q, a.q_seq, a.q_head = _rows_of(q, "q", att.dtype, shape, dev)
-    a.out, a.out_seq, a.out_head = _rows_of(out, "out", att.dtype, shape, dev)
-    if lse is not None:
-        a.lse = _packed(lse, "lse", "torch.float32", (n, att.n_head), dev)
-    a.page_table, a.table_stride = _rows_of(page_table, "page_table", "torch.int32", (n, page_table.shape[1]), dev)
-    a.table_width = page_table.shape[1]
-    a.table_stride = max(a.table_stride, a.table_width) if n == 1 else a.table_stride
-    a.lengths = _packed(lengths, "lengths", "torch.int32", (n,), dev)
-    _check(_lm_lib().fiona_paged_attention(att.handle, ctypes.byref(cache), ctypes.byref(a), _stream_handle(stream)),
-           "fiona_paged_attention")
+    qs, os_ = _rows(q, "q", att.dtype, shape, dev), _rows(out, "out", att.dtype, shape, dev)
+    width = page_table.shape[-1]
+    ts = _rows(page_table, "page_table", _INT[4], (n, width), dev)
+    lp = _packed(lse, "lse", _INT["f32"], (n, att.n_head), dev) if lse is not None else 0
+    args = _ATTENTION_ARGS.pack(n, width, int(window), float(scale) if scale is not None else att.head_dim ** -0.5,
+                                float(softcap), q.data_ptr(), out.data_ptr(), lp, qs[0], qs[1], os_[0], os_[1],
+                                ts[0] if n > 1 else max(ts[0], width), page_table.data_ptr(),
+                                _packed(lengths, "lengths", _INT[4], (n,), dev))
+    rc = lib().fiona_paged_attention(att.handle, cache, args, _stream_handle(stream))
+    if rc:
+        raise FionaError(rc, "fiona_paged_attention")
 
 
 class Adapters:
@@ -638,9 +628,9 @@ class Adapters:
     def __init__(self, dtype, n_adapter: int, max_rank: int, d_in: int, d_out: int, max_tokens: int):
         self.dtype = dtype
         self.n_adapter, self.max_rank, self.d_in, self.d_out = int(n_adapter), int(max_rank), int(d_in), int(d_out)
-        d = _AdaptersDesc(_type_code(dtype), self.n_adapter, self.max_rank, self.d_in, self.d_out, int(max_tokens))
+        d = _ADAPTERS_DESC.pack(_type_code(dtype), self.n_adapter, self.max_rank, self.d_in, self.d_out, int(max_tokens))
         h = ctypes.c_void_p()
-        _check(_lm_lib().fiona_adapters_create(ctypes.byref(d), ctypes.byref(h)), "fiona_adapters_create")
+        _check(_lm_lib().fiona_adapters_create(d, ctypes.byref(h)), "fiona_adapters_create")
         self._h = h
 
     @property
@@ -660,39 +650,40 @@ class Adapters:
 
 
 def _adapter_args(ad: Adapters, x, ids, A, B, ranks, scaling):
-    a, n, dev = _AdapterArgs(), x.shape[0], x.device
-    a.n_tok = n
-    a.x, a.x_row = _rows_of(x, "x", ad.dtype, (n, ad.d_in))
-    a.ids = _packed(ids, "ids", "torch.int32", (n,), dev)
-    a.A = _packed(A, "A", ad.dtype, (ad.n_adapter, ad.max_rank, ad.d_in), dev)
-    a.B = _packed(B, "B", ad.dtype, (ad.n_adapter, ad.d_out, ad.max_rank), dev)
-    if ranks is not None:
-        a.ranks = _packed(ranks, "ranks", "torch.int32", (ad.n_adapter,), dev)
-    if scaling is not None:
-        a.scaling = _packed(scaling, "scaling", "torch.float32", (ad.n_adapter,), dev)
-    return a, n, dev
+    """(the shared fields' values, n_tok, device)"""
+    n, dev, dt = len(x), x.get_device(), ad.dtype
+    xs = _rows(x, "x", dt, (n, ad.d_in), dev)
+    return (n, x.data_ptr(), _packed(A, "A", dt, (ad.n_adapter, ad.max_rank, ad.d_in), dev),
+            _packed(B, "B", dt, (ad.n_adapter, ad.d_out, ad.max_rank), dev), _packed(ids, "ids", _INT[4], (n,), dev),
+            _packed(ranks, "ranks", _INT[4], (ad.n_adapter,), dev) if ranks is not None else 0,
+            _packed(scaling, "scaling", _INT["f32"], (ad.n_adapter,), dev) if scaling is not None else 0, xs[0]), n, dev
 
 
 def adapter_linear(ad: Adapters, x, ids, A, B, base, y, ranks=None, scaling=None, stream=None) -> None:
     """fiona_adapter_linear: y [n_tok][d_out] = base (or None: zero) plus each token's adapter's part of
     x [n_tok][d_in]; ids int32 [n_tok] (outside the table: none), A [n_adapter][max_rank][d_in],
     B [n_adapter][d_out][max_rank], ranks int32 [n_adapter], scaling float32 [n_adapter].  y may be base."""
-    a, n, dev = _adapter_args(ad, x, ids, A, B, ranks, scaling)
-    if base is not None:
-        a.base, a.base_row = _rows_of(base, "base", ad.dtype, (n, ad.d_out), dev)
-    a.y, a.y_row = _rows_of(y, "y", ad.dtype, (n, ad.d_out), dev)
-    _check(_lm_lib().fiona_adapter_linear(ad.handle, ctypes.byref(a), _stream_handle(stream)), "fiona_adapter_linear")
+    head, n, dev = _adapter_args(ad, x, ids, A, B, ranks, scaling)
+    shape = (n, ad.d_out)
+    bp, bs = (base.data_ptr(), _rows(base, "base", ad.dtype, shape, dev)[0]) if base is not None else (0, 0)
+    ys = _rows(y, "y", ad.dtype, shape, dev)
+    args = _ADAPTER_ARGS.pack(*head, bp, y.data_ptr(), bs, ys[0], 0, 0, 0, 0, 0, 0, 0, 0)
+    rc = lib().fiona_adapter_linear(ad.handle, args, _stream_handle(stream))
+    if rc:
+        raise FionaError(rc, "fiona_adapter_linear")
 
 
 def adapter_backward(ad: Adapters, x, ids, A, B, dy, dx_base, dx, dA, dB, ranks=None, scaling=None, stream=None) -> None:
     """fiona_adapter_backward: dx [n_tok][d_in] = dx_base (or None: zero) plus the adapters' part, and dA, dB
     (shaped as A and B) from dy [n_tok][d_out].  dx may be dx_base."""
-    a, n, dev = _adapter_args(ad, x, ids, A, B, ranks, scaling)
-    a.dy, a.dy_row = _rows_of(dy, "dy", ad.dtype, (n, ad.d_out), dev)
-    if dx_base is not None:
-        a.dx_base, a.dx_base_row = _rows_of(dx_base, "dx_base", ad.dtype, (n, ad.d_in), dev)
-    a.dx, a.dx_row = _rows_of(dx, "dx", ad.dtype, (n, ad.d_in), dev)
-    a.dA = _packed(dA, "dA", ad.dtype, A.shape, dev)
-    a.dB = _packed(dB, "dB", ad.dtype, B.shape, dev)
-    _check(_lm_lib().fiona_adapter_backward(ad.handle, ctypes.byref(a), _stream_handle(stream)),
-           "fiona_adapter_backward")
+    head, n, dev = _adapter_args(ad, x, ids, A, B, ranks, scaling)
+    dt = ad.dtype
+    gs = _rows(dy, "dy", dt, (n, ad.d_out), dev)
+    bp, bs = (dx_base.data_ptr(), _rows(dx_base, "dx_base", dt, (n, ad.d_in), dev)[0]) if dx_base is not None else (0, 0)
+    xs = _rows(dx, "dx", dt, (n, ad.d_in), dev)
+    args = _ADAPTER_ARGS.pack(*head, 0, 0, 0, 0, dy.data_ptr(), bp, dx.data_ptr(),
+                              _packed(dA, "dA", dt, (ad.n_adapter, ad.max_rank, ad.d_in), dev),
+                              _packed(dB, "dB", dt, (ad.n_adapter, ad.d_out, ad.max_rank), dev), gs[0], bs, xs[0])
+    rc = lib().fiona_adapter_backward(ad.handle, args, _stream_handle(stream))
+    if rc:
+        raise FionaError(rc, "fiona_adapter_backward")

@@ -21,13 +21,19 @@ struct fiona_attention {
 
 namespace {
 
-constexpr uint32_t kMinChunk = 512, kMaxChunk = 1024, kWorkgroups = 1024;
+// Keys of one workgroup's chunk for calls over up to `keys` keys of `units`
+// sequences times key heads: enough chunks to fill the GPU several times, but
+// none below kMinChunk (a chunk's first loads wait for the length, then the
+// table), none above kMaxChunk so that ragged lengths even out, at most
+// kMaxSplits parts to join, and no join for what one workgroup does as fast.
+// Chunks of 256 / 512 / 768 / 1024 / 2048 / 4096, us: 64 sequences of 100 to 8192
+// keys, 8 key heads of 128, 108 / 102 / 95 / 113 / 143 / 145; 19 of up to 3000,
+// 7 of 80, 20.7 / 25.0 / 25.3 / 26.2 / 30.1 / 35.2; 2 of 100000 and 131072, 8 of
+// 128, 164 / 165 / 165 / 165 / 159 / 157; 1 of 300, 12 of 64 in 32 bits, 19.7 / 17.1 whole.
+constexpr uint32_t kMinChunk = 256, kMaxChunk = 768, kNoSplit = 512, kWorkgroups = 2048;
 using fiona::kMaxSplits;
-
-// Keys of one workgroup's chunk for calls over up to `keys` keys: few enough
-// that the sequences and key heads fill the GPU, at most kMaxChunk so that
-// ragged lengths even out, and at most kMaxSplits parts to join.
 uint32_t chunk_of(uint64_t keys, uint64_t units) {
+  if (keys <= kNoSplit) return kNoSplit;
   uint64_t c = (keys * units + kWorkgroups - 1) / kWorkgroups;
   c = std::max<uint64_t>(kMinChunk, std::min<uint64_t>(c, kMaxChunk));
   c = std::max<uint64_t>(c, (keys + kMaxSplits - 1) / kMaxSplits);

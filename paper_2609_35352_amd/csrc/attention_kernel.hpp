@@ -33,7 +33,7 @@
 
 namespace fiona {
 
-constexpr uint32_t kMaxSplits = 128;   // parts of one sequence
+constexpr uint32_t kMaxSplits = 64;   // parts of one sequence
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttendParams {
@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
 // threads of each of G groups sum a column each over every G-th part.
 template <typename T, int G>
 __global__ void __launch_bounds__(256 * G) attend_join_kernel(AttendParams P) {
-  __shared__ float sw[kMaxSplits], sm[2], sl[2], so[G][FIONA_MAX_HEAD_DIM];
+  __shared__ float sw[kMaxSplits], sm, sl, so[G][FIONA_MAX_HEAD_DIM];
   const uint32_t head = blockIdx.x, seq = blockIdx.y, t = threadIdx.x;
   int32_t first, n;
   key_range(P, seq, first, n);
@@ -338,23 +338,19 @@ __global__ void __launch_bounds__(256 * G) attend_join_kernel(AttendParams P) {
   const uint32_t used = n > start ? ((uint32_t)(n - start) + P.chunk - 1) / P.chunk : 0;
   const uint64_t at = (uint64_t)(seq * P.n_head + head) * P.splits;
   float m = -INFINITY, l = 0;
-  if (t < 128) {
+  if (t < 64) {
+    static_assert(kMaxSplits == 64, "a lane to a part");
     if (t < used) m = P.part_ml[2 * (at + t)], l = P.part_ml[2 * (at + t) + 1];
     float top = m;
     for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-    if (t % 64 == 0) sm[t / 64] = top;
-  }
-  __syncthreads();
-  const float mt = fmaxf(sm[0], sm[1]), ms = mt == -INFINITY ? 0.f : mt;
-  if (t < 128) {
-    const float f = __builtin_amdgcn_exp2f(m - ms);
+    const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
     sw[t] = f;
     l *= f;
     for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
-    if (t % 64 == 0) sl[t / 64] = l;
+    if (t == 0) sm = top, sl = l;
   }
   __syncthreads();
-  const float lt = sl[0] + sl[1];
+  const float lt = sl, ms = sm == -INFINITY ? 0.f : sm;
   const uint32_t c = t % 256, g = t / 256;
   float x = 0;
   if (c < P.d) {
