@@ -569,8 +569,10 @@ int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cach
  * two streams at the same time.  Errors (nothing is launched): FIONA_ERR_ARG,
  * FIONA_ERR_ALIGN, FIONA_ERR_ALIAS, FIONA_ERR_HIP.
  */
+#define FIONA_ADAPTERS_FORWARD_ONLY 1u   /* no workspace for fiona_adapter_backward (FIONA_ERR_ARG on such a handle) */
+
 typedef struct fiona_adapters_desc {
-  uint32_t type, n_adapter, max_rank, d_in, d_out, max_tokens;
+  uint32_t type, n_adapter, max_rank, d_in, d_out, max_tokens, flags;
 } fiona_adapters_desc;
 
 typedef struct fiona_adapter_args {

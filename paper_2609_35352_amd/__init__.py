@@ -468,7 +468,7 @@ _KV_CACHE = struct.Struct("@5I2P6Q")
 _APPEND_ARGS = struct.Struct("@6I4P8Q4P")
 _ATTENTION_DESC = struct.Struct("@7I")
 _ATTENTION_ARGS = struct.Struct("@3I2f3P5Q2P")
-_ADAPTERS_DESC = struct.Struct("@6I")
+_ADAPTERS_DESC = struct.Struct("@7I")
 _ADAPTER_ARGS = struct.Struct("@I6PQ2P2Q5P3Q")
 
 _DTYPES = {}   # torch dtype -> fiona_type
@@ -625,10 +625,12 @@ def paged_attention(att: Attention, q, k_cache, v_cache, page_table, lengths, ou
 class Adapters:
     """The workspace of adapter_linear and adapter_backward (fiona_adapters_create)."""
 
-    def __init__(self, dtype, n_adapter: int, max_rank: int, d_in: int, d_out: int, max_tokens: int):
+    def __init__(self, dtype, n_adapter: int, max_rank: int, d_in: int, d_out: int, max_tokens: int,
+                 forward_only: bool = False):
         self.dtype = dtype
         self.n_adapter, self.max_rank, self.d_in, self.d_out = int(n_adapter), int(max_rank), int(d_in), int(d_out)
-        d = _ADAPTERS_DESC.pack(_type_code(dtype), self.n_adapter, self.max_rank, self.d_in, self.d_out, int(max_tokens))
+        d = _ADAPTERS_DESC.pack(_type_code(dtype), self.n_adapter, self.max_rank, self.d_in, self.d_out, int(max_tokens),
+                                1 if forward_only else 0)
         h = ctypes.c_void_p()
         _check(_lm_lib().fiona_adapters_create(d, ctypes.byref(h)), "fiona_adapters_create")
         self._h = h

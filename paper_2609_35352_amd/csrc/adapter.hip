@@ -4,7 +4,9 @@
 
 #include <cstdint>
 #include <new>
+#include <type_traits>
 
+#include "adapter_kernel.hpp"
 #include "fiona.h"
 #include "rows.hpp"
 
@@ -13,8 +15,18 @@ using namespace fiona_host;
 struct fiona_adapters {
   fiona_adapters_desc desc{};
   int device = -1;
-  float *h = nullptr, *g = nullptr;   // [max_tokens][max_rank] each
+  uint32_t RP = 0;                       // ranks in whole tiles
+  uint64_t part_cap = 0, grad_splits = 1;
+  char *ws = nullptr;
+  // Into ws.  part: sums of h and g; g: whole g; column: h and g by rank; AT, BT:
+  // the factors transposed; grad: a split's gradients.
+  float *part[2] = {}, *g = nullptr, *grad[2] = {};
+  void *column[2] = {}, *AT = nullptr, *BT = nullptr;
 };
+
+// Rows below kMinWidth elements, too short for 16-byte pieces: one value per
+// wavefront or thread.
+constexpr uint32_t kMinWidth = 8;
 
 namespace fiona {
 
@@ -112,12 +124,76 @@ int check_common(const fiona_adapters *H, const fiona_adapter_args *args, fiona:
   P.x = A.x, P.A = A.A, P.B = A.B, P.ids = A.ids, P.ranks = A.ranks, P.scaling = A.scaling;
   P.x_row = A.x_row;
   P.n_tok = A.n_tok, P.n_adapter = D.n_adapter, P.R = D.max_rank, P.d_in = D.d_in, P.d_out = D.d_out;
-  P.h = H->h, P.g = H->g;
+  P.h = H->part[0], P.g = H->part[1];
   return FIONA_OK;
 }
 
 Rows matrix(const void *p, uint64_t e, uint64_t n, uint64_t width, uint64_t row) {
   return Rows{p, e, width, {n, 1, 1}, {row, 0, 0}};
+}
+
+bool narrow(const fiona_adapters_desc &D) { return D.d_in < kMinWidth || D.d_out < kMinWidth; }
+
+uint32_t blocks_of(uint64_t n) { return (uint32_t)((n + fiona::kRows - 1) / fiona::kRows); }
+
+// Workgroups that share the adapters among 64 tokens: many where there are few
+// tokens, as each may have its own.
+uint32_t slots_of(uint32_t n, uint32_t adapters) {
+  const uint32_t want = std::max(1u, 64 / blocks_of(n));
+  return std::min({want, adapters, std::min(n, fiona::kRows)});
+}
+
+constexpr uint32_t kMaxSplits = 8, kWorkgroups = 1024, kGradWorkgroups = 512;
+
+// Parts of a row's contraction: enough workgroups to fill the GPU.
+uint32_t splits_of(uint32_t n, uint32_t adapters) {
+  const uint32_t wgs = blocks_of(n) * slots_of(n, adapters);
+  return std::max(1u, std::min(kMaxSplits, (kWorkgroups + wgs - 1) / wgs));
+}
+
+uint32_t grad_slices(uint32_t n, uint32_t type) {
+  const uint32_t cols = type == FIONA_F32 ? fiona::kGradCols<float> : fiona::kGradCols<__bf16>;
+  return (n + cols - 1) / cols;
+}
+
+// Parts of the tokens in the gradients' sums, where their columns alone do not fill the GPU.
+uint32_t grad_splits_of(const fiona_adapters_desc &D, uint32_t RP, uint32_t n) {
+  const uint64_t wgs = (uint64_t)(grad_slices(D.d_in, D.type) + grad_slices(D.d_out, D.type)) * D.n_adapter * ((RP + 63) / 64);
+  const uint64_t want = (kGradWorkgroups + wgs - 1) / wgs;
+  return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(want, (n + 255) / 256));
+}
+
+template <typename F>
+void with_tiles(uint32_t RP, F f) {
+  if (RP == 16) f(std::integral_constant<int, 1>{});
+  else if (RP == 32) f(std::integral_constant<int, 2>{});
+  else if (RP == 64) f(std::integral_constant<int, 4>{});
+  else f(std::integral_constant<int, 8>{});
+}
+
+template <typename T>
+void launch_shrink(const fiona_adapters *H, const fiona::AdapterIds &I, const fiona::ShrinkSide *sides, uint32_t n_sides,
+                   uint32_t splits, hipStream_t stream) {
+  fiona::ShrinkParams P{};
+  P.I = I, P.splits = splits, P.slots = slots_of(I.n_tok, I.n_adapter);
+  for (uint32_t i = 0; i < n_sides; ++i) P.side[i] = sides[i];
+  with_tiles(H->RP, [&](auto rt) {
+    hipLaunchKernelGGL((fiona::shrink_kernel<T, decltype(rt)::value>), dim3(blocks_of(I.n_tok), splits, P.slots * n_sides),
+                       dim3(256), 0, stream, P);
+  });
+}
+
+template <typename T>
+void launch_expand(const fiona_adapters *H, fiona::ExpandParams P, hipStream_t stream) {
+  const uint32_t n = P.I.n_tok, steps = (P.O + 255) / 256;
+  P.slots = slots_of(n, P.I.n_adapter + 1);
+  const uint32_t wgs = blocks_of(n) * P.slots;
+  const uint32_t slices = std::max(1u, std::min(steps, (kWorkgroups + wgs - 1) / wgs));
+  P.slice = (steps + slices - 1) / slices * 256;
+  with_tiles(H->RP, [&](auto rt) {
+    hipLaunchKernelGGL((fiona::expand_kernel<T, decltype(rt)::value>), dim3((P.O + P.slice - 1) / P.slice, blocks_of(n), P.slots),
+                       dim3(256), 0, stream, P);
+  });
 }
 
 // FIONA_ERR_ALIAS where an output's rows overlap each other, another output
@@ -156,8 +232,8 @@ int fiona_adapters_create(const fiona_adapters_desc *desc, fiona_adapters **out)
   const fiona_adapters_desc &D = *desc;
   if (!known_type(D.type)) return FIONA_ERR_UNSUPPORTED;
   if (!D.n_adapter || !D.max_rank || !D.d_in || !D.d_out || !D.max_tokens) return FIONA_ERR_ARG;
-  if (D.max_rank > FIONA_MAX_RANK || D.n_adapter > 65535 || D.d_in > (1u << 20) || D.d_out > (1u << 20) ||
-      D.max_tokens > (1u << 22))
+  if (D.max_rank > FIONA_MAX_RANK || D.n_adapter > 32767 || D.d_in > (1u << 20) || D.d_out > (1u << 20) ||
+      D.max_tokens > (1u << 21))
     return FIONA_ERR_UNSUPPORTED;
   fiona_adapters *H = new (std::nothrow) fiona_adapters;
   if (!H) return FIONA_ERR_NOMEM;
@@ -166,20 +242,38 @@ int fiona_adapters_create(const fiona_adapters_desc *desc, fiona_adapters **out)
     delete H;
     return FIONA_ERR_HIP;
   }
-  const size_t words = (size_t)D.max_tokens * D.max_rank;
-  if (hipMalloc((void **)&H->h, 2 * words * sizeof(float)) != hipSuccess) {
+  H->RP = D.max_rank <= 16 ? 16 : D.max_rank <= 32 ? 32 : D.max_rank <= 64 ? 64 : 128;
+  const bool both = !(D.flags & FIONA_ADAPTERS_FORWARD_ONLY);
+  const uint64_t e = type_size(D.type), n_pad = (uint64_t)blocks_of(D.max_tokens) * 64, RP = H->RP;
+  for (uint32_t n = std::min(64u, D.max_tokens);; n = std::min(n + 64, D.max_tokens)) {
+    H->part_cap = std::max<uint64_t>(H->part_cap, (uint64_t)n * splits_of(n, D.n_adapter));
+    if (n == D.max_tokens) break;
+  }
+  H->part_cap = std::max<uint64_t>(H->part_cap, 64 * kMaxSplits);   // (fewer than 64 tokens)
+  H->grad_splits = grad_splits_of(D, H->RP, D.max_tokens);
+  // Sizes in order; every part starts at a multiple of 256 bytes.
+  const uint64_t grads = (uint64_t)D.n_adapter * D.max_rank * 4 * (H->grad_splits > 1 ? H->grad_splits : 0);
+  const uint64_t size[] = {H->part_cap * RP * 4, both ? H->part_cap * RP * 4 : 0, both ? D.max_tokens * RP * 4 : 0,
+                           both ? n_pad * RP * 4 : 0, both ? n_pad * RP * 4 : 0,
+                           both ? RP * D.n_adapter * D.d_in * e : 0, both ? RP * D.n_adapter * D.d_out * e : 0,
+                           both ? grads * D.d_in : 0, both ? grads * D.d_out : 0};
+  uint64_t at[10] = {0};
+  for (int i = 0; i < 9; ++i) at[i + 1] = at[i] + (size[i] + 255) / 256 * 256;
+  if (hipMalloc((void **)&H->ws, at[9]) != hipSuccess) {
     (void)hipGetLastError();
     delete H;
     return FIONA_ERR_NOMEM;
   }
-  H->g = H->h + words;
+  H->part[0] = (float *)(H->ws + at[0]), H->part[1] = (float *)(H->ws + at[1]), H->g = (float *)(H->ws + at[2]);
+  H->column[0] = H->ws + at[3], H->column[1] = H->ws + at[4], H->AT = H->ws + at[5], H->BT = H->ws + at[6];
+  H->grad[0] = (float *)(H->ws + at[7]), H->grad[1] = (float *)(H->ws + at[8]);
   *out = H;
   return FIONA_OK;
 }
 
 void fiona_adapters_destroy(fiona_adapters *H) {
   if (!H) return;
-  if (H->h) (void)hipFree(H->h);
+  if (H->ws) (void)hipFree(H->ws);
   delete H;
 }
 
@@ -204,6 +298,15 @@ int fiona_adapter_linear(const fiona_adapters *H, const fiona_adapter_args *args
   P.base = A.base, P.y = A.y, P.base_row = A.base_row, P.y_row = A.y_row;
   with_type(D.type, [&](auto t) {
     using T = decltype(t);
+    if (!narrow(D)) {
+      const uint32_t splits = splits_of(A.n_tok, D.n_adapter);
+      const fiona::AdapterIds I{A.ids, A.ranks, A.n_tok, D.n_adapter, D.max_rank};
+      const fiona::ShrinkSide side{A.x, A.A, H->part[0], A.x_row, D.d_in, D.max_rank};
+      launch_shrink<T>(H, I, &side, 1, splits, stream);
+      launch_expand<T>(H, fiona::ExpandParams{I, H->part[0], A.scaling, A.B, A.base, A.y, A.base_row, A.y_row, D.d_out,
+                                              D.max_rank, splits, 0, 0}, stream);
+      return;
+    }
     hipLaunchKernelGGL(fiona::adapter_inner_kernel<T>, dim3(A.n_tok, D.max_rank, 1), dim3(64), 0, stream, P);
     hipLaunchKernelGGL(fiona::adapter_outer_kernel<T>, dim3(A.n_tok, (D.d_out + 255) / 256), dim3(256), 0, stream, P, false);
   });
@@ -216,6 +319,7 @@ int fiona_adapter_backward(const fiona_adapters *H, const fiona_adapter_args *ar
   if (rc != FIONA_OK) return rc;
   const fiona_adapter_args &A = *args;
   const fiona_adapters_desc &D = H->desc;
+  if (D.flags & FIONA_ADAPTERS_FORWARD_ONLY) return FIONA_ERR_ARG;
   if (!A.dA || !A.dB || (A.n_tok && (!A.dy || !A.dx))) return FIONA_ERR_ARG;
   const uint64_t e = type_size(D.type), n = A.n_tok;
   if (misaligned(A.dy, e) || misaligned(A.dx_base, e) || misaligned(A.dx, e) || misaligned(A.dA, e) || misaligned(A.dB, e))
@@ -233,6 +337,36 @@ int fiona_adapter_backward(const fiona_adapters *H, const fiona_adapter_args *ar
   P.dy_row = A.dy_row, P.dx_base_row = A.dx_base_row, P.dx_row = A.dx_row;
   with_type(D.type, [&](auto t) {
     using T = decltype(t);
+    if (!narrow(D)) {
+      const uint32_t splits = splits_of(std::max(1u, A.n_tok), D.n_adapter), blocks = blocks_of(A.n_tok);
+      const fiona::AdapterIds I{A.ids, A.ranks, A.n_tok, D.n_adapter, D.max_rank};
+      if (A.n_tok) {
+        hipLaunchKernelGGL(fiona::transpose_kernel<T>, dim3((D.d_in + 63) / 64 + (D.d_out + 63) / 64, D.n_adapter), dim3(256), 0,
+                           stream, fiona::TransposeParams{I, A.A, A.B, H->AT, H->BT, D.d_in, D.d_out, H->RP});
+        const fiona::ShrinkSide sides[2] = {{A.x, A.A, H->part[0], A.x_row, D.d_in, D.max_rank},
+                                            {A.dy, H->BT, H->part[1], A.dy_row, D.d_out, H->RP}};
+        launch_shrink<T>(H, I, sides, 2, splits, stream);
+        hipLaunchKernelGGL(fiona::inner_kernel<T>, dim3(blocks, (H->RP + 31) / 32, 2), dim3(256), 0, stream,
+                           fiona::InnerParams{I, {H->part[0], H->part[1]}, A.scaling, H->g, {H->column[0], H->column[1]},
+                                              H->RP, blocks * 64, splits});
+        launch_expand<T>(H, fiona::ExpandParams{I, H->g, nullptr, H->AT, A.dx_base, A.dx, A.dx_base_row, A.dx_row, D.d_in,
+                                                H->RP, 1, 0, 0}, stream);
+      }
+      fiona::GradParams G{};
+      G.I = I, G.RP = H->RP, G.n_pad = blocks * 64, G.r_chunks = (H->RP + 63) / 64;
+      G.splits = (uint32_t)std::min<uint64_t>(H->grad_splits, grad_splits_of(D, H->RP, A.n_tok));
+      G.per_split = (std::max(1u, A.n_tok) + G.splits * 64 - 1) / (G.splits * 64) * 64;
+      G.side[0] = {A.x, H->column[1], A.dA, H->grad[0], A.x_row, D.d_in, grad_slices(D.d_in, D.type)};
+      G.side[1] = {A.dy, H->column[0], A.dB, H->grad[1], A.dy_row, D.d_out, grad_slices(D.d_out, D.type)};
+      const dim3 grid(G.side[0].slices + G.side[1].slices, D.n_adapter * G.r_chunks, G.splits);
+      if (H->RP == 16) hipLaunchKernelGGL((fiona::grad_kernel<T, 1>), grid, dim3(512), 0, stream, G);
+      else if (H->RP == 32) hipLaunchKernelGGL((fiona::grad_kernel<T, 2>), grid, dim3(512), 0, stream, G);
+      else hipLaunchKernelGGL((fiona::grad_kernel<T, 4>), grid, dim3(512), 0, stream, G);
+      if (G.splits > 1)
+        hipLaunchKernelGGL(fiona::grad_sum_kernel<T>, dim3((uint32_t)((wa + wb + 255) / 256)), dim3(256), 0, stream,
+                           fiona::GradSumParams{{H->grad[0], H->grad[1]}, {A.dA, A.dB}, {wa, wb}, G.splits});
+      return;
+    }
     if (A.n_tok) {
       hipLaunchKernelGGL(fiona::adapter_inner_kernel<T>, dim3(A.n_tok, D.max_rank, 2), dim3(64), 0, stream, P);
       hipLaunchKernelGGL(fiona::adapter_outer_kernel<T>, dim3(A.n_tok, (D.d_in + 255) / 256), dim3(256), 0, stream, P, true);

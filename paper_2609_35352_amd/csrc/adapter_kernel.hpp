@@ -1,0 +1,558 @@
+// Kernels of fiona_adapter_linear and fiona_adapter_backward.
+//
+// An adapter's product goes through its rank: h = A x is a few numbers a token,
+// y = base + c B h as long as the row.  So a call is two passes, each bound by
+// the rows it reads or writes: `shrink` contracts rows with A into partial sums
+// of h (split over the row where there are few tokens), `expand` adds them up,
+// multiplies by B and adds the base row.  The backward pass is the same two
+// passes on dy with the factors transposed, and `grad`, which contracts over
+// the tokens.
+//
+// Tokens come in any order.  A workgroup of shrink or expand takes 64 of them
+// and goes through the adapters among them (a ballot per adapter): one for a
+// prompt, up to 64 for single tokens, which are then spread over workgroups
+// (slots).  Products run on the matrix cores with all rows of a tile; rows of
+// other adapters are dropped on the way out.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "mma.hpp"
+
+namespace fiona {
+
+constexpr uint32_t kRows = 64;        // tokens of a workgroup in shrink and expand
+
+struct AdapterIds {
+  const int32_t *ids, *ranks;
+  uint32_t n_tok, n_adapter, R;
+};
+
+// The adapter of token t and its rank; rank 0 for none.
+__device__ __forceinline__ uint32_t adapter_rank(const AdapterIds &I, int32_t a) {
+  if ((uint32_t)a >= I.n_adapter) return 0;
+  if (!I.ranks) return I.R;
+  const int32_t r = I.ranks[a];
+  return r < 0 ? 0 : (uint32_t)r > I.R ? I.R : (uint32_t)r;
+}
+
+// Calls f(adapter or -1, its rank, the rows that have it) for every adapter
+// among the workgroup's rows whose turn it is; the same in every wavefront.
+template <typename F>
+__device__ __forceinline__ void for_adapters(const AdapterIds &I, uint32_t row0, uint32_t lane, uint32_t slot,
+                                             uint32_t slots, bool with_none, F f) {
+  const bool in = row0 + lane < I.n_tok;
+  int32_t id = in ? I.ids[row0 + lane] : -1;
+  const uint32_t rank = adapter_rank(I, id);
+  if (rank == 0) id = -1;
+  uint64_t left = __ballot(in && (with_none || rank > 0));
+  for (uint32_t i = 0; left; ++i) {
+    const int lead = __builtin_ctzll(left);
+    const int32_t a = __builtin_amdgcn_readlane(id, lead);
+    const uint64_t rows = __ballot(in && id == a) & left;
+    left &= ~rows;
+    if (i % slots == slot) f(a, (uint32_t)__builtin_amdgcn_readlane((int)rank, lead), rows, (uint32_t)lead);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// shrink: part[split][t][r] = sum over the split's columns of x_t[k] w_a[r][k]
+// ---------------------------------------------------------------------------
+struct ShrinkSide {
+  const void *x, *w;        // w [n_adapter][w_rows][K]
+  float *part;              // [splits][n_tok][16 RT]
+  uint64_t x_row;
+  uint32_t K, w_rows;
+};
+struct ShrinkParams {
+  AdapterIds I;
+  ShrinkSide side[2];
+  uint32_t splits, slots;
+};
+
+// Row pieces of 256 bytes pass through LDS to become fragments: rows are read
+// whole (16 lanes to a piece) and the factor's rows are shared by the
+// workgroup's four wavefronts, 16 tokens each.
+template <typename T, int RT>
+__global__ void __launch_bounds__(256) shrink_kernel(ShrinkParams P) {
+  constexpr uint32_t E = kLaneElems<T>, CE = 16 * E, RP = 16 * RT;
+  __shared__ alignas(16) uint8_t sx[kRows][272], sw[RP][272];
+  const ShrinkSide &S = P.side[blockIdx.z / P.slots];
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+  const uint32_t row0 = blockIdx.x * kRows, tr = threadIdx.x / 16, pc = threadIdx.x % 16;
+  const uint32_t chunks = (S.K + CE - 1) / CE, split = blockIdx.y;
+  const uint32_t c0 = chunks * split / P.splits, c1 = chunks * (split + 1) / P.splits;
+  for_adapters(P.I, row0, lane, blockIdx.z % P.slots, P.slots, false,
+               [&](int32_t a, uint32_t rank, uint64_t rows, uint32_t lead) {
+    const T *xr[4], *wr[RT];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t r = tr + 16 * i;
+      xr[i] = (const T *)S.x + (uint64_t)(row0 + (rows >> r & 1 ? r : lead)) * S.x_row;
+    }
+#pragma unroll
+    for (int j = 0; j < RT; ++j) {
+      const uint32_t r = tr + 16 * j;
+      wr[j] = (const T *)S.w + ((uint64_t)a * S.w_rows + (r < rank ? r : rank - 1)) * S.K;
+    }
+    f4 acc[RT];
+#pragma unroll
+    for (int j = 0; j < RT; ++j) acc[j] = (f4){0, 0, 0, 0};
+    u4 xv[4], wv[RT];
+    auto load = [&](uint32_t c) {
+      const uint32_t at = c * CE + pc * E;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xv[i] = load_once<T>(piece_at<T>(xr[i], at, S.K));
+#pragma unroll
+      for (int j = 0; j < RT; ++j) wv[j] = load_shared<T>(piece_at<T>(wr[j], at, S.K));
+    };
+    if (c0 < c1) load(c0);
+    for (uint32_t c = c0; c < c1; ++c) {
+      if ((c + 1) * CE > S.K) {
+        const uint32_t at = c * CE + pc * E;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xv[i] = piece_fix<T>(xv[i], at, S.K);
+#pragma unroll
+        for (int j = 0; j < RT; ++j) wv[j] = piece_fix<T>(wv[j], at, S.K);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *(u4 *)&sx[tr + 16 * i][pc * 16] = xv[i];
+#pragma unroll
+      for (int j = 0; j < RT; ++j) *(u4 *)&sw[tr + 16 * j][pc * 16] = wv[j];
+      __syncthreads();
+      if (c + 1 < c1) load(c + 1);
+      if ((rows >> (16 * wave) & 0xFFFF) == 0) continue;
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {
+        const u4 x = *(const u4 *)&sx[16 * wave + col][(f * 4 + grp) * 16];
+#pragma unroll
+        for (int j = 0; j < RT; ++j) acc[j] = mma<T>(x, *(const u4 *)&sw[16 * j + col][(f * 4 + grp) * 16], acc[j]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t r = 16 * wave + 4 * grp + i;
+      if (!(rows >> r & 1)) continue;
+      float *out = S.part + ((uint64_t)split * P.I.n_tok + row0 + r) * RP;
+#pragma unroll
+      for (int j = 0; j < RT; ++j) out[16 * j + col] = 16 * j + col < rank ? acc[j][i] : 0.f;   // (rows from rank on repeat another)
+    }
+  });
+}
+
+// ---------------------------------------------------------------------------
+// expand: out_t[o] = base_t[o] + c_a sum_r w_a[o][r] h_t[r],  h = sum of parts
+// ---------------------------------------------------------------------------
+struct ExpandParams {
+  AdapterIds I;
+  const float *part, *scaling;   // part [splits][n_tok][16 RT]; scaling may be null
+  const void *w, *base;          // w [n_adapter][O][w_cols]; base may be null
+  void *out;
+  uint64_t base_row, out_row;
+  uint32_t O, w_cols, splits, slots, slice;   // slice: columns of a workgroup, a multiple of 256
+};
+
+// A wavefront takes 64 columns of all 64 tokens at a time: the factor's rows
+// are fragments as they lie (contiguous, and shared through the caches), the
+// tokens' h stay in registers, and a tile of 16 tokens passes through LDS to
+// meet the base rows 128 or 256 bytes of a row at a time.
+template <typename T, int RT>
+__global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
+  constexpr uint32_t E = kLaneElems<T>, FK = kFragElems<T>, RP = 16 * RT;
+  constexpr int KF = (RP + FK - 1) / FK;
+  constexpr uint32_t LP = 64 / E, NI = 16 * LP / 64;    // lanes of a row's 64 columns, and rows of a lane in a tile of 16
+  __shared__ alignas(16) float so[4][16][68];
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+  const uint32_t row0 = blockIdx.y * kRows, tr = lane / LP, pc = lane % LP;
+  for_adapters(P.I, row0, lane, blockIdx.z, P.slots, true, [&](int32_t a, uint32_t rank, uint64_t rows, uint32_t lead) {
+    if (rank == 0 && P.base == P.out) return;
+    Wide<T, KF> h[4];
+    u4 mask[KF];
+    const T *wa = (const T *)P.w;
+    uint32_t wn = 0;
+    float scale = 1;
+    if (rank) {
+      wa += (uint64_t)a * P.O * P.w_cols;
+      const uint64_t left = (uint64_t)(P.I.n_adapter - a) * P.O * P.w_cols;
+      wn = left < 0x7FFFFFFF ? (uint32_t)left : 0x7FFFFFFF;
+      if (P.scaling) scale = P.scaling[a];
+#pragma unroll
+      for (int f = 0; f < KF; ++f) {
+        const uint32_t r = f * FK + grp * E;
+        mask[f] = first_mask<T>((int)rank - (int)r);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t row = 16 * t + col;
+          const bool mine = (rows >> row & 1) && r < RP;
+          const float *p = P.part + (uint64_t)(row0 + (mine ? row : lead)) * RP + (mine ? r : 0);
+          f4 x[E / 4];
+#pragma unroll
+          for (uint32_t e = 0; e < E / 4; ++e) x[e] = (f4){0, 0, 0, 0};
+          for (uint32_t s = 0; s < P.splits; ++s, p += (uint64_t)P.I.n_tok * RP)
+#pragma unroll
+            for (uint32_t e = 0; e < E / 4; ++e) x[e] += ((const f4 *)p)[e];
+          if (!mine)
+#pragma unroll
+            for (uint32_t e = 0; e < E / 4; ++e) x[e] = (f4){0, 0, 0, 0};
+          if constexpr (sizeof(T) == 4) {
+            h[t].hi[f] = __builtin_bit_cast(u4, x[0]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t lo;
+              h[t].hi[f][i] = split_pair(x[i / 2][2 * (i % 2)], x[i / 2][2 * (i % 2) + 1], lo);
+              h[t].lo[f][i] = lo;
+            }
+          }
+        }
+      }
+    }
+    const uint32_t end = blockIdx.x * P.slice + P.slice < P.O ? blockIdx.x * P.slice + P.slice : P.O;
+    for (uint32_t o0 = blockIdx.x * P.slice + 64 * wave; o0 < end; o0 += 256) {
+      // Base rows of all the tokens first: they come from memory.
+      const uint32_t at = o0 + pc * E;
+      u4 b[4][NI];
+      if (P.base) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (uint32_t i = 0; i < NI; ++i) {
+            const uint32_t row = 16 * t + tr + (64 / LP) * i;
+            b[t][i] = load_once<T>(piece_at<T>((const T *)P.base + (uint64_t)(row0 + (rows >> row & 1 ? row : lead)) * P.base_row, at, P.O));
+          }
+      }
+      u4 w[4][KF];
+      if (rank) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t o = o0 + 16 * u + col;
+#pragma unroll
+          for (int f = 0; f < KF; ++f)
+            w[u][f] = load_shared<T>(piece_at<T>(wa, (o < P.O ? o : P.O - 1) * P.w_cols + f * FK + grp * E, wn));
+        }
+        if ((o0 + 64) * P.w_cols + KF * FK > wn) {   // the table's end
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const uint32_t o = o0 + 16 * u + col;
+#pragma unroll
+            for (int f = 0; f < KF; ++f) w[u][f] = piece_fix<T>(w[u][f], (o < P.O ? o : P.O - 1) * P.w_cols + f * FK + grp * E, wn);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int f = 0; f < KF; ++f) w[u][f] &= mask[f];   // what an adapter's rank leaves out holds anything
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if ((rows >> (16 * t) & 0xFFFF) == 0) continue;
+        if (rank) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            f4 acc = (f4){0, 0, 0, 0};
+#pragma unroll
+            for (int f = 0; f < KF; ++f) acc = mma_wide<T>(w[u][f], h[t].hi[f], h[t].lo[sizeof(T) == 2 ? f : 0], acc);
+            *(f4 *)&so[wave][col][16 * u + 4 * grp] = acc * scale;
+          }
+          wave_sync();
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) {
+          const uint32_t row = 16 * t + tr + (64 / LP) * i;
+          f4 y[E / 4];
+#pragma unroll
+          for (uint32_t e = 0; e < E / 4; ++e)
+            y[e] = rank ? *(const f4 *)&so[wave][tr + (64 / LP) * i][pc * E + 4 * e] : (f4){0, 0, 0, 0};
+          if (P.base) {
+            u4 v = b[t][i];
+            if (o0 + 64 > P.O) v = piece_fix<T>(v, at, P.O);
+            if constexpr (sizeof(T) == 4) {
+              y[0] += __builtin_bit_cast(f4, v);
+            } else {
+              typedef T t8 __attribute__((ext_vector_type(8)));
+              const t8 z = __builtin_bit_cast(t8, v);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) y[e / 4][e % 4] += (float)z[e];
+            }
+          }
+          u4 out;
+          if constexpr (sizeof(T) == 4) {
+            out = __builtin_bit_cast(u4, y[0]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = pack2<T>(y[e / 2][2 * (e % 2)], y[e / 2][2 * (e % 2) + 1]);
+          }
+          if (!(rows >> row & 1)) continue;
+          T *p = (T *)P.out + (uint64_t)(row0 + row) * P.out_row + at;
+          if (at + E <= P.O) {
+            __builtin_nontemporal_store(out, (u4_any *)p);
+          } else {
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e) {
+              if (at + e >= P.O) break;
+              if constexpr (sizeof(T) == 4) ((uint32_t *)p)[e] = out[e];
+              else ((uint16_t *)p)[e] = (uint16_t)(out[e / 2] >> (16 * (e % 2)));
+            }
+          }
+        }
+      }
+    }
+  });
+}
+
+// ---------------------------------------------------------------------------
+// transpose: the factors for the backward pass, rows from the rank on zero
+// ---------------------------------------------------------------------------
+struct TransposeParams {
+  AdapterIds I;
+  const void *A, *B;
+  void *AT, *BT;                 // [n_adapter][d_in][RP], [n_adapter][RP][d_out]
+  uint32_t d_in, d_out, RP;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) transpose_kernel(TransposeParams P) {
+  __shared__ T tile[64][65];
+  const uint32_t a = blockIdx.y, nb_in = (P.d_in + 63) / 64, c = threadIdx.x % 64, q = threadIdx.x / 64;
+  const uint32_t rank = adapter_rank(P.I, (int32_t)a);
+  const bool of_b = blockIdx.x >= nb_in;
+  const uint32_t n = of_b ? P.d_out : P.d_in, k0 = (blockIdx.x - (of_b ? nb_in : 0)) * 64;
+  for (uint32_t r0 = 0; r0 < P.RP; r0 += 64) {
+    if (r0) __syncthreads();
+    for (uint32_t i = q; i < 64; i += 4) {
+      const uint32_t k = k0 + (of_b ? i : c), r = r0 + (of_b ? c : i);
+      T v = (T)0.f;
+      if (k < n && r < rank)
+        v = of_b ? ((const T *)P.B)[((uint64_t)a * n + k) * P.I.R + r] : ((const T *)P.A)[((uint64_t)a * P.I.R + r) * n + k];
+      tile[i][c] = v;
+    }
+    __syncthreads();
+    for (uint32_t i = q; i < 64; i += 4) {
+      const uint32_t k = k0 + (of_b ? c : i), r = r0 + (of_b ? i : c);
+      if (k >= n || r >= P.RP) continue;
+      if (of_b) ((T *)P.BT)[((uint64_t)a * P.RP + r) * n + k] = tile[c][i];
+      else ((T *)P.AT)[((uint64_t)a * n + k) * P.RP + r] = tile[c][i];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// inner: parts of h and g summed and scaled; g as rows for dx, both as columns
+// of tokens for the gradients, in two bfloat16 parts for 16-bit types
+// ---------------------------------------------------------------------------
+struct InnerParams {
+  AdapterIds I;
+  const float *part[2], *scaling;   // of h, of g
+  float *g;                         // [n_tok][RP]
+  void *column[2];                  // [2 parts][RP][n_pad] bfloat16, or [RP][n_pad] float32
+  uint32_t RP, n_pad, splits;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) inner_kernel(InnerParams P) {
+  __shared__ float tile[32][65];
+  const uint32_t side = blockIdx.z, row0 = blockIdx.x * 64, r0 = blockIdx.y * 32;
+  for (uint32_t e = threadIdx.x; e < 64 * 32; e += 256) {
+    const uint32_t t = row0 + e / 32, r = r0 + e % 32;
+    float x = 0;
+    if (t < P.I.n_tok && r < P.RP) {
+      const int32_t a = P.I.ids[t];
+      if (adapter_rank(P.I, a)) {
+        const float *p = P.part[side] + (uint64_t)t * P.RP + r;
+        for (uint32_t s = 0; s < P.splits; ++s, p += (uint64_t)P.I.n_tok * P.RP) x += *p;
+        if (P.scaling) x *= P.scaling[a];
+      }
+      if (side == 1) P.g[(uint64_t)t * P.RP + r] = x;
+    }
+    tile[e % 32][e / 32] = x;
+  }
+  __syncthreads();
+  for (uint32_t e = threadIdx.x; e < 32 * 64; e += 256) {
+    const uint32_t r = r0 + e / 64, t = row0 + e % 64;
+    if (r >= P.RP) continue;
+    const float x = tile[e / 64][e % 64];
+    const uint64_t at = (uint64_t)r * P.n_pad + t;
+    if constexpr (sizeof(T) == 4) {
+      ((float *)P.column[side])[at] = x;
+    } else {
+      const __bf16 hi = (__bf16)x;
+      ((__bf16 *)P.column[side])[at] = hi;
+      ((__bf16 *)P.column[side])[(uint64_t)P.RP * P.n_pad + at] = (__bf16)(x - (float)hi);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// grad: dA_a[r] = sum_t g_t[r] x_t and dB_a[.][r] = sum_t c h_t[r] dy_t
+// ---------------------------------------------------------------------------
+struct GradSide {
+  const void *x, *column;
+  void *out;                 // dA [n_adapter][R][n] or dB [n_adapter][n][R]
+  float *part;               // the same in 32 bits, [splits] times, where the tokens are split
+  uint64_t x_row;
+  uint32_t n, slices;
+};
+struct GradParams {
+  AdapterIds I;
+  GradSide side[2];
+  uint32_t RP, n_pad, splits, per_split, r_chunks;   // per_split: tokens, a multiple of 64
+};
+template <typename T>
+constexpr uint32_t kGradTokens = sizeof(T) == 2 ? 32 : 16;    // tokens of a step
+template <typename T>
+constexpr uint32_t kGradCols = 16 * kLaneElems<T>;            // columns of a workgroup
+constexpr uint32_t kGradWaves = 8;
+
+// A workgroup takes 256 bytes of the rows' columns for one adapter and up to 64
+// of its ranks; its eight wavefronts take the steps that hold a token of the
+// adapter in turn.  Rows are read whole pieces at a time, 16 lanes to a piece,
+// eight tokens to a lane; the transposed fragments (columns x tokens) are
+// picked from the tokens' words in registers, as values are in the attention.
+template <typename T, int RT>
+__global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
+  constexpr uint32_t E = kLaneElems<T>, TB = kGradTokens<T>, SP = TB / 4;
+  __shared__ float so[kGradWaves][16][kGradCols<T>];   // column c of rank r at c ^ 4 r, off each other's banks
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+  const bool second = blockIdx.x >= P.side[0].slices;
+  const GradSide &S = P.side[second];
+  const uint32_t slice = blockIdx.x - (second ? P.side[0].slices : 0), c0 = slice * kGradCols<T>;
+  const uint32_t a = blockIdx.y / P.r_chunks, n0 = blockIdx.y % P.r_chunks * 64, split = blockIdx.z;
+  const uint32_t rank = adapter_rank(P.I, (int32_t)a);
+  const uint32_t t0 = split * P.per_split, t1 = t0 + P.per_split < P.I.n_tok ? t0 + P.per_split : P.I.n_tok;
+  f4 acc[E][RT];
+#pragma unroll
+  for (uint32_t u = 0; u < E; ++u)
+#pragma unroll
+    for (int j = 0; j < RT; ++j) acc[u][j] = (f4){0, 0, 0, 0};
+
+  // The lane's columns; at the row's end they step back to its last 16 bytes
+  // (and are dropped on the way out where another lane has them).
+  const uint32_t at = c0 + col * E, cat = at + E <= S.n ? at : S.n - E;
+  u4 x[SP], hi[RT], lo[sizeof(T) == 2 ? RT : 1];
+  int32_t id[SP];
+  auto load = [&](uint32_t step) {   // (its first token)
+    const uint32_t t = step + grp * SP;
+#pragma unroll
+    for (uint32_t j = 0; j < SP; ++j) {
+      const uint32_t row = t + j < t1 ? t + j : t1 - 1;
+      x[j] = load_once<T>((const T *)S.x + (uint64_t)row * S.x_row + cat);
+      id[j] = P.I.ids[row];
+    }
+#pragma unroll
+    for (int j = 0; j < RT; ++j) {
+      const uint64_t r = (uint64_t)(n0 + 16 * j + col) * P.n_pad + t;
+      if constexpr (sizeof(T) == 4) {
+        hi[j] = *(const u4 *)((const float *)S.column + r);
+      } else {
+        hi[j] = *(const u4 *)((const __bf16 *)S.column + r);
+        lo[j] = *(const u4 *)((const __bf16 *)S.column + (uint64_t)P.RP * P.n_pad + r);
+      }
+    }
+  };
+  for (uint32_t w0 = t0; rank > n0 && w0 < t1; w0 += 64 * TB) {
+    // Which of 64 steps hold a token of the adapter (a step per lane), and this
+    // wavefront's: every eighth of them.
+    bool any = false;
+    if (w0 + lane * TB < t1)
+      for (uint32_t i = 0; i < TB; ++i) any |= P.I.ids[w0 + lane * TB + i < t1 ? w0 + lane * TB + i : t1 - 1] == (int32_t)a;
+    uint64_t steps = __ballot(any), mine = 0;
+    for (uint32_t i = 0; steps; ++i, steps &= steps - 1)
+      if (i % kGradWaves == wave) mine |= steps & -steps;
+    if (mine) load(w0 + __builtin_ctzll(mine) * TB);
+    while (mine) {
+      const uint32_t t = w0 + __builtin_ctzll(mine) * TB + grp * SP;
+      mine &= mine - 1;
+      // Rows of other adapters count nothing, whatever they hold.
+      bool whole = true;
+      bool live[SP];
+#pragma unroll
+      for (uint32_t j = 0; j < SP; ++j) {
+        live[j] = (int)(t + j < t1) & (int)(id[j] == (int32_t)a);
+        whole &= live[j];
+      }
+      if (!__all(whole)) {
+#pragma unroll
+        for (uint32_t j = 0; j < SP; ++j) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[j][i] = live[j] ? x[j][i] : 0;
+          const uint32_t keep = live[j] ? 0 : sizeof(T) == 4 ? ~0u : 0xFFFFu << (16 * (j % 2));
+#pragma unroll
+          for (int i = 0; i < RT; ++i) {
+            hi[i][sizeof(T) == 4 ? j : j / 2] &= ~keep;
+            if constexpr (sizeof(T) == 2) lo[i][j / 2] &= ~keep;
+          }
+        }
+      }
+      u4 y[SP], vh[RT], vl[RT];
+#pragma unroll
+      for (uint32_t j = 0; j < SP; ++j) y[j] = x[j];
+#pragma unroll
+      for (int j = 0; j < RT; ++j) {
+        vh[j] = hi[j];
+        if constexpr (sizeof(T) == 2) vl[j] = lo[j];
+      }
+      if (mine) load(w0 + __builtin_ctzll(mine) * TB);
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (uint32_t u = 0; u < E; ++u)
+#pragma unroll
+          for (int j = 0; j < RT; ++j) acc[u][j] = mma<T>((u4){y[0][u], y[1][u], y[2][u], y[3][u]}, vh[j], acc[u][j]);
+      } else {
+#pragma unroll
+        for (uint32_t u = 0; u < E; ++u) {
+          u4 f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[i] = u & 1 ? pair_high(y[2 * i][u / 2], y[2 * i + 1][u / 2]) : pair_low(y[2 * i][u / 2], y[2 * i + 1][u / 2]);
+#pragma unroll
+          for (int j = 0; j < RT; ++j) acc[u][j] = mma_wide<T>(f, vh[j], vl[j], acc[u][j]);
+        }
+      }
+    }
+  }
+
+  // The wavefronts' sums, 16 ranks at a time.  acc[u][j][i]: column (4 grp + i) of the
+  // slice's 16 lanes, its element u; rank n0 + 16 j + col.
+#pragma unroll
+  for (int j = 0; j < RT; ++j) {
+    __syncthreads();
+#pragma unroll
+    for (uint32_t u = 0; u < E; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) so[wave][col][((4 * grp + i) * E + u) ^ (4 * col)] = acc[u][j][i];
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < 16 * kGradCols<T>; e += 512) {
+      // dA: consecutive threads along the columns; dB: along the ranks
+      const uint32_t r = second ? e % 16 : e / kGradCols<T>, c = second ? e / 16 : e % kGradCols<T>;
+      float s = 0;
+#pragma unroll
+      for (uint32_t w = 0; w < kGradWaves; ++w) s += so[w][r][c ^ (4 * r)];
+      // Column c of the slice is element c % E of lane c / E, whose columns may have stepped back.
+      const uint32_t want = c0 + c / E * E, from = want + E <= S.n ? want : S.n - E, k = from + c % E;
+      const uint32_t rr = n0 + 16 * j + r;
+      if (k < want || want >= S.n || rr >= P.I.R) continue;
+      const uint64_t o = second ? ((uint64_t)a * S.n + k) * P.I.R + rr : ((uint64_t)a * P.I.R + rr) * S.n + k;
+      if (rr >= rank) s = 0;   // (a NaN row times the zeros there)
+      if (P.splits > 1) S.part[(uint64_t)split * P.I.n_adapter * P.I.R * S.n + o] = s;
+      else ((T *)S.out)[o] = (T)s;
+    }
+  }
+}
+
+// The splits' sums of a gradient, rounded once.
+struct GradSumParams {
+  const float *part[2];
+  void *out[2];
+  uint64_t n[2];
+  uint32_t splits;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) grad_sum_kernel(GradSumParams P) {
+  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint32_t side = i >= P.n[0];
+  const uint64_t k = i - (side ? P.n[0] : 0);
+  if (k >= P.n[side]) return;
+  float s = 0;
+  for (uint32_t j = 0; j < P.splits; ++j) s += P.part[side][(uint64_t)j * P.n[side] + k];
+  ((T *)P.out[side])[k] = (T)s;
+}
+
+}  // namespace fiona

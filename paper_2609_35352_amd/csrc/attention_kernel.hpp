@@ -209,6 +209,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
       }
     page = page_next, place = place_next;
     load_k(base + step);
+    wave_sync();
 
     f4 acc[RT];
 #pragma unroll

@@ -67,6 +67,81 @@ __device__ __forceinline__ void load_row(const T *p, int valid, uint32_t (&w)[W 
   }
 }
 
+// A lane's 16 bytes of a row of n >= kLaneElems elements, from element `at`.
+// piece_at gives an address inside the row whatever `at` is (the row's last 16
+// bytes where fewer follow), so that loads need no branch; piece_fix then
+// moves what was loaded to its place, zero from n on.  Rows start at any
+// element: the memory system takes 16-byte accesses at any address.
+typedef u4 u4_any __attribute__((aligned(2)));
+template <typename T>
+__device__ __forceinline__ const T *piece_at(const T *row, uint32_t at, uint32_t n) {
+  return row + (at + kLaneElems<T> <= n ? at : n - kLaneElems<T>);
+}
+template <typename T>
+__device__ __forceinline__ u4 piece_fix(u4 v, uint32_t at, uint32_t n) {
+  if (at + kLaneElems<T> <= n) return v;
+  if (at >= n) return (u4){0, 0, 0, 0};
+  const uint32_t bits = (at + kLaneElems<T> - n) * 8 * sizeof(T);
+  return __builtin_bit_cast(u4, __builtin_bit_cast(unsigned __int128, v) >> bits);
+}
+// Read once per call (past the caches), or by many workgroups.
+template <typename T>
+__device__ __forceinline__ u4 load_once(const T *p) {
+  return __builtin_nontemporal_load((const u4_any *)p);
+}
+template <typename T>
+__device__ __forceinline__ u4 load_shared(const T *p) {
+  return *(const u4_any *)p;
+}
+
+// The first `valid` elements of a lane's 16 bytes as a mask.
+template <typename T>
+__device__ __forceinline__ u4 first_mask(int valid) {
+  u4 m;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) m[i] = i < valid ? ~0u : 0;
+    else m[i] = 2 * i + 1 < valid ? ~0u : 2 * i < valid ? 0xFFFFu : 0;
+  }
+  return m;
+}
+
+// 32-bit values for a contraction with rows of T: in 16 bits as the sum of two
+// bfloat16 parts (an error of 2^-16 of the value, and its whole range; one part
+// would lose 2^-8, binary16 its range as well).
+template <typename T, int KF>
+struct Wide {
+  u4 hi[KF], lo[sizeof(T) == 2 ? KF : 1];
+};
+__device__ __forceinline__ uint32_t split_pair(float a, float b, uint32_t &lo) {
+  typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+  const bf2 h = {(__bf16)a, (__bf16)b};
+  const bf2 l = {(__bf16)(a - (float)h[0]), (__bf16)(b - (float)h[1])};
+  lo = __builtin_bit_cast(uint32_t, l);
+  return __builtin_bit_cast(uint32_t, h);
+}
+
+// c += a * w, a a fragment of T, w one of 32-bit values in two parts.  binary16
+// rows are split the same way, exactly (11 bits).
+template <typename T>
+__device__ __forceinline__ f4 mma_wide(u4 a, u4 hi, u4 lo, f4 c) {
+  if constexpr (sizeof(T) == 4) {
+    return mma<T>(a, hi, c);
+  } else if constexpr (__is_same(T, _Float16)) {
+    const h8 x = __builtin_bit_cast(h8, a);
+    u4 ah, al;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t l;
+      ah[i] = split_pair((float)x[2 * i], (float)x[2 * i + 1], l);
+      al[i] = l;
+    }
+    return mma<__bf16>(ah, hi, mma<__bf16>(ah, lo, mma<__bf16>(al, hi, c)));
+  } else {
+    return mma<T>(a, hi, mma<T>(a, lo, c));
+  }
+}
+
 // Two values rounded to 16 bits, the first in the low half.
 template <typename T>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -79,6 +154,12 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // The halves of two rows' words side by side: (low a, low b) or (high a, high b).
 __device__ __forceinline__ uint32_t pair_low(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t pair_high(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+// What one lane of a wavefront wrote to LDS another reads next.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
 // Sum and maximum over the four lanes of one column (l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float column_max(float x) {
