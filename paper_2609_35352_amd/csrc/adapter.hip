@@ -19,9 +19,10 @@ struct fiona_adapters {
   uint64_t part_cap = 0, grad_splits = 1;
   char *ws = nullptr;
   // Into ws.  part: sums of h and g; g: whole g; column: h and g by rank; AT, BT:
-  // the factors transposed; grad: a split's gradients.
+  // the factors transposed; grad: a split's gradients; ids: whole steps of them.
   float *part[2] = {}, *g = nullptr, *grad[2] = {};
   void *column[2] = {}, *AT = nullptr, *BT = nullptr;
+  int32_t *ids = nullptr;
 };
 
 // Rows below kMinWidth elements, too short for 16-byte pieces: one value per
@@ -139,15 +140,15 @@ uint32_t blocks_of(uint64_t n) { return (uint32_t)((n + fiona::kRows - 1) / fion
 // Workgroups that share the adapters among 64 tokens: many where there are few
 // tokens, as each may have its own.
 uint32_t slots_of(uint32_t n, uint32_t adapters) {
-  const uint32_t want = std::max(1u, 64 / blocks_of(n));
+  const uint32_t want = std::max(1u, 256 / blocks_of(n));
   return std::min({want, adapters, std::min(n, fiona::kRows)});
 }
 
 constexpr uint32_t kMaxSplits = 8, kWorkgroups = 1024, kGradWorkgroups = 512;
 
 // Parts of a row's contraction: enough workgroups to fill the GPU.
-uint32_t splits_of(uint32_t n, uint32_t adapters) {
-  const uint32_t wgs = blocks_of(n) * slots_of(n, adapters);
+uint32_t splits_of(uint32_t n, uint32_t adapters, uint32_t sides) {
+  const uint32_t wgs = blocks_of(n) * slots_of(n, adapters) * sides;
   return std::max(1u, std::min(kMaxSplits, (kWorkgroups + wgs - 1) / wgs));
 }
 
@@ -246,7 +247,7 @@ int fiona_adapters_create(const fiona_adapters_desc *desc, fiona_adapters **out)
   const bool both = !(D.flags & FIONA_ADAPTERS_FORWARD_ONLY);
   const uint64_t e = type_size(D.type), n_pad = (uint64_t)blocks_of(D.max_tokens) * 64, RP = H->RP;
   for (uint32_t n = std::min(64u, D.max_tokens);; n = std::min(n + 64, D.max_tokens)) {
-    H->part_cap = std::max<uint64_t>(H->part_cap, (uint64_t)n * splits_of(n, D.n_adapter));
+    H->part_cap = std::max<uint64_t>(H->part_cap, (uint64_t)n * splits_of(n, D.n_adapter, 1));
     if (n == D.max_tokens) break;
   }
   H->part_cap = std::max<uint64_t>(H->part_cap, 64 * kMaxSplits);   // (fewer than 64 tokens)
@@ -256,17 +257,17 @@ int fiona_adapters_create(const fiona_adapters_desc *desc, fiona_adapters **out)
   const uint64_t size[] = {H->part_cap * RP * 4, both ? H->part_cap * RP * 4 : 0, both ? D.max_tokens * RP * 4 : 0,
                            both ? n_pad * RP * 4 : 0, both ? n_pad * RP * 4 : 0,
                            both ? RP * D.n_adapter * D.d_in * e : 0, both ? RP * D.n_adapter * D.d_out * e : 0,
-                           both ? grads * D.d_in : 0, both ? grads * D.d_out : 0};
-  uint64_t at[10] = {0};
-  for (int i = 0; i < 9; ++i) at[i + 1] = at[i] + (size[i] + 255) / 256 * 256;
-  if (hipMalloc((void **)&H->ws, at[9]) != hipSuccess) {
+                           both ? grads * D.d_in : 0, both ? grads * D.d_out : 0, both ? n_pad * 4 : 0};
+  uint64_t at[11] = {0};
+  for (int i = 0; i < 10; ++i) at[i + 1] = at[i] + (size[i] + 255) / 256 * 256;
+  if (hipMalloc((void **)&H->ws, at[10]) != hipSuccess) {
     (void)hipGetLastError();
     delete H;
     return FIONA_ERR_NOMEM;
   }
   H->part[0] = (float *)(H->ws + at[0]), H->part[1] = (float *)(H->ws + at[1]), H->g = (float *)(H->ws + at[2]);
   H->column[0] = H->ws + at[3], H->column[1] = H->ws + at[4], H->AT = H->ws + at[5], H->BT = H->ws + at[6];
-  H->grad[0] = (float *)(H->ws + at[7]), H->grad[1] = (float *)(H->ws + at[8]);
+  H->grad[0] = (float *)(H->ws + at[7]), H->grad[1] = (float *)(H->ws + at[8]), H->ids = (int32_t *)(H->ws + at[9]);
   *out = H;
   return FIONA_OK;
 }
@@ -299,7 +300,7 @@ int fiona_adapter_linear(const fiona_adapters *H, const fiona_adapter_args *args
   with_type(D.type, [&](auto t) {
     using T = decltype(t);
     if (!narrow(D)) {
-      const uint32_t splits = splits_of(A.n_tok, D.n_adapter);
+      const uint32_t splits = splits_of(A.n_tok, D.n_adapter, 1);
       const fiona::AdapterIds I{A.ids, A.ranks, A.n_tok, D.n_adapter, D.max_rank};
       const fiona::ShrinkSide side{A.x, A.A, H->part[0], A.x_row, D.d_in, D.max_rank};
       launch_shrink<T>(H, I, &side, 1, splits, stream);
@@ -338,7 +339,7 @@ int fiona_adapter_backward(const fiona_adapters *H, const fiona_adapter_args *ar
   with_type(D.type, [&](auto t) {
     using T = decltype(t);
     if (!narrow(D)) {
-      const uint32_t splits = splits_of(std::max(1u, A.n_tok), D.n_adapter), blocks = blocks_of(A.n_tok);
+      const uint32_t splits = splits_of(std::max(1u, A.n_tok), D.n_adapter, 2), blocks = blocks_of(A.n_tok);
       const fiona::AdapterIds I{A.ids, A.ranks, A.n_tok, D.n_adapter, D.max_rank};
       if (A.n_tok) {
         hipLaunchKernelGGL(fiona::transpose_kernel<T>, dim3((D.d_in + 63) / 64 + (D.d_out + 63) / 64, D.n_adapter), dim3(256), 0,
@@ -347,13 +348,13 @@ int fiona_adapter_backward(const fiona_adapters *H, const fiona_adapter_args *ar
                                             {A.dy, H->BT, H->part[1], A.dy_row, D.d_out, H->RP}};
         launch_shrink<T>(H, I, sides, 2, splits, stream);
         hipLaunchKernelGGL(fiona::inner_kernel<T>, dim3(blocks, (H->RP + 31) / 32, 2), dim3(256), 0, stream,
-                           fiona::InnerParams{I, {H->part[0], H->part[1]}, A.scaling, H->g, {H->column[0], H->column[1]},
+                           fiona::InnerParams{I, {H->part[0], H->part[1]}, A.scaling, H->g, H->ids, {H->column[0], H->column[1]},
                                               H->RP, blocks * 64, splits});
         launch_expand<T>(H, fiona::ExpandParams{I, H->g, nullptr, H->AT, A.dx_base, A.dx, A.dx_base_row, A.dx_row, D.d_in,
                                                 H->RP, 1, 0, 0}, stream);
       }
       fiona::GradParams G{};
-      G.I = I, G.RP = H->RP, G.n_pad = blocks * 64, G.r_chunks = (H->RP + 63) / 64;
+      G.I = I, G.ids = H->ids, G.RP = H->RP, G.n_pad = blocks * 64, G.r_chunks = (H->RP + 63) / 64;
       G.splits = (uint32_t)std::min<uint64_t>(H->grad_splits, grad_splits_of(D, H->RP, A.n_tok));
       G.per_split = (std::max(1u, A.n_tok) + G.splits * 64 - 1) / (G.splits * 64) * 64;
       G.side[0] = {A.x, H->column[1], A.dA, H->grad[0], A.x_row, D.d_in, grad_slices(D.d_in, D.type)};

@@ -153,21 +153,37 @@ struct ExpandParams {
   uint32_t O, w_cols, splits, slots, slice;   // slice: columns of a workgroup, a multiple of 256
 };
 
-// A wavefront takes 64 columns of all 64 tokens at a time: the factor's rows
-// are fragments as they lie (contiguous, and shared through the caches), the
-// tokens' h stay in registers, and a tile of 16 tokens passes through LDS to
-// meet the base rows 128 or 256 bytes of a row at a time.
+// The workgroup first adds up its tokens' parts of h and keeps them in LDS as
+// fragments (two bfloat16 parts for 16-bit types).  A wavefront then takes 64
+// columns of all 64 tokens at a time: the factor's rows are fragments as they
+// lie (contiguous, and shared through the caches), and a tile of 16 tokens
+// passes through LDS to meet the base rows 128 or 256 bytes of a row at a time.
 template <typename T, int RT>
 __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
   constexpr uint32_t E = kLaneElems<T>, FK = kFragElems<T>, RP = 16 * RT;
-  constexpr int KF = (RP + FK - 1) / FK;
+  constexpr int KF = (RP + FK - 1) / FK, PARTS = sizeof(T) == 2 ? 2 : 1;
   constexpr uint32_t LP = 64 / E, NI = 16 * LP / 64;    // lanes of a row's 64 columns, and rows of a lane in a tile of 16
+  constexpr uint32_t HB = KF * 64;                      // bytes of a token's h, and of its second part
   __shared__ alignas(16) float so[4][16][68];
+  __shared__ alignas(16) uint8_t sh[kRows][PARTS * HB + 16];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
   const uint32_t row0 = blockIdx.y * kRows, tr = lane / LP, pc = lane % LP;
+  const uint32_t end = blockIdx.x * P.slice + P.slice < P.O ? blockIdx.x * P.slice + P.slice : P.O;
   for_adapters(P.I, row0, lane, blockIdx.z, P.slots, true, [&](int32_t a, uint32_t rank, uint64_t rows, uint32_t lead) {
     if (rank == 0 && P.base == P.out) return;
-    Wide<T, KF> h[4];
+    uint32_t o0 = blockIdx.x * P.slice + 64 * wave;
+    // Base rows come from memory: the first ones are on their way while h is added up.
+    u4 b[4][NI];
+    auto load_base = [&](uint32_t o) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) {
+          const uint32_t row = 16 * t + tr + (64 / LP) * i;
+          b[t][i] = load_once<T>(piece_at<T>((const T *)P.base + (uint64_t)(row0 + (rows >> row & 1 ? row : lead)) * P.base_row, o + pc * E, P.O));
+        }
+    };
+    if (P.base && o0 < end) load_base(o0);
     u4 mask[KF];
     const T *wa = (const T *)P.w;
     uint32_t wn = 0;
@@ -178,50 +194,47 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
       wn = left < 0x7FFFFFFF ? (uint32_t)left : 0x7FFFFFFF;
       if (P.scaling) scale = P.scaling[a];
 #pragma unroll
-      for (int f = 0; f < KF; ++f) {
-        const uint32_t r = f * FK + grp * E;
-        mask[f] = first_mask<T>((int)rank - (int)r);
+      for (int f = 0; f < KF; ++f) mask[f] = first_mask<T>((int)rank - (int)(f * FK + grp * E));
+      // h: a thread takes four ranks of RT tokens.
+      f4 x[RT];
+      const float *p[RT];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const uint32_t row = 16 * t + col;
-          const bool mine = (rows >> row & 1) && r < RP;
-          const float *p = P.part + (uint64_t)(row0 + (mine ? row : lead)) * RP + (mine ? r : 0);
-          f4 x[E / 4];
+      for (int j = 0; j < RT; ++j) {
+        const uint32_t e = threadIdx.x + 256 * j, row = e / (RP / 4);
+        x[j] = (f4){0, 0, 0, 0};
+        p[j] = P.part + (uint64_t)(row0 + (rows >> row & 1 ? row : lead)) * RP + e % (RP / 4) * 4;
+      }
+#pragma unroll 4
+      for (uint32_t s = 0; s < P.splits; ++s)
 #pragma unroll
-          for (uint32_t e = 0; e < E / 4; ++e) x[e] = (f4){0, 0, 0, 0};
-          for (uint32_t s = 0; s < P.splits; ++s, p += (uint64_t)P.I.n_tok * RP)
+        for (int j = 0; j < RT; ++j) x[j] += *(const f4 *)(p[j] + (uint64_t)s * P.I.n_tok * RP);
+      __syncthreads();   // (the last adapter's fragments are read)
 #pragma unroll
-            for (uint32_t e = 0; e < E / 4; ++e) x[e] += ((const f4 *)p)[e];
-          if (!mine)
+      for (int j = 0; j < RT; ++j) {
+        const uint32_t e = threadIdx.x + 256 * j, row = e / (RP / 4), r = e % (RP / 4) * 4;
+        if (!(rows >> row & 1)) x[j] = (f4){0, 0, 0, 0};
+        if constexpr (sizeof(T) == 4) {
+          *(f4 *)&sh[row][r * 4] = x[j];
+        } else {
+          u2 hi, lo;
 #pragma unroll
-            for (uint32_t e = 0; e < E / 4; ++e) x[e] = (f4){0, 0, 0, 0};
-          if constexpr (sizeof(T) == 4) {
-            h[t].hi[f] = __builtin_bit_cast(u4, x[0]);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t lo;
-              h[t].hi[f][i] = split_pair(x[i / 2][2 * (i % 2)], x[i / 2][2 * (i % 2) + 1], lo);
-              h[t].lo[f][i] = lo;
-            }
+          for (int i = 0; i < 2; ++i) {
+            uint32_t l;
+            hi[i] = split_pair(x[j][2 * i], x[j][2 * i + 1], l);
+            lo[i] = l;
           }
+          *(u2 *)&sh[row][r * 2] = hi;
+          *(u2 *)&sh[row][HB + r * 2] = lo;
         }
       }
-    }
-    const uint32_t end = blockIdx.x * P.slice + P.slice < P.O ? blockIdx.x * P.slice + P.slice : P.O;
-    for (uint32_t o0 = blockIdx.x * P.slice + 64 * wave; o0 < end; o0 += 256) {
-      // Base rows of all the tokens first: they come from memory.
-      const uint32_t at = o0 + pc * E;
-      u4 b[4][NI];
-      if (P.base) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (uint32_t i = 0; i < NI; ++i) {
-            const uint32_t row = 16 * t + tr + (64 / LP) * i;
-            b[t][i] = load_once<T>(piece_at<T>((const T *)P.base + (uint64_t)(row0 + (rows >> row & 1 ? row : lead)) * P.base_row, at, P.O));
-          }
+      if constexpr (RP < FK * KF) {   // ranks of a fragment that no tile holds
+        const uint32_t row = threadIdx.x / 4, part = threadIdx.x / 2 % 2, half = threadIdx.x % 2;
+        *(u4 *)&sh[row][part * HB + 32 + 16 * half] = (u4){0, 0, 0, 0};
       }
+      __syncthreads();
+    }
+    for (; o0 < end; o0 += 256) {
+      const uint32_t at = o0 + pc * E;
       u4 w[4][KF];
       if (rank) {
 #pragma unroll
@@ -248,13 +261,18 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
       for (int t = 0; t < 4; ++t) {
         if ((rows >> (16 * t) & 0xFFFF) == 0) continue;
         if (rank) {
+          f4 acc[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            f4 acc = (f4){0, 0, 0, 0};
+          for (int u = 0; u < 4; ++u) acc[u] = (f4){0, 0, 0, 0};
 #pragma unroll
-            for (int f = 0; f < KF; ++f) acc = mma_wide<T>(w[u][f], h[t].hi[f], h[t].lo[sizeof(T) == 2 ? f : 0], acc);
-            *(f4 *)&so[wave][col][16 * u + 4 * grp] = acc * scale;
+          for (int f = 0; f < KF; ++f) {
+            const u4 hi = *(const u4 *)&sh[16 * t + col][f * 64 + grp * 16];
+            const u4 lo = *(const u4 *)&sh[16 * t + col][(PARTS - 1) * HB + f * 64 + grp * 16];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) acc[u] = mma_wide<T>(w[u][f], hi, lo, acc[u]);
           }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) *(f4 *)&so[wave][col][16 * u + 4 * grp] = acc[u] * scale;
           wave_sync();
         }
 #pragma unroll
@@ -297,6 +315,7 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
           }
         }
       }
+      if (P.base && o0 + 256 < end) load_base(o0 + 256);
     }
   });
 }
@@ -344,6 +363,7 @@ struct InnerParams {
   AdapterIds I;
   const float *part[2], *scaling;   // of h, of g
   float *g;                         // [n_tok][RP]
+  int32_t *ids;                     // [n_pad]: the tokens' adapters, -1 for none
   void *column[2];                  // [2 parts][RP][n_pad] bfloat16, or [RP][n_pad] float32
   uint32_t RP, n_pad, splits;
 };
@@ -351,6 +371,11 @@ template <typename T>
 __global__ void __launch_bounds__(256) inner_kernel(InnerParams P) {
   __shared__ float tile[32][65];
   const uint32_t side = blockIdx.z, row0 = blockIdx.x * 64, r0 = blockIdx.y * 32;
+  if (side == 0 && r0 == 0 && threadIdx.x < 64) {
+    const uint32_t t = row0 + threadIdx.x;
+    const int32_t a = t < P.I.n_tok ? P.I.ids[t] : -1;
+    P.ids[t] = adapter_rank(P.I, a) ? a : -1;
+  }
   for (uint32_t e = threadIdx.x; e < 64 * 32; e += 256) {
     const uint32_t t = row0 + e / 32, r = r0 + e % 32;
     float x = 0;
@@ -358,6 +383,7 @@ __global__ void __launch_bounds__(256) inner_kernel(InnerParams P) {
       const int32_t a = P.I.ids[t];
       if (adapter_rank(P.I, a)) {
         const float *p = P.part[side] + (uint64_t)t * P.RP + r;
+#pragma unroll 4
         for (uint32_t s = 0; s < P.splits; ++s, p += (uint64_t)P.I.n_tok * P.RP) x += *p;
         if (P.scaling) x *= P.scaling[a];
       }
@@ -394,6 +420,7 @@ struct GradSide {
 struct GradParams {
   AdapterIds I;
   GradSide side[2];
+  const int32_t *ids;        // [n_pad], -1 for tokens without an adapter and past the last (inner_kernel)
   uint32_t RP, n_pad, splits, per_split, r_chunks;   // per_split: tokens, a multiple of 64
 };
 template <typename T>
@@ -435,7 +462,12 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
     for (uint32_t j = 0; j < SP; ++j) {
       const uint32_t row = t + j < t1 ? t + j : t1 - 1;
       x[j] = load_once<T>((const T *)S.x + (uint64_t)row * S.x_row + cat);
-      id[j] = P.I.ids[row];
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < SP; j += 4) {
+      const u4 v = *(const u4 *)(P.ids + t + j);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) id[j + e] = (int32_t)v[e];
     }
 #pragma unroll
     for (int j = 0; j < RT; ++j) {
@@ -452,8 +484,15 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
     // Which of 64 steps hold a token of the adapter (a step per lane), and this
     // wavefront's: every eighth of them.
     bool any = false;
-    if (w0 + lane * TB < t1)
-      for (uint32_t i = 0; i < TB; ++i) any |= P.I.ids[w0 + lane * TB + i < t1 ? w0 + lane * TB + i : t1 - 1] == (int32_t)a;
+    const uint32_t s0 = w0 + lane * TB;
+    if (s0 < t1) {
+#pragma unroll
+      for (uint32_t i = 0; i < TB; i += 4) {
+        const u4 v = *(const u4 *)(P.ids + s0 + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) any |= v[e] == a;
+      }
+    }
     uint64_t steps = __ballot(any), mine = 0;
     for (uint32_t i = 0; steps; ++i, steps &= steps - 1)
       if (i % kGradWaves == wave) mine |= steps & -steps;
@@ -466,7 +505,7 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
       bool live[SP];
 #pragma unroll
       for (uint32_t j = 0; j < SP; ++j) {
-        live[j] = (int)(t + j < t1) & (int)(id[j] == (int32_t)a);
+        live[j] = id[j] == (int32_t)a;
         whole &= live[j];
       }
       if (!__all(whole)) {
