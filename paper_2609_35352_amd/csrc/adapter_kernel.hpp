@@ -154,10 +154,10 @@ struct ExpandParams {
 };
 
 // The workgroup first adds up its tokens' parts of h and keeps them in LDS as
-// fragments (two bfloat16 parts for 16-bit types).  A wavefront then takes 64
-// columns of all 64 tokens at a time: the factor's rows are fragments as they
-// lie (contiguous, and shared through the caches), and a tile of 16 tokens
-// passes through LDS to meet the base rows 128 or 256 bytes of a row at a time.
+// fragments (two bfloat16 parts for 16-bit types).  A wavefront then takes 16
+// tokens and 64 columns at a time: the factor's rows are fragments as they lie
+// (contiguous, and shared through the caches), and the tile passes through LDS
+// to meet the base rows 128 or 256 bytes of a row at a time.
 template <typename T, int RT>
 __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
   constexpr uint32_t E = kLaneElems<T>, FK = kFragElems<T>, RP = 16 * RT;
@@ -169,21 +169,9 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
   const uint32_t row0 = blockIdx.y * kRows, tr = lane / LP, pc = lane % LP;
   const uint32_t end = blockIdx.x * P.slice + P.slice < P.O ? blockIdx.x * P.slice + P.slice : P.O;
+  const uint32_t here = P.I.n_tok - row0 < kRows ? P.I.n_tok - row0 : kRows;   // tokens of this workgroup
   for_adapters(P.I, row0, lane, blockIdx.z, P.slots, true, [&](int32_t a, uint32_t rank, uint64_t rows, uint32_t lead) {
     if (rank == 0 && P.base == P.out) return;
-    uint32_t o0 = blockIdx.x * P.slice + 64 * wave;
-    // Base rows come from memory: the first ones are on their way while h is added up.
-    u4 b[4][NI];
-    auto load_base = [&](uint32_t o) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) {
-          const uint32_t row = 16 * t + tr + (64 / LP) * i;
-          b[t][i] = load_once<T>(piece_at<T>((const T *)P.base + (uint64_t)(row0 + (rows >> row & 1 ? row : lead)) * P.base_row, o + pc * E, P.O));
-        }
-    };
-    if (P.base && o0 < end) load_base(o0);
     u4 mask[KF];
     const T *wa = (const T *)P.w;
     uint32_t wn = 0;
@@ -233,34 +221,40 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
       }
       __syncthreads();
     }
-    for (; o0 < end; o0 += 256) {
-      const uint32_t at = o0 + pc * E;
-      u4 w[4][KF];
-      if (rank) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const uint32_t o = o0 + 16 * u + col;
+    const uint32_t start = blockIdx.x * P.slice + 64 * wave;
+    for (uint32_t t = 0; t < 4; ++t) {
+      if ((rows >> (16 * t) & 0xFFFF) == 0 || start >= end) continue;
+      // The next columns' rows and factor are on their way while these are computed.
+      u4 b[NI], w[KF][4];
+      auto load = [&](uint32_t o0) {
+        if (rank)
 #pragma unroll
           for (int f = 0; f < KF; ++f)
-            w[u][f] = load_shared<T>(piece_at<T>(wa, (o < P.O ? o : P.O - 1) * P.w_cols + f * FK + grp * E, wn));
-        }
-        if ((o0 + 64) * P.w_cols + KF * FK > wn) {   // the table's end
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const uint32_t o = o0 + 16 * u + col;
+            for (int u = 0; u < 4; ++u) {
+              const uint32_t o = o0 + 16 * u + col < P.O ? o0 + 16 * u + col : P.O - 1;
+              w[f][u] = load_shared<T>(piece_at<T>(wa, o * P.w_cols + f * FK + grp * E, wn));
+            }
+        if (P.base)
 #pragma unroll
-            for (int f = 0; f < KF; ++f) w[u][f] = piece_fix<T>(w[u][f], (o < P.O ? o : P.O - 1) * P.w_cols + f * FK + grp * E, wn);
+          for (uint32_t i = 0; i < NI; ++i) {
+            const uint32_t r = 16 * t + tr + (64 / LP) * i, row = r < here ? r : here - 1;
+            b[i] = load_shared<T>(piece_at<T>((const T *)P.base + (uint64_t)(row0 + row) * P.base_row, o0 + pc * E, P.O));
           }
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int f = 0; f < KF; ++f) w[u][f] &= mask[f];   // what an adapter's rank leaves out holds anything
-      }
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if ((rows >> (16 * t) & 0xFFFF) == 0) continue;
+      };
+      load(start);
+      for (uint32_t o0 = start; o0 < end; o0 += 256) {
+        const uint32_t at = o0 + pc * E;
         if (rank) {
+          if ((o0 + 64) * P.w_cols + KF * FK > wn) {   // the table's end
+#pragma unroll
+            for (int f = 0; f < KF; ++f)
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                const uint32_t o = o0 + 16 * u + col < P.O ? o0 + 16 * u + col : P.O - 1;
+                w[f][u] = piece_fix<T>(w[f][u], o * P.w_cols + f * FK + grp * E, wn);
+              }
+          }
           f4 acc[4];
 #pragma unroll
           for (int u = 0; u < 4; ++u) acc[u] = (f4){0, 0, 0, 0};
@@ -269,12 +263,17 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
             const u4 hi = *(const u4 *)&sh[16 * t + col][f * 64 + grp * 16];
             const u4 lo = *(const u4 *)&sh[16 * t + col][(PARTS - 1) * HB + f * 64 + grp * 16];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) acc[u] = mma_wide<T>(w[u][f], hi, lo, acc[u]);
+            for (int u = 0; u < 4; ++u) acc[u] = mma_wide<T>(w[f][u] & mask[f], hi, lo, acc[u]);   // what the rank leaves out holds anything
           }
+          wave_sync();   // (the last tile is read)
 #pragma unroll
           for (int u = 0; u < 4; ++u) *(f4 *)&so[wave][col][16 * u + 4 * grp] = acc[u] * scale;
           wave_sync();
         }
+        u4 v[NI];
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) v[i] = b[i];
+        if (o0 + 256 < end) load(o0 + 256);
 #pragma unroll
         for (uint32_t i = 0; i < NI; ++i) {
           const uint32_t row = 16 * t + tr + (64 / LP) * i;
@@ -283,13 +282,12 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
           for (uint32_t e = 0; e < E / 4; ++e)
             y[e] = rank ? *(const f4 *)&so[wave][tr + (64 / LP) * i][pc * E + 4 * e] : (f4){0, 0, 0, 0};
           if (P.base) {
-            u4 v = b[t][i];
-            if (o0 + 64 > P.O) v = piece_fix<T>(v, at, P.O);
+            if (o0 + 64 > P.O) v[i] = piece_fix<T>(v[i], at, P.O);
             if constexpr (sizeof(T) == 4) {
-              y[0] += __builtin_bit_cast(f4, v);
+              y[0] += __builtin_bit_cast(f4, v[i]);
             } else {
               typedef T t8 __attribute__((ext_vector_type(8)));
-              const t8 z = __builtin_bit_cast(t8, v);
+              const t8 z = __builtin_bit_cast(t8, v[i]);
 #pragma unroll
               for (int e = 0; e < 8; ++e) y[e / 4][e % 4] += (float)z[e];
             }
@@ -315,7 +313,6 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
           }
         }
       }
-      if (P.base && o0 + 256 < end) load_base(o0 + 256);
     }
   });
 }
@@ -359,12 +356,22 @@ __global__ void __launch_bounds__(256) transpose_kernel(TransposeParams P) {
 // inner: parts of h and g summed and scaled; g as rows for dx, both as columns
 // of tokens for the gradients, in two bfloat16 parts for 16-bit types
 // ---------------------------------------------------------------------------
+// Tokens of one step of the gradients: a fragment's.
+template <typename T>
+constexpr uint32_t kGradTokens = sizeof(T) == 2 ? 32 : 16;
+// The lane's 16 bytes of the fragment of a step's tokens and 16 ranks: ranks by
+// lane % 16, tokens by lane / 16; bfloat16 has a second fragment for the rest.
+template <typename T>
+__device__ __forceinline__ char *column_at(const void *column, uint32_t RP, uint64_t step, uint32_t tile, uint32_t part, uint32_t lane) {
+  return (char *)column + (((step * (RP / 16) + tile) * (sizeof(T) == 2 ? 2 : 1) + part) * 64 + lane) * 16;
+}
+
 struct InnerParams {
   AdapterIds I;
   const float *part[2], *scaling;   // of h, of g
   float *g;                         // [n_tok][RP]
   int32_t *ids;                     // [n_pad]: the tokens' adapters, -1 for none
-  void *column[2];                  // [2 parts][RP][n_pad] bfloat16, or [RP][n_pad] float32
+  void *column[2];                  // h and g as fragments of the gradients' steps (see column_at)
   uint32_t RP, n_pad, splits;
 };
 template <typename T>
@@ -392,18 +399,27 @@ __global__ void __launch_bounds__(256) inner_kernel(InnerParams P) {
     tile[e % 32][e / 32] = x;
   }
   __syncthreads();
-  for (uint32_t e = threadIdx.x; e < 32 * 64; e += 256) {
-    const uint32_t r = r0 + e / 64, t = row0 + e % 64;
-    if (r >= P.RP) continue;
-    const float x = tile[e / 64][e % 64];
-    const uint64_t at = (uint64_t)r * P.n_pad + t;
-    if constexpr (sizeof(T) == 4) {
-      ((float *)P.column[side])[at] = x;
-    } else {
-      const __bf16 hi = (__bf16)x;
-      ((__bf16 *)P.column[side])[at] = hi;
-      ((__bf16 *)P.column[side])[(uint64_t)P.RP * P.n_pad + at] = (__bf16)(x - (float)hi);
+  if constexpr (sizeof(T) == 4) {   // 4 steps of 16 tokens, 2 tiles of 16 ranks, 64 lanes of 4 tokens
+    for (uint32_t e = threadIdx.x; e < 512; e += 256) {
+      const uint32_t lane = e % 64, j = e / 64 % 2, step = e / 128, t = 16 * step + lane / 16 * 4;
+      if (r0 + 16 * j >= P.RP) continue;
+      f4 x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = tile[16 * j + lane % 16][t + i];
+      *(f4 *)column_at<T>(P.column[side], P.RP, row0 / 16 + step, r0 / 16 + j, 0, lane) = x;
     }
+  } else {                          // 2 steps of 32 tokens, 2 tiles of 16 ranks, 64 lanes of 8 tokens
+    const uint32_t lane = threadIdx.x % 64, j = threadIdx.x / 64 % 2, step = threadIdx.x / 128, t = 32 * step + lane / 16 * 8;
+    if (r0 + 16 * j >= P.RP) return;
+    u4 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t l;
+      hi[i] = split_pair(tile[16 * j + lane % 16][t + 2 * i], tile[16 * j + lane % 16][t + 2 * i + 1], l);
+      lo[i] = l;
+    }
+    *(u4 *)column_at<T>(P.column[side], P.RP, row0 / 32 + step, r0 / 16 + j, 0, lane) = hi;
+    *(u4 *)column_at<T>(P.column[side], P.RP, row0 / 32 + step, r0 / 16 + j, 1, lane) = lo;
   }
 }
 
@@ -423,25 +439,27 @@ struct GradParams {
   const int32_t *ids;        // [n_pad], -1 for tokens without an adapter and past the last (inner_kernel)
   uint32_t RP, n_pad, splits, per_split, r_chunks;   // per_split: tokens, a multiple of 64
 };
+// Columns of a lane and of a workgroup: 16 bytes of 16 lanes, or 8 where 64
+// ranks of 16 bytes' columns would not fit the registers.
 template <typename T>
-constexpr uint32_t kGradTokens = sizeof(T) == 2 ? 32 : 16;    // tokens of a step
-template <typename T>
-constexpr uint32_t kGradCols = 16 * kLaneElems<T>;            // columns of a workgroup
+constexpr uint32_t grad_width(uint32_t RP) {
+  return sizeof(T) == 2 && RP >= 64 ? 4 : kLaneElems<T>;
+}
 constexpr uint32_t kGradWaves = 8;
 
-// A workgroup takes 256 bytes of the rows' columns for one adapter and up to 64
+// A workgroup takes 128 or 256 bytes of the rows' columns for one adapter and up to 64
 // of its ranks; its eight wavefronts take the steps that hold a token of the
 // adapter in turn.  Rows are read whole pieces at a time, 16 lanes to a piece,
 // eight tokens to a lane; the transposed fragments (columns x tokens) are
 // picked from the tokens' words in registers, as values are in the attention.
 template <typename T, int RT>
 __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
-  constexpr uint32_t E = kLaneElems<T>, TB = kGradTokens<T>, SP = TB / 4;
-  __shared__ float so[kGradWaves][16][kGradCols<T>];   // column c of rank r at c ^ 4 r, off each other's banks
+  constexpr uint32_t E = grad_width<T>(16 * RT), C = 16 * E, TB = kGradTokens<T>, SP = TB / 4, W = E * sizeof(T) / 4;
+  __shared__ float so[kGradWaves][16][C];   // column c of rank r at c ^ 4 r, off each other's banks
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
   const bool second = blockIdx.x >= P.side[0].slices;
   const GradSide &S = P.side[second];
-  const uint32_t slice = blockIdx.x - (second ? P.side[0].slices : 0), c0 = slice * kGradCols<T>;
+  const uint32_t slice = blockIdx.x - (second ? P.side[0].slices : 0), c0 = slice * C;
   const uint32_t a = blockIdx.y / P.r_chunks, n0 = blockIdx.y % P.r_chunks * 64, split = blockIdx.z;
   const uint32_t rank = adapter_rank(P.I, (int32_t)a);
   const uint32_t t0 = split * P.per_split, t1 = t0 + P.per_split < P.I.n_tok ? t0 + P.per_split : P.I.n_tok;
@@ -454,14 +472,23 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
   // The lane's columns; at the row's end they step back to its last 16 bytes
   // (and are dropped on the way out where another lane has them).
   const uint32_t at = c0 + col * E, cat = at + E <= S.n ? at : S.n - E;
-  u4 x[SP], hi[RT], lo[sizeof(T) == 2 ? RT : 1];
+  uint32_t x[SP][W];
+  u4 hi[RT], lo[sizeof(T) == 2 ? RT : 1];
   int32_t id[SP];
   auto load = [&](uint32_t step) {   // (its first token)
     const uint32_t t = step + grp * SP;
 #pragma unroll
     for (uint32_t j = 0; j < SP; ++j) {
       const uint32_t row = t + j < t1 ? t + j : t1 - 1;
-      x[j] = load_once<T>((const T *)S.x + (uint64_t)row * S.x_row + cat);
+      const T *p = (const T *)S.x + (uint64_t)row * S.x_row + cat;
+      if constexpr (W == 4) {
+        const u4 v = load_once<T>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[j][i] = v[i];
+      } else {
+        const u2 v = __builtin_nontemporal_load((const u2_any *)p);
+        x[j][0] = v[0], x[j][1] = v[1];
+      }
     }
 #pragma unroll
     for (uint32_t j = 0; j < SP; j += 4) {
@@ -471,13 +498,8 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
     }
 #pragma unroll
     for (int j = 0; j < RT; ++j) {
-      const uint64_t r = (uint64_t)(n0 + 16 * j + col) * P.n_pad + t;
-      if constexpr (sizeof(T) == 4) {
-        hi[j] = *(const u4 *)((const float *)S.column + r);
-      } else {
-        hi[j] = *(const u4 *)((const __bf16 *)S.column + r);
-        lo[j] = *(const u4 *)((const __bf16 *)S.column + (uint64_t)P.RP * P.n_pad + r);
-      }
+      hi[j] = *(const u4 *)column_at<T>(S.column, P.RP, step / TB, n0 / 16 + j, 0, lane);
+      if constexpr (sizeof(T) == 2) lo[j] = *(const u4 *)column_at<T>(S.column, P.RP, step / TB, n0 / 16 + j, 1, lane);
     }
   };
   for (uint32_t w0 = t0; rank > n0 && w0 < t1; w0 += 64 * TB) {
@@ -512,7 +534,7 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
 #pragma unroll
         for (uint32_t j = 0; j < SP; ++j) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[j][i] = live[j] ? x[j][i] : 0;
+          for (uint32_t i = 0; i < W; ++i) x[j][i] = live[j] ? x[j][i] : 0;
           const uint32_t keep = live[j] ? 0 : sizeof(T) == 4 ? ~0u : 0xFFFFu << (16 * (j % 2));
 #pragma unroll
           for (int i = 0; i < RT; ++i) {
@@ -521,9 +543,12 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
           }
         }
       }
-      u4 y[SP], vh[RT], vl[RT];
+      uint32_t y[SP][W];
+      u4 vh[RT], vl[RT];
 #pragma unroll
-      for (uint32_t j = 0; j < SP; ++j) y[j] = x[j];
+      for (uint32_t j = 0; j < SP; ++j)
+#pragma unroll
+        for (uint32_t i = 0; i < W; ++i) y[j][i] = x[j][i];
 #pragma unroll
       for (int j = 0; j < RT; ++j) {
         vh[j] = hi[j];
@@ -558,9 +583,9 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) so[wave][col][((4 * grp + i) * E + u) ^ (4 * col)] = acc[u][j][i];
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < 16 * kGradCols<T>; e += 512) {
+    for (uint32_t e = threadIdx.x; e < 16 * C; e += 512) {
       // dA: consecutive threads along the columns; dB: along the ranks
-      const uint32_t r = second ? e % 16 : e / kGradCols<T>, c = second ? e / 16 : e % kGradCols<T>;
+      const uint32_t r = second ? e % 16 : e / C, c = second ? e / 16 : e % C;
       float s = 0;
 #pragma unroll
       for (uint32_t w = 0; w < kGradWaves; ++w) s += so[w][r][c ^ (4 * r)];

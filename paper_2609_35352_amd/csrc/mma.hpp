@@ -73,6 +73,7 @@ __device__ __forceinline__ void load_row(const T *p, int valid, uint32_t (&w)[W 
 // moves what was loaded to its place, zero from n on.  Rows start at any
 // element: the memory system takes 16-byte accesses at any address.
 typedef u4 u4_any __attribute__((aligned(2)));
+typedef u2 u2_any __attribute__((aligned(2)));
 template <typename T>
 __device__ __forceinline__ const T *piece_at(const T *row, uint32_t at, uint32_t n) {
   return row + (at + kLaneElems<T> <= n ? at : n - kLaneElems<T>);
