@@ -567,7 +567,8 @@ int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cach
  * Both: asynchronous on stream, kernel launches only, allocate nothing.  The
  * workspace is shared by the handle's calls: one handle must not be used by
  * two streams at the same time.  Errors (nothing is launched): FIONA_ERR_ARG,
- * FIONA_ERR_ALIGN, FIONA_ERR_ALIAS, FIONA_ERR_HIP.
+ * FIONA_ERR_UNSUPPORTED (rows more than 2^24 elements apart), FIONA_ERR_ALIGN,
+ * FIONA_ERR_ALIAS, FIONA_ERR_HIP.
  */
 #define FIONA_ADAPTERS_FORWARD_ONLY 1u   /* no workspace for fiona_adapter_backward (FIONA_ERR_ARG on such a handle) */
 

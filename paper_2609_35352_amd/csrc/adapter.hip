@@ -118,6 +118,7 @@ int check_common(const fiona_adapters *H, const fiona_adapter_args *args, fiona:
   if (A.n_tok > D.max_tokens) return FIONA_ERR_ARG;
   const uint64_t e = type_size(D.type);
   if (A.n_tok && (!A.x || !A.ids)) return FIONA_ERR_ARG;
+  if (A.n_tok > 1 && A.x_row > fiona::kMaxStride) return FIONA_ERR_UNSUPPORTED;
   if (D.n_adapter && D.max_rank && (!A.A || !A.B)) return FIONA_ERR_ARG;
   if (misaligned(A.x, e) || misaligned(A.A, e) || misaligned(A.B, e) || misaligned(A.ids, 4) ||
       misaligned(A.ranks, 4) || misaligned(A.scaling, 4))
@@ -138,17 +139,19 @@ bool narrow(const fiona_adapters_desc &D) { return D.d_in < kMinWidth || D.d_out
 uint32_t blocks_of(uint64_t n) { return (uint32_t)((n + fiona::kRows - 1) / fiona::kRows); }
 
 // Workgroups that share the adapters among 64 tokens: many where there are few
-// tokens, as each may have its own.
+// tokens, as each may have its own; two in any case, for the blocks in which
+// one request ends and the next begins (8192 tokens of 12 requests, shrink and
+// expand: 16 and 26 us with two, 19 and 33 with one).
 uint32_t slots_of(uint32_t n, uint32_t adapters) {
-  const uint32_t want = std::max(1u, 256 / blocks_of(n));
+  const uint32_t want = std::max(2u, 256 / blocks_of(n));
   return std::min({want, adapters, std::min(n, fiona::kRows)});
 }
 
-constexpr uint32_t kMaxSplits = 8, kWorkgroups = 1024, kGradWorkgroups = 512;
+constexpr uint32_t kMaxSplits = 8, kWorkgroups = 512, kGradWorkgroups = 512;
 
 // Parts of a row's contraction: enough workgroups to fill the GPU.
-uint32_t splits_of(uint32_t n, uint32_t adapters, uint32_t sides) {
-  const uint32_t wgs = blocks_of(n) * slots_of(n, adapters) * sides;
+uint32_t splits_of(uint32_t n, uint32_t adapters) {
+  const uint32_t slots = slots_of(n, adapters), wgs = blocks_of(n) * (slots > 2 ? slots : 1);
   return std::max(1u, std::min(kMaxSplits, (kWorkgroups + wgs - 1) / wgs));
 }
 
@@ -249,7 +252,7 @@ int fiona_adapters_create(const fiona_adapters_desc *desc, fiona_adapters **out)
   const bool both = !(D.flags & FIONA_ADAPTERS_FORWARD_ONLY);
   const uint64_t e = type_size(D.type), n_pad = (uint64_t)blocks_of(D.max_tokens) * 64, RP = H->RP;
   for (uint32_t n = std::min(64u, D.max_tokens);; n = std::min(n + 64, D.max_tokens)) {
-    H->part_cap = std::max<uint64_t>(H->part_cap, (uint64_t)n * splits_of(n, D.n_adapter, 1));
+    H->part_cap = std::max<uint64_t>(H->part_cap, (uint64_t)n * splits_of(n, D.n_adapter));
     if (n == D.max_tokens) break;
   }
   H->part_cap = std::max<uint64_t>(H->part_cap, 64 * kMaxSplits);   // (fewer than 64 tokens)
@@ -290,6 +293,7 @@ int fiona_adapter_linear(const fiona_adapters *H, const fiona_adapter_args *args
   if (!A.y) return FIONA_ERR_ARG;
   const uint64_t e = type_size(D.type), n = A.n_tok;
   if (misaligned(A.base, e) || misaligned(A.y, e)) return FIONA_ERR_ALIGN;
+  if (n > 1 && (A.base_row > fiona::kMaxStride || A.y_row > fiona::kMaxStride)) return FIONA_ERR_UNSUPPORTED;
   const Rows in[] = {matrix(A.x, e, n, D.d_in, A.x_row), matrix(A.A, e, 1, (uint64_t)D.n_adapter * D.max_rank * D.d_in, 0),
                      matrix(A.B, e, 1, (uint64_t)D.n_adapter * D.max_rank * D.d_out, 0), matrix(A.ids, 4, 1, n, 0),
                      matrix(A.ranks, 4, 1, D.n_adapter, 0), matrix(A.scaling, 4, 1, D.n_adapter, 0),
@@ -302,7 +306,7 @@ int fiona_adapter_linear(const fiona_adapters *H, const fiona_adapter_args *args
   with_type(D.type, [&](auto t) {
     using T = decltype(t);
     if (!narrow(D)) {
-      const uint32_t splits = splits_of(A.n_tok, D.n_adapter, 1);
+      const uint32_t splits = splits_of(A.n_tok, D.n_adapter);
       const fiona::AdapterIds I{A.ids, A.ranks, A.n_tok, D.n_adapter, D.max_rank};
       const fiona::ShrinkSide side{A.x, A.A, H->part[0], A.x_row, D.d_in, D.max_rank};
       launch_shrink<T>(H, I, &side, 1, splits, stream);
@@ -327,6 +331,8 @@ int fiona_adapter_backward(const fiona_adapters *H, const fiona_adapter_args *ar
   const uint64_t e = type_size(D.type), n = A.n_tok;
   if (misaligned(A.dy, e) || misaligned(A.dx_base, e) || misaligned(A.dx, e) || misaligned(A.dA, e) || misaligned(A.dB, e))
     return FIONA_ERR_ALIGN;
+  if (n > 1 && (A.dy_row > fiona::kMaxStride || A.dx_base_row > fiona::kMaxStride || A.dx_row > fiona::kMaxStride))
+    return FIONA_ERR_UNSUPPORTED;
   const uint64_t wa = (uint64_t)D.n_adapter * D.max_rank * D.d_in, wb = (uint64_t)D.n_adapter * D.max_rank * D.d_out;
   const Rows in[] = {matrix(A.x, e, n, D.d_in, A.x_row), matrix(A.A, e, 1, wa, 0), matrix(A.B, e, 1, wb, 0),
                      matrix(A.ids, 4, 1, n, 0), matrix(A.ranks, 4, 1, D.n_adapter, 0),
@@ -341,7 +347,7 @@ int fiona_adapter_backward(const fiona_adapters *H, const fiona_adapter_args *ar
   with_type(D.type, [&](auto t) {
     using T = decltype(t);
     if (!narrow(D)) {
-      const uint32_t splits = splits_of(std::max(1u, A.n_tok), D.n_adapter, 2), blocks = blocks_of(A.n_tok);
+      const uint32_t splits = splits_of(std::max(1u, A.n_tok), D.n_adapter), blocks = blocks_of(A.n_tok);
       const fiona::AdapterIds I{A.ids, A.ranks, A.n_tok, D.n_adapter, D.max_rank};
       if (A.n_tok) {
         hipLaunchKernelGGL(fiona::transpose_kernel<T>, dim3((D.d_in + 63) / 64 + (D.d_out + 63) / 64, D.n_adapter), dim3(256), 0,

@@ -21,6 +21,7 @@
 
 namespace fiona {
 
+constexpr uint64_t kMaxStride = 1 << 24;   // elements from one token's row to the next
 constexpr uint32_t kRows = 64;        // tokens of a workgroup in shrink and expand
 
 struct AdapterIds {
@@ -78,7 +79,7 @@ __global__ void __launch_bounds__(256) shrink_kernel(ShrinkParams P) {
   constexpr uint32_t E = kLaneElems<T>, CE = 16 * E, RP = 16 * RT;
   __shared__ alignas(16) uint8_t sx[kRows][272], sw[RP][272];
   const ShrinkSide &S = P.side[blockIdx.z / P.slots];
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+  const uint32_t lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, grp = lane >> 4;
   const uint32_t row0 = blockIdx.x * kRows, tr = threadIdx.x / 16, pc = threadIdx.x % 16;
   const uint32_t chunks = (S.K + CE - 1) / CE, split = blockIdx.y;
   const uint32_t c0 = chunks * split / P.splits, c1 = chunks * (split + 1) / P.splits;
@@ -166,7 +167,7 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
   constexpr uint32_t HB = KF * 64;                      // bytes of a token's h, and of its second part
   __shared__ alignas(16) float so[4][16][68];
   __shared__ alignas(16) uint8_t sh[kRows][PARTS * HB + 16];
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+  const uint32_t lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, grp = lane >> 4;
   const uint32_t row0 = blockIdx.y * kRows, tr = lane / LP, pc = lane % LP;
   const uint32_t end = blockIdx.x * P.slice + P.slice < P.O ? blockIdx.x * P.slice + P.slice : P.O;
   const uint32_t here = P.I.n_tok - row0 < kRows ? P.I.n_tok - row0 : kRows;   // tokens of this workgroup
@@ -221,32 +222,96 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
       }
       __syncthreads();
     }
-    const uint32_t start = blockIdx.x * P.slice + 64 * wave;
+    uint32_t start = blockIdx.x * P.slice + 64 * wave;
+    if (start >= end) return;
+    // A tile's base rows are asked for four tiles ahead, the next columns'
+    // factor as soon as the last tile's products are done.
+    u4 b[4][NI], w[KF][4];
+    auto load_w = [&](uint32_t o0) {
+#pragma unroll
+      for (int f = 0; f < KF; ++f)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t o = o0 + 16 * u + col < P.O ? o0 + 16 * u + col : P.O - 1;
+          w[f][u] = load_shared<T>(piece_at<T>(wa, o * P.w_cols + f * FK + grp * E, wn));
+        }
+    };
+    auto load_base = [&](u4 (&b)[NI], uint32_t o0, uint32_t t) {
+#pragma unroll
+      for (uint32_t i = 0; i < NI; ++i) {
+        const uint32_t r = 16 * t + tr + (64 / LP) * i, row = r < here ? r : here - 1;
+        b[i] = load_shared<T>(piece_at<T>((const T *)P.base + (uint64_t)(row0 + row) * P.base_row, o0 + pc * E, P.O));
+      }
+    };
+    // Values of a lane's row piece: products from LDS and base, as they are stored.
+    auto finish = [&](uint32_t i, u4 v) {
+      f4 y[E / 4];
+#pragma unroll
+      for (uint32_t e = 0; e < E / 4; ++e)
+        y[e] = rank ? *(const f4 *)&so[wave][tr + (64 / LP) * i][pc * E + 4 * e] : (f4){0, 0, 0, 0};
+      u4 out;
+      if constexpr (sizeof(T) == 4) {
+        out = __builtin_bit_cast(u4, y[0] + __builtin_bit_cast(f4, v));
+      } else {
+        typedef T t8 __attribute__((ext_vector_type(8)));
+        const t8 z = __builtin_bit_cast(t8, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e / 4][e % 4] += (float)z[e];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = pack2<T>(y[e / 2][2 * (e % 2)], y[e / 2][2 * (e % 2) + 1]);
+      }
+      return out;
+    };
+    // The products of a tile of tokens and 64 columns, into LDS.
+    auto multiply = [&](uint32_t t) {
+      f4 acc[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) acc[u] = (f4){0, 0, 0, 0};
+#pragma unroll
+      for (int f = 0; f < KF; ++f) {
+        const u4 hi = *(const u4 *)&sh[16 * t + col][f * 64 + grp * 16];
+        const u4 lo = *(const u4 *)&sh[16 * t + col][(PARTS - 1) * HB + f * 64 + grp * 16];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) acc[u] = mma_wide<T>(w[f][u] & mask[f], hi, lo, acc[u]);   // what the rank leaves out holds anything
+      }
+      wave_sync();   // (the last tile is read)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) *(f4 *)&so[wave][col][16 * u + 4 * grp] = acc[u] * scale;
+      wave_sync();
+    };
+    // All 64 tokens have the adapter: no branches, so that a wait is for what
+    // is used next only (loads and stores complete in order).
+    if (rank && P.base && rows == ~(uint64_t)0 && start + 64 <= end && ((uint64_t)P.O * P.w_cols + KF * FK <= wn)) {
+      load_w(start);
+#pragma unroll
+      for (uint32_t t = 0; t < 4; ++t) load_base(b[t], start, t);
+      for (; start + 64 <= end; start += 256) {
+        const uint32_t next = start + 256 + 64 <= end ? start + 256 : start;   // (the last columns' again)
+#pragma unroll
+        for (uint32_t t = 0; t < 4; ++t) {
+          multiply(t);
+          if (t == 3) load_w(next);
+          u4 out[NI];
+#pragma unroll
+          for (uint32_t i = 0; i < NI; ++i) out[i] = finish(i, b[t][i]);
+          load_base(b[t], next, t);
+#pragma unroll
+          for (uint32_t i = 0; i < NI; ++i)
+            __builtin_nontemporal_store(out[i], (u4_any *)((T *)P.out + (uint64_t)(row0 + 16 * t + tr + (64 / LP) * i) * P.out_row +
+                                                           start + pc * E));
+        }
+      }
+      if (start >= end) return;
+    }
+    // Tiles that hold other adapters' tokens, the last columns and the table's end.
     for (uint32_t t = 0; t < 4; ++t) {
-      if ((rows >> (16 * t) & 0xFFFF) == 0 || start >= end) continue;
-      // The next columns' rows and factor are on their way while these are computed.
-      u4 b[NI], w[KF][4];
-      auto load = [&](uint32_t o0) {
-        if (rank)
-#pragma unroll
-          for (int f = 0; f < KF; ++f)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const uint32_t o = o0 + 16 * u + col < P.O ? o0 + 16 * u + col : P.O - 1;
-              w[f][u] = load_shared<T>(piece_at<T>(wa, o * P.w_cols + f * FK + grp * E, wn));
-            }
-        if (P.base)
-#pragma unroll
-          for (uint32_t i = 0; i < NI; ++i) {
-            const uint32_t r = 16 * t + tr + (64 / LP) * i, row = r < here ? r : here - 1;
-            b[i] = load_shared<T>(piece_at<T>((const T *)P.base + (uint64_t)(row0 + row) * P.base_row, o0 + pc * E, P.O));
-          }
-      };
-      load(start);
+      if ((rows >> (16 * t) & 0xFFFF) == 0) continue;
+      if (rank) load_w(start);
+      if (P.base) load_base(b[0], start, t);
       for (uint32_t o0 = start; o0 < end; o0 += 256) {
         const uint32_t at = o0 + pc * E;
         if (rank) {
-          if ((o0 + 64) * P.w_cols + KF * FK > wn) {   // the table's end
+          if ((o0 + 64) * P.w_cols + KF * FK > wn) {
 #pragma unroll
             for (int f = 0; f < KF; ++f)
 #pragma unroll
@@ -255,50 +320,17 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
                 w[f][u] = piece_fix<T>(w[f][u], o * P.w_cols + f * FK + grp * E, wn);
               }
           }
-          f4 acc[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) acc[u] = (f4){0, 0, 0, 0};
-#pragma unroll
-          for (int f = 0; f < KF; ++f) {
-            const u4 hi = *(const u4 *)&sh[16 * t + col][f * 64 + grp * 16];
-            const u4 lo = *(const u4 *)&sh[16 * t + col][(PARTS - 1) * HB + f * 64 + grp * 16];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) acc[u] = mma_wide<T>(w[f][u] & mask[f], hi, lo, acc[u]);   // what the rank leaves out holds anything
-          }
-          wave_sync();   // (the last tile is read)
-#pragma unroll
-          for (int u = 0; u < 4; ++u) *(f4 *)&so[wave][col][16 * u + 4 * grp] = acc[u] * scale;
-          wave_sync();
+          multiply(t);
+          if (o0 + 256 < end) load_w(o0 + 256);
         }
         u4 v[NI];
 #pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) v[i] = b[i];
-        if (o0 + 256 < end) load(o0 + 256);
+        for (uint32_t i = 0; i < NI; ++i) v[i] = P.base ? piece_fix<T>(b[0][i], at, P.O) : (u4){0, 0, 0, 0};
+        if (P.base && o0 + 256 < end) load_base(b[0], o0 + 256, t);
 #pragma unroll
         for (uint32_t i = 0; i < NI; ++i) {
           const uint32_t row = 16 * t + tr + (64 / LP) * i;
-          f4 y[E / 4];
-#pragma unroll
-          for (uint32_t e = 0; e < E / 4; ++e)
-            y[e] = rank ? *(const f4 *)&so[wave][tr + (64 / LP) * i][pc * E + 4 * e] : (f4){0, 0, 0, 0};
-          if (P.base) {
-            if (o0 + 64 > P.O) v[i] = piece_fix<T>(v[i], at, P.O);
-            if constexpr (sizeof(T) == 4) {
-              y[0] += __builtin_bit_cast(f4, v[i]);
-            } else {
-              typedef T t8 __attribute__((ext_vector_type(8)));
-              const t8 z = __builtin_bit_cast(t8, v[i]);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) y[e / 4][e % 4] += (float)z[e];
-            }
-          }
-          u4 out;
-          if constexpr (sizeof(T) == 4) {
-            out = __builtin_bit_cast(u4, y[0]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) out[e] = pack2<T>(y[e / 2][2 * (e % 2)], y[e / 2][2 * (e % 2) + 1]);
-          }
+          const u4 out = finish(i, v[i]);
           if (!(rows >> row & 1)) continue;
           T *p = (T *)P.out + (uint64_t)(row0 + row) * P.out_row + at;
           if (at + E <= P.O) {
@@ -439,13 +471,25 @@ struct GradParams {
   const int32_t *ids;        // [n_pad], -1 for tokens without an adapter and past the last (inner_kernel)
   uint32_t RP, n_pad, splits, per_split, r_chunks;   // per_split: tokens, a multiple of 64
 };
-// Columns of a lane and of a workgroup: 16 bytes of 16 lanes, or 8 where 64
+// Columns of a lane and of a workgroup: 16 bytes of 16 lanes, or 8 where 32
 // ranks of 16 bytes' columns would not fit the registers.
 template <typename T>
 constexpr uint32_t grad_width(uint32_t RP) {
-  return sizeof(T) == 2 && RP >= 64 ? 4 : kLaneElems<T>;
+  return sizeof(T) == 2 && RP >= 32 ? 4 : kLaneElems<T>;
 }
 constexpr uint32_t kGradWaves = 8;
+
+// Element u of each of a lane's tokens: the lane's part of a transposed fragment.
+template <typename T, int SP, int W>
+__device__ __forceinline__ u4 column_of(const uint32_t (&x)[SP][W], uint32_t u) {
+  if constexpr (sizeof(T) == 4) {
+    return (u4){x[0][u], x[1][u], x[2][u], x[3][u]};
+  } else {
+    const uint32_t i = u / 2;
+    if (u & 1) return (u4){pair_high(x[0][i], x[1][i]), pair_high(x[2][i], x[3][i]), pair_high(x[4][i], x[5][i]), pair_high(x[6][i], x[7][i])};
+    return (u4){pair_low(x[0][i], x[1][i]), pair_low(x[2][i], x[3][i]), pair_low(x[4][i], x[5][i]), pair_low(x[6][i], x[7][i])};
+  }
+}
 
 // A workgroup takes 128 or 256 bytes of the rows' columns for one adapter and up to 64
 // of its ranks; its eight wavefronts take the steps that hold a token of the
@@ -455,8 +499,8 @@ constexpr uint32_t kGradWaves = 8;
 template <typename T, int RT>
 __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
   constexpr uint32_t E = grad_width<T>(16 * RT), C = 16 * E, TB = kGradTokens<T>, SP = TB / 4, W = E * sizeof(T) / 4;
-  __shared__ float so[kGradWaves][16][C];   // column c of rank r at c ^ 4 r, off each other's banks
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+  __shared__ alignas(16) float so[kGradWaves][16][C];   // column c of rank r at c ^ 4 r, off each other's banks
+  const uint32_t lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, grp = lane >> 4;
   const bool second = blockIdx.x >= P.side[0].slices;
   const GradSide &S = P.side[second];
   const uint32_t slice = blockIdx.x - (second ? P.side[0].slices : 0), c0 = slice * C;
@@ -472,105 +516,133 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
   // The lane's columns; at the row's end they step back to its last 16 bytes
   // (and are dropped on the way out where another lane has them).
   const uint32_t at = c0 + col * E, cat = at + E <= S.n ? at : S.n - E;
-  uint32_t x[SP][W];
-  u4 hi[RT], lo[sizeof(T) == 2 ? RT : 1];
-  int32_t id[SP];
-  auto load = [&](uint32_t step) {   // (its first token)
-    const uint32_t t = step + grp * SP;
+  // Rows are asked for two steps ahead, fragments of h or g one: in between
+  // lie the products of a step, and loads return in order.
+  struct Rows {
+    uint32_t x[SP][W];
+  } x0, x1, x2;
+  struct Columns {
+    u4 hi[RT], lo[sizeof(T) == 2 ? RT : 1];
+  } v0, v1;
+  // A row's address is a scalar (token step + j) plus the lane's offset of its
+  // own tokens and columns, below 2^32 bytes (row strides are at most kMaxStride).
+  const uint32_t row_bytes = (uint32_t)(S.x_row * sizeof(T)), lane_at = grp * SP * row_bytes + cat * (uint32_t)sizeof(T);
+  auto load_rows = [&](Rows &r, uint32_t step) {   // (its first token)
 #pragma unroll
     for (uint32_t j = 0; j < SP; ++j) {
-      const uint32_t row = t + j < t1 ? t + j : t1 - 1;
-      const T *p = (const T *)S.x + (uint64_t)row * S.x_row + cat;
+      const uint32_t row = step + j < P.I.n_tok ? step + j : P.I.n_tok - 1;
+      const char *p = (const char *)S.x + (uint64_t)row * row_bytes +
+                      (row + grp * SP < P.I.n_tok ? lane_at : cat * (uint32_t)sizeof(T));
       if constexpr (W == 4) {
-        const u4 v = load_once<T>(p);
+        const u4 v = load_once<T>((const T *)p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[j][i] = v[i];
+        for (int i = 0; i < 4; ++i) r.x[j][i] = v[i];
       } else {
         const u2 v = __builtin_nontemporal_load((const u2_any *)p);
-        x[j][0] = v[0], x[j][1] = v[1];
+        r.x[j][0] = v[0], r.x[j][1] = v[1];
       }
-    }
-#pragma unroll
-    for (uint32_t j = 0; j < SP; j += 4) {
-      const u4 v = *(const u4 *)(P.ids + t + j);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) id[j + e] = (int32_t)v[e];
-    }
-#pragma unroll
-    for (int j = 0; j < RT; ++j) {
-      hi[j] = *(const u4 *)column_at<T>(S.column, P.RP, step / TB, n0 / 16 + j, 0, lane);
-      if constexpr (sizeof(T) == 2) lo[j] = *(const u4 *)column_at<T>(S.column, P.RP, step / TB, n0 / 16 + j, 1, lane);
     }
   };
-  for (uint32_t w0 = t0; rank > n0 && w0 < t1; w0 += 64 * TB) {
-    // Which of 64 steps hold a token of the adapter (a step per lane), and this
-    // wavefront's: every eighth of them.
-    bool any = false;
-    const uint32_t s0 = w0 + lane * TB;
-    if (s0 < t1) {
+  auto load_columns = [&](Columns &c, uint32_t step) {
 #pragma unroll
-      for (uint32_t i = 0; i < TB; i += 4) {
-        const u4 v = *(const u4 *)(P.ids + s0 + i);
+    for (int j = 0; j < RT; ++j) {
+      c.hi[j] = *(const u4 *)column_at<T>(S.column, P.RP, step / TB, n0 / 16 + j, 0, lane);
+      if constexpr (sizeof(T) == 2) c.lo[j] = *(const u4 *)column_at<T>(S.column, P.RP, step / TB, n0 / 16 + j, 1, lane);
+    }
+  };
+  constexpr uint32_t kWindow = 256;   // steps looked over at a time
+  __shared__ uint16_t lists[kGradWaves][kWindow / kGradWaves];
+  __shared__ uint32_t any_of[kWindow / 32], all_of[kWindow / 32];   // a bit per step
+  static_assert(kWindow / 32 == kGradWaves, "32 steps to a wavefront");
+  for (uint32_t w0 = t0; rank > n0 && w0 < t1; w0 += kWindow * TB) {
+    // The steps that hold a token of the adapter: each wavefront looks over 32,
+    // 64 tokens at a time.
+    uint32_t any = 0, all = 0;
+#pragma unroll 8
+    for (uint32_t i = 0; i < 32; i += 64 / TB) {
+      const uint32_t t = w0 + (32 * wave + i) * TB + lane;
+      const uint64_t is = __ballot(t < P.n_pad && P.ids[t < P.n_pad ? t : 0] == (int32_t)a);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) any |= v[e] == a;
+      for (uint32_t k = 0; k < 64 / TB; ++k) {
+        const uint32_t m = (uint32_t)(is >> (TB * k)) & (TB == 32 ? ~0u : 0xFFFFu);
+        any |= (uint32_t)(m != 0) << (i + k);
+        all |= (uint32_t)(m == (TB == 32 ? ~0u : 0xFFFFu)) << (i + k);
       }
     }
-    uint64_t steps = __ballot(any), mine = 0;
-    for (uint32_t i = 0; steps; ++i, steps &= steps - 1)
-      if (i % kGradWaves == wave) mine |= steps & -steps;
-    if (mine) load(w0 + __builtin_ctzll(mine) * TB);
-    while (mine) {
-      const uint32_t t = w0 + __builtin_ctzll(mine) * TB + grp * SP;
-      mine &= mine - 1;
-      // Rows of other adapters count nothing, whatever they hold.
-      bool whole = true;
-      bool live[SP];
+    // (a split's steps end at its last token's)
+    const uint32_t left = w0 + 32 * wave * TB < t1 ? (t1 - w0 - 32 * wave * TB + TB - 1) / TB : 0;
+    if (left < 32) any &= (1u << left) - 1;
+    __syncthreads();   // (the last window's are read)
+    if (lane == 0) any_of[wave] = any, all_of[wave] = all;
+    __syncthreads();
+    // This wavefront's every eighth of them: the step's number, and kWindow if
+    // it holds others' tokens as well.
+    uint32_t found = 0;
 #pragma unroll
-      for (uint32_t j = 0; j < SP; ++j) {
-        live[j] = id[j] == (int32_t)a;
-        whole &= live[j];
-      }
-      if (!__all(whole)) {
+    for (uint32_t k = 0; k < kWindow / 64; ++k) {
+      const bool any_k = any_of[2 * k + lane / 32] >> (lane % 32) & 1, all_k = all_of[2 * k + lane / 32] >> (lane % 32) & 1;
+      const uint64_t have = __ballot(any_k);
+      const uint32_t i = found + __builtin_popcountll(have & (((uint64_t)1 << lane) - 1));
+      if (any_k && i % kGradWaves == wave) lists[wave][i / kGradWaves] = (uint16_t)(64 * k + lane + (all_k ? 0 : kWindow));
+      found += __builtin_popcountll(have);
+    }
+    wave_sync();
+    const uint32_t mine = found / kGradWaves + (wave < found % kGradWaves);
+    auto step_of = [&](uint32_t i) {
+      return (uint32_t)__builtin_amdgcn_readfirstlane(lists[wave][i < mine ? i : mine - 1]);
+    };
+    if (mine == 0) continue;
+    auto first_token = [&](uint32_t i) { return w0 + step_of(i) % kWindow * TB; };
+    load_rows(x0, first_token(0));
+    load_columns(v0, first_token(0));
+    load_rows(x1, first_token(1));
+    // Step i; its operands are asked for without branches, which would make the
+    // waits wait for all, and stay in the registers they come to.
+    auto compute = [&](uint32_t i, Rows &x, Columns &v, Columns &v_next, Rows &x_next) {
+      load_columns(v_next, first_token(i + 1));
+      load_rows(x_next, first_token(i + 2));
+      const uint32_t s = step_of(i);
+      if (s >= kWindow) {   // rows of other adapters count nothing, whatever they hold
+        const uint32_t t = w0 + s % kWindow * TB + grp * SP;
 #pragma unroll
         for (uint32_t j = 0; j < SP; ++j) {
+          const bool live = P.ids[t + j] == (int32_t)a;
 #pragma unroll
-          for (uint32_t i = 0; i < W; ++i) x[j][i] = live[j] ? x[j][i] : 0;
-          const uint32_t keep = live[j] ? 0 : sizeof(T) == 4 ? ~0u : 0xFFFFu << (16 * (j % 2));
+          for (uint32_t k = 0; k < W; ++k) x.x[j][k] = live ? x.x[j][k] : 0;
+          const uint32_t keep = live || sizeof(T) == 4 ? ~0u : ~(0xFFFFu << (16 * (j % 2)));
 #pragma unroll
-          for (int i = 0; i < RT; ++i) {
-            hi[i][sizeof(T) == 4 ? j : j / 2] &= ~keep;
-            if constexpr (sizeof(T) == 2) lo[i][j / 2] &= ~keep;
+          for (int q = 0; q < RT; ++q) {
+            if constexpr (sizeof(T) == 4) {
+              v.hi[q][j] = live ? v.hi[q][j] : 0;
+            } else {
+              v.hi[q][j / 2] &= keep;
+              v.lo[q][j / 2] &= keep;
+            }
           }
         }
       }
-      uint32_t y[SP][W];
-      u4 vh[RT], vl[RT];
 #pragma unroll
-      for (uint32_t j = 0; j < SP; ++j)
+      for (uint32_t u = 0; u < E; ++u) {
+        const u4 f = column_of<T>(x.x, u);
 #pragma unroll
-        for (uint32_t i = 0; i < W; ++i) y[j][i] = x[j][i];
-#pragma unroll
-      for (int j = 0; j < RT; ++j) {
-        vh[j] = hi[j];
-        if constexpr (sizeof(T) == 2) vl[j] = lo[j];
+        for (int j = 0; j < RT; ++j) acc[u][j] = mma_wide<T>(f, v.hi[j], v.lo[sizeof(T) == 2 ? j : 0], acc[u][j]);
       }
-      if (mine) load(w0 + __builtin_ctzll(mine) * TB);
-      if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (uint32_t u = 0; u < E; ++u)
-#pragma unroll
-          for (int j = 0; j < RT; ++j) acc[u][j] = mma<T>((u4){y[0][u], y[1][u], y[2][u], y[3][u]}, vh[j], acc[u][j]);
-      } else {
-#pragma unroll
-        for (uint32_t u = 0; u < E; ++u) {
-          u4 f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) f[i] = u & 1 ? pair_high(y[2 * i][u / 2], y[2 * i + 1][u / 2]) : pair_low(y[2 * i][u / 2], y[2 * i + 1][u / 2]);
-#pragma unroll
-          for (int j = 0; j < RT; ++j) acc[u][j] = mma_wide<T>(f, vh[j], vl[j], acc[u][j]);
-        }
-      }
+    };
+    for (uint32_t i = 0;; i += 6) {
+      compute(i, x0, v0, v1, x2);
+      if (i + 1 >= mine) break;
+      compute(i + 1, x1, v1, v0, x0);
+      if (i + 2 >= mine) break;
+      compute(i + 2, x2, v0, v1, x1);
+      if (i + 3 >= mine) break;
+      compute(i + 3, x0, v1, v0, x2);
+      if (i + 4 >= mine) break;
+      compute(i + 4, x1, v0, v1, x0);
+      if (i + 5 >= mine) break;
+      compute(i + 5, x2, v1, v0, x1);
+      if (i + 6 >= mine) break;
     }
+    wave_sync();   // (the list is read)
   }
 
   // The wavefronts' sums, 16 ranks at a time.  acc[u][j][i]: column (4 grp + i) of the
@@ -579,24 +651,30 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
   for (int j = 0; j < RT; ++j) {
     __syncthreads();
 #pragma unroll
-    for (uint32_t u = 0; u < E; ++u)
+    for (uint32_t u = 0; u < E; u += 4)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) so[wave][col][((4 * grp + i) * E + u) ^ (4 * col)] = acc[u][j][i];
+      for (int i = 0; i < 4; ++i)
+        *(f4 *)&so[wave][col][((4 * grp + i) * E + u) ^ (4 * col)] = (f4){acc[u][j][i], acc[u + 1][j][i], acc[u + 2][j][i], acc[u + 3][j][i]};
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < 16 * C; e += 512) {
+    for (uint32_t e = threadIdx.x; e < 4 * C; e += 512) {   // four columns of a rank
       // dA: consecutive threads along the columns; dB: along the ranks
-      const uint32_t r = second ? e % 16 : e / C, c = second ? e / 16 : e % C;
-      float s = 0;
+      const uint32_t r = second ? e % 16 : e / (C / 4), c = (second ? e / 16 : e % (C / 4)) * 4;
+      f4 s = (f4){0, 0, 0, 0};
 #pragma unroll
-      for (uint32_t w = 0; w < kGradWaves; ++w) s += so[w][r][c ^ (4 * r)];
+      for (uint32_t w = 0; w < kGradWaves; ++w) s += *(const f4 *)&so[w][r][c ^ (4 * r)];
       // Column c of the slice is element c % E of lane c / E, whose columns may have stepped back.
       const uint32_t want = c0 + c / E * E, from = want + E <= S.n ? want : S.n - E, k = from + c % E;
       const uint32_t rr = n0 + 16 * j + r;
-      if (k < want || want >= S.n || rr >= P.I.R) continue;
+      if (want >= S.n || rr >= P.I.R) continue;
+      if (rr >= rank) s = (f4){0, 0, 0, 0};   // (a NaN row times the zeros there)
       const uint64_t o = second ? ((uint64_t)a * S.n + k) * P.I.R + rr : ((uint64_t)a * P.I.R + rr) * S.n + k;
-      if (rr >= rank) s = 0;   // (a NaN row times the zeros there)
-      if (P.splits > 1) S.part[(uint64_t)split * P.I.n_adapter * P.I.R * S.n + o] = s;
-      else ((T *)S.out)[o] = (T)s;
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) {
+        if (k + q < want) continue;
+        const uint64_t at = o + (second ? q * P.I.R : q);
+        if (P.splits > 1) S.part[(uint64_t)split * P.I.n_adapter * P.I.R * S.n + at] = s[q];
+        else ((T *)S.out)[at] = (T)s[q];
+      }
     }
   }
 }

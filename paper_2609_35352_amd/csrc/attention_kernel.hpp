@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
   __shared__ Shared sh;
 
   const uint32_t split = blockIdx.y, kv = blockIdx.x / P.head_blocks, hb = blockIdx.x % P.head_blocks, seq = blockIdx.z;
-  const uint32_t lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+  const uint32_t lane = threadIdx.x & 63, w = wave_index(), col = lane & 15, grp = lane >> 4;
   int32_t first, n;
   key_range(P, seq, first, n);
   const int32_t start = first / TK * TK + (int32_t)(split * P.chunk);
