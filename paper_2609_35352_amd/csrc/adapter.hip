@@ -369,9 +369,9 @@ int fiona_adapter_backward(const fiona_adapters *H, const fiona_adapter_args *ar
       G.side[0] = {A.x, H->column[1], A.dA, H->grad[0], A.x_row, D.d_in, grad_slices(D.d_in, D.type, RP)};
       G.side[1] = {A.dy, H->column[0], A.dB, H->grad[1], A.dy_row, D.d_out, grad_slices(D.d_out, D.type, RP)};
       const dim3 grid(G.side[0].slices + G.side[1].slices, D.n_adapter * G.r_chunks, G.splits);
-      if (H->RP == 16) hipLaunchKernelGGL((fiona::grad_kernel<T, 1>), grid, dim3(512), 0, stream, G);
-      else if (H->RP == 32) hipLaunchKernelGGL((fiona::grad_kernel<T, 2>), grid, dim3(512), 0, stream, G);
-      else hipLaunchKernelGGL((fiona::grad_kernel<T, 4>), grid, dim3(512), 0, stream, G);
+      if (H->RP == 16) hipLaunchKernelGGL((fiona::grad_kernel<T, 1>), grid, dim3(256), 0, stream, G);
+      else if (H->RP == 32) hipLaunchKernelGGL((fiona::grad_kernel<T, 2>), grid, dim3(256), 0, stream, G);
+      else hipLaunchKernelGGL((fiona::grad_kernel<T, 4>), grid, dim3(256), 0, stream, G);
       if (G.splits > 1)
         hipLaunchKernelGGL(fiona::grad_sum_kernel<T>, dim3((uint32_t)((wa + wb + 255) / 256)), dim3(256), 0, stream,
                            fiona::GradSumParams{{H->grad[0], H->grad[1]}, {A.dA, A.dB}, {wa, wb}, G.splits});

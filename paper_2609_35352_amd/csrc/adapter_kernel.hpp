@@ -17,6 +17,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "mma.hpp"
 
 namespace fiona {
@@ -160,7 +162,7 @@ struct ExpandParams {
 // (contiguous, and shared through the caches), and the tile passes through LDS
 // to meet the base rows 128 or 256 bytes of a row at a time.
 template <typename T, int RT>
-__global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
+__global__ void __launch_bounds__(256, (sizeof(T) == 2 ? RT <= 4 : RT <= 2) ? 2 : 1) expand_kernel(ExpandParams P) {
   constexpr uint32_t E = kLaneElems<T>, FK = kFragElems<T>, RP = 16 * RT;
   constexpr int KF = (RP + FK - 1) / FK, PARTS = sizeof(T) == 2 ? 2 : 1;
   constexpr uint32_t LP = 64 / E, NI = 16 * LP / 64;    // lanes of a row's 64 columns, and rows of a lane in a tile of 16
@@ -174,13 +176,14 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
   for_adapters(P.I, row0, lane, blockIdx.z, P.slots, true, [&](int32_t a, uint32_t rank, uint64_t rows, uint32_t lead) {
     if (rank == 0 && P.base == P.out) return;
     u4 mask[KF];
-    const T *wa = (const T *)P.w;
-    uint32_t wn = 0;
+    // The adapter's factor and the elements from there to the table's end (rows
+    // without an adapter read the first one's where there is no branch, unused).
+    const uint32_t fa = rank ? (uint32_t)a : 0;
+    const T *wa = (const T *)P.w + (uint64_t)fa * P.O * P.w_cols;
+    const uint64_t left = (uint64_t)(P.I.n_adapter - fa) * P.O * P.w_cols;
+    const uint32_t wn = left < 0x7FFFFFFF ? (uint32_t)left : 0x7FFFFFFF;
     float scale = 1;
     if (rank) {
-      wa += (uint64_t)a * P.O * P.w_cols;
-      const uint64_t left = (uint64_t)(P.I.n_adapter - a) * P.O * P.w_cols;
-      wn = left < 0x7FFFFFFF ? (uint32_t)left : 0x7FFFFFFF;
       if (P.scaling) scale = P.scaling[a];
 #pragma unroll
       for (int f = 0; f < KF; ++f) mask[f] = first_mask<T>((int)rank - (int)(f * FK + grp * E));
@@ -224,9 +227,10 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
     }
     uint32_t start = blockIdx.x * P.slice + 64 * wave;
     if (start >= end) return;
-    // A tile's base rows are asked for four tiles ahead, the next columns'
+    // A tile's base rows are asked for four tiles (in 32 bits two) ahead, the next columns'
     // factor as soon as the last tile's products are done.
-    u4 b[4][NI], w[KF][4];
+    constexpr uint32_t SETS = sizeof(T) == 2 ? 4 : 2;
+    u4 b[SETS][NI], w[KF][4];
     auto load_w = [&](uint32_t o0) {
 #pragma unroll
       for (int f = 0; f < KF; ++f)
@@ -236,11 +240,17 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
           w[f][u] = load_shared<T>(piece_at<T>(wa, o * P.w_cols + f * FK + grp * E, wn));
         }
     };
+    // Rows are a scalar address and a 32-bit offset: 64 rows at most kMaxStride apart.
+    const char *base0 = (const char *)P.base + (uint64_t)row0 * P.base_row * sizeof(T);
+    char *out0 = (char *)P.out + (uint64_t)row0 * P.out_row * sizeof(T);
+    const uint32_t base_bytes = (uint32_t)(P.base_row * sizeof(T)), out_bytes = (uint32_t)(P.out_row * sizeof(T));
+    const uint32_t base_last = (here - 1) * base_bytes;
     auto load_base = [&](u4 (&b)[NI], uint32_t o0, uint32_t t) {
+      const uint32_t at = o0 + pc * E, from = (at + E <= P.O ? at : P.O - E) * (uint32_t)sizeof(T);
 #pragma unroll
       for (uint32_t i = 0; i < NI; ++i) {
-        const uint32_t r = 16 * t + tr + (64 / LP) * i, row = r < here ? r : here - 1;
-        b[i] = load_shared<T>(piece_at<T>((const T *)P.base + (uint64_t)(row0 + row) * P.base_row, o0 + pc * E, P.O));
+        const uint32_t off = (tr + 16 * t + (64 / LP) * i) * base_bytes;
+        b[i] = load_shared<T>((const T *)(base0 + ((off < base_last ? off : base_last) + from)));
       }
     };
     // Values of a lane's row piece: products from LDS and base, as they are stored.
@@ -279,31 +289,43 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
       for (int u = 0; u < 4; ++u) *(f4 *)&so[wave][col][16 * u + 4 * grp] = acc[u] * scale;
       wave_sync();
     };
-    // All 64 tokens have the adapter: no branches, so that a wait is for what
-    // is used next only (loads and stores complete in order).
-    if (rank && P.base && rows == ~(uint64_t)0 && start + 64 <= end && ((uint64_t)P.O * P.w_cols + KF * FK <= wn)) {
+    // Whole tiles of columns with a base: loads without branches, so that a wait
+    // is for what is used next only (loads and stores complete in order).
+    auto whole = [&](uint32_t o0) { return o0 + 64 <= end && (rank == 0 || (o0 + 63) * P.w_cols + KF * FK <= wn); };
+    auto columns = [&](auto full) {   // full: all 64 tokens have the adapter
+      constexpr bool FULL = decltype(full)::value;
       load_w(start);
 #pragma unroll
-      for (uint32_t t = 0; t < 4; ++t) load_base(b[t], start, t);
-      for (; start + 64 <= end; start += 256) {
-        const uint32_t next = start + 256 + 64 <= end ? start + 256 : start;   // (the last columns' again)
+      for (uint32_t t = 0; t < SETS; ++t) load_base(b[t], start, t);
+      for (; whole(start); start += 256) {
+        const uint32_t next = whole(start + 256) ? start + 256 : start;   // (the last columns' again)
 #pragma unroll
         for (uint32_t t = 0; t < 4; ++t) {
-          multiply(t);
+          const bool any = FULL || (rows >> (16 * t) & 0xFFFF) != 0;
+          if (any && (FULL || rank)) multiply(t);
           if (t == 3) load_w(next);
           u4 out[NI];
 #pragma unroll
-          for (uint32_t i = 0; i < NI; ++i) out[i] = finish(i, b[t][i]);
-          load_base(b[t], next, t);
+          for (uint32_t i = 0; i < NI; ++i) out[i] = finish(i, b[t % SETS][i]);
+          load_base(b[t % SETS], t + SETS < 4 ? start : next, (t + SETS) % 4);
 #pragma unroll
-          for (uint32_t i = 0; i < NI; ++i)
-            __builtin_nontemporal_store(out[i], (u4_any *)((T *)P.out + (uint64_t)(row0 + 16 * t + tr + (64 / LP) * i) * P.out_row +
-                                                           start + pc * E));
+          for (uint32_t i = 0; i < NI; ++i) {
+            const uint32_t row = 16 * t + tr + (64 / LP) * i;
+            if (FULL || (rows >> row & 1))
+              __builtin_nontemporal_store(out[i], (u4_any *)(out0 + (row * out_bytes + (start + pc * E) * (uint32_t)sizeof(T))));
+          }
         }
       }
-      if (start >= end) return;
+    };
+    // (the registers of 128 ranks in 32 bits leave no room for it)
+    if constexpr (sizeof(T) == 2 || RT < 8) {
+      if (P.base && whole(start)) {
+        if (sizeof(T) == 2 && rows == ~(uint64_t)0 && rank) columns(std::true_type{});
+        else columns(std::false_type{});
+        if (start >= end) return;
+      }
     }
-    // Tiles that hold other adapters' tokens, the last columns and the table's end.
+    // The last columns, the table's end, and calls without a base.
     for (uint32_t t = 0; t < 4; ++t) {
       if ((rows >> (16 * t) & 0xFFFF) == 0) continue;
       if (rank) load_w(start);
@@ -332,7 +354,7 @@ __global__ void __launch_bounds__(256) expand_kernel(ExpandParams P) {
           const uint32_t row = 16 * t + tr + (64 / LP) * i;
           const u4 out = finish(i, v[i]);
           if (!(rows >> row & 1)) continue;
-          T *p = (T *)P.out + (uint64_t)(row0 + row) * P.out_row + at;
+          T *p = (T *)(out0 + (row * out_bytes + at * (uint32_t)sizeof(T)));
           if (at + E <= P.O) {
             __builtin_nontemporal_store(out, (u4_any *)p);
           } else {
@@ -477,7 +499,7 @@ template <typename T>
 constexpr uint32_t grad_width(uint32_t RP) {
   return sizeof(T) == 2 && RP >= 32 ? 4 : kLaneElems<T>;
 }
-constexpr uint32_t kGradWaves = 8;
+constexpr uint32_t kGradWaves = 4;
 
 // Element u of each of a lane's tokens: the lane's part of a transposed fragment.
 template <typename T, int SP, int W>
@@ -492,12 +514,12 @@ __device__ __forceinline__ u4 column_of(const uint32_t (&x)[SP][W], uint32_t u) 
 }
 
 // A workgroup takes 128 or 256 bytes of the rows' columns for one adapter and up to 64
-// of its ranks; its eight wavefronts take the steps that hold a token of the
+// of its ranks; its four wavefronts take the steps that hold a token of the
 // adapter in turn.  Rows are read whole pieces at a time, 16 lanes to a piece,
-// eight tokens to a lane; the transposed fragments (columns x tokens) are
+// eight tokens (four in 32 bits) to a lane; the transposed fragments (columns x tokens) are
 // picked from the tokens' words in registers, as values are in the attention.
 template <typename T, int RT>
-__global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
+__global__ void __launch_bounds__(256) grad_kernel(GradParams P) {
   constexpr uint32_t E = grad_width<T>(16 * RT), C = 16 * E, TB = kGradTokens<T>, SP = TB / 4, W = E * sizeof(T) / 4;
   __shared__ alignas(16) float so[kGradWaves][16][C];   // column c of rank r at c ^ 4 r, off each other's banks
   const uint32_t lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, grp = lane >> 4;
@@ -516,11 +538,10 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
   // The lane's columns; at the row's end they step back to its last 16 bytes
   // (and are dropped on the way out where another lane has them).
   const uint32_t at = c0 + col * E, cat = at + E <= S.n ? at : S.n - E;
-  // Rows are asked for two steps ahead, fragments of h or g one: in between
-  // lie the products of a step, and loads return in order.
+  // The next step's rows and fragments are on their way while a step is computed.
   struct Rows {
     uint32_t x[SP][W];
-  } x0, x1, x2;
+  } x0, x1;
   struct Columns {
     u4 hi[RT], lo[sizeof(T) == 2 ? RT : 1];
   } v0, v1;
@@ -550,7 +571,7 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
       if constexpr (sizeof(T) == 2) c.lo[j] = *(const u4 *)column_at<T>(S.column, P.RP, step / TB, n0 / 16 + j, 1, lane);
     }
   };
-  constexpr uint32_t kWindow = 256;   // steps looked over at a time
+  constexpr uint32_t kWindow = 128;   // steps looked over at a time
   __shared__ uint16_t lists[kGradWaves][kWindow / kGradWaves];
   __shared__ uint32_t any_of[kWindow / 32], all_of[kWindow / 32];   // a bit per step
   static_assert(kWindow / 32 == kGradWaves, "32 steps to a wavefront");
@@ -575,7 +596,7 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
     __syncthreads();   // (the last window's are read)
     if (lane == 0) any_of[wave] = any, all_of[wave] = all;
     __syncthreads();
-    // This wavefront's every eighth of them: the step's number, and kWindow if
+    // This wavefront's every fourth of them: the step's number, and kWindow if
     // it holds others' tokens as well.
     uint32_t found = 0;
 #pragma unroll
@@ -595,12 +616,11 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
     auto first_token = [&](uint32_t i) { return w0 + step_of(i) % kWindow * TB; };
     load_rows(x0, first_token(0));
     load_columns(v0, first_token(0));
-    load_rows(x1, first_token(1));
     // Step i; its operands are asked for without branches, which would make the
     // waits wait for all, and stay in the registers they come to.
     auto compute = [&](uint32_t i, Rows &x, Columns &v, Columns &v_next, Rows &x_next) {
       load_columns(v_next, first_token(i + 1));
-      load_rows(x_next, first_token(i + 2));
+      load_rows(x_next, first_token(i + 1));
       const uint32_t s = step_of(i);
       if (s >= kWindow) {   // rows of other adapters count nothing, whatever they hold
         const uint32_t t = w0 + s % kWindow * TB + grp * SP;
@@ -628,19 +648,11 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
         for (int j = 0; j < RT; ++j) acc[u][j] = mma_wide<T>(f, v.hi[j], v.lo[sizeof(T) == 2 ? j : 0], acc[u][j]);
       }
     };
-    for (uint32_t i = 0;; i += 6) {
-      compute(i, x0, v0, v1, x2);
+    for (uint32_t i = 0;; i += 2) {
+      compute(i, x0, v0, v1, x1);
       if (i + 1 >= mine) break;
       compute(i + 1, x1, v1, v0, x0);
       if (i + 2 >= mine) break;
-      compute(i + 2, x2, v0, v1, x1);
-      if (i + 3 >= mine) break;
-      compute(i + 3, x0, v1, v0, x2);
-      if (i + 4 >= mine) break;
-      compute(i + 4, x1, v0, v1, x0);
-      if (i + 5 >= mine) break;
-      compute(i + 5, x2, v1, v0, x1);
-      if (i + 6 >= mine) break;
     }
     wave_sync();   // (the list is read)
   }
@@ -656,7 +668,7 @@ __global__ void __launch_bounds__(512) grad_kernel(GradParams P) {
       for (int i = 0; i < 4; ++i)
         *(f4 *)&so[wave][col][((4 * grp + i) * E + u) ^ (4 * col)] = (f4){acc[u][j][i], acc[u + 1][j][i], acc[u + 2][j][i], acc[u + 3][j][i]};
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < 4 * C; e += 512) {   // four columns of a rank
+    for (uint32_t e = threadIdx.x; e < 4 * C; e += 256) {   // four columns of a rank
       // dA: consecutive threads along the columns; dB: along the ranks
       const uint32_t r = second ? e % 16 : e / (C / 4), c = (second ? e / 16 : e % (C / 4)) * 4;
       f4 s = (f4){0, 0, 0, 0};
