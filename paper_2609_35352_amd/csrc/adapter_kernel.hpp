@@ -162,7 +162,7 @@ struct ExpandParams {
 // (contiguous, and shared through the caches), and the tile passes through LDS
 // to meet the base rows 128 or 256 bytes of a row at a time.
 template <typename T, int RT>
-__global__ void __launch_bounds__(256, (sizeof(T) == 2 ? RT <= 4 : RT <= 2) ? 2 : 1) expand_kernel(ExpandParams P) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 && RT <= 2 ? 3 : (sizeof(T) == 2 ? RT <= 4 : RT <= 2) ? 2 : 1) expand_kernel(ExpandParams P) {
   constexpr uint32_t E = kLaneElems<T>, FK = kFragElems<T>, RP = 16 * RT;
   constexpr int KF = (RP + FK - 1) / FK, PARTS = sizeof(T) == 2 ? 2 : 1;
   constexpr uint32_t LP = 64 / E, NI = 16 * LP / 64;    // lanes of a row's 64 columns, and rows of a lane in a tile of 16
@@ -227,9 +227,9 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 2 ? RT <= 4 : RT <= 2) ? 2 
     }
     uint32_t start = blockIdx.x * P.slice + 64 * wave;
     if (start >= end) return;
-    // A tile's base rows are asked for four tiles (in 32 bits two) ahead, the next columns'
+    // A tile's base rows are asked for two tiles ahead, the next columns'
     // factor as soon as the last tile's products are done.
-    constexpr uint32_t SETS = sizeof(T) == 2 ? 4 : 2;
+    constexpr uint32_t SETS = 2;
     u4 b[SETS][NI], w[KF][4];
     auto load_w = [&](uint32_t o0) {
 #pragma unroll

@@ -20,55 +20,144 @@ struct AppendParams {
   uint64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, qo_tok, qo_head;
   uint64_t kc_page, kc_token, kc_head, vc_page, vc_token, vc_head;
   uint32_t n_tok, n_head, n_kv, d, half, n_pos, interleaved, page_size;
+  uint32_t page_mul, page_shift;   // slot / page_size (see page_divisor)
+  uint32_t tokens;                 // of a workgroup
   int64_t n_slot;
 };
 
-// One workgroup per token, one pair or copied element per thread and turn.
+// The page and place of a token's slot; false where it is not in the cache.
+__device__ __forceinline__ bool place_of(const AppendParams &P, uint32_t t, uint64_t &page, uint64_t &at) {
+  const int64_t slot = P.slots[t];
+  if (slot < 0 || slot >= P.n_slot) return false;
+  page = P.page_mul ? __umulhi((uint32_t)slot, P.page_mul) >> P.page_shift : (uint32_t)slot;
+  at = (uint32_t)slot - (uint32_t)page * P.page_size;
+  return true;
+}
+
+// A row's source and destination by its number in the token: query heads, key
+// heads, value heads; false where it is not written.
+template <typename T, typename C>
+__device__ __forceinline__ bool row_of(const AppendParams &P, uint32_t t, uint32_t h, const T *&in, C *&out, bool &turn) {
+  turn = true;
+  if (h < P.n_head) {
+    in = (const T *)P.q + t * P.q_tok + h * P.q_head;
+    out = (C *)P.q_out + t * P.qo_tok + h * P.qo_head;
+    return true;
+  }
+  uint64_t page, at;
+  if (!place_of(P, t, page, at)) return false;
+  h -= P.n_head;
+  if (h < P.n_kv) {
+    in = (const T *)P.k + t * P.k_tok + h * P.k_head;
+    out = (C *)P.kc + page * P.kc_page + at * P.kc_token + h * P.kc_head;
+  } else {
+    h -= P.n_kv;
+    in = (const T *)P.v + t * P.v_tok + h * P.v_head;
+    out = (C *)P.vc + page * P.vc_page + at * P.vc_token + h * P.vc_head;
+    turn = false;
+  }
+  return true;
+}
+
+// Eight elements from and to 16-byte aligned rows, through 32 bits.
+template <typename T>
+struct alignas(16) Eight {
+  T x[8];
+};
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, float (&x)[8]) {
+  const Eight<T> v = *(const Eight<T> *)p;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (float)v.x[i];
+}
+template <typename C>
+__device__ __forceinline__ void store8(C *p, const float (&x)[8]) {
+  Eight<C> v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v.x[i] = (C)x[i];
+  typedef uint32_t w4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (uint32_t i = 0; i < sizeof(v) / 16; ++i) __builtin_nontemporal_store(((const w4 *)&v)[i], (w4 *)p + i);
+}
+
+// Whole pieces: a thread takes 16 elements of a row (eight pairs, or up to two
+// runs of eight copied ones), consecutive threads consecutive pieces of a row,
+// then rows, then tokens.  Everything is read and written once: what bounds it
+// is memory, or for a few tokens the launch.
 template <typename T, typename C>
 __global__ void __launch_bounds__(256) append_kernel(AppendParams P) {
-  const uint32_t t = blockIdx.x, rot = 2 * P.half, units = P.d - P.half;   // pairs, then copied elements
-  const int64_t slot = P.slots[t];
-  const bool keep = slot >= 0 && slot < P.n_slot;
-  const uint64_t page = keep ? (uint64_t)slot / P.page_size : 0, at = keep ? (uint64_t)slot % P.page_size : 0;
-  const int32_t pos = P.half ? P.positions[t] : 0;
-  const bool known = pos >= 0 && (uint32_t)pos < P.n_pos;
-  const uint32_t heads = P.n_head + 2 * P.n_kv;
-  for (uint32_t i = threadIdx.x; i < heads * units; i += 256) {
-    uint32_t h = i / units, u = i % units;
-    const T *in;
-    C *out;
-    bool turn = true;
-    if (h < P.n_head) {
-      in = (const T *)P.q + t * P.q_tok + h * P.q_head;
-      out = (C *)P.q_out + t * P.qo_tok + h * P.qo_head;
+  const uint32_t units = (P.d + 15) / 16, items = (P.n_head + 2 * P.n_kv) * units;
+  const uint32_t i = blockIdx.y * 256 + threadIdx.x;
+  const uint32_t t = blockIdx.x * P.tokens + i / items, h = i % items / units, u = i % units;
+  if (i >= P.tokens * items || t >= P.n_tok) return;
+  const T *in;
+  C *out;
+  bool turn;
+  if (!row_of(P, t, h, in, out, turn)) return;
+  float a[8], b[8], x[8], y[8];
+  if (turn && 8 * u < P.half) {
+    const uint32_t ia = P.interleaved ? 16 * u : 8 * u, ib = P.interleaved ? 16 * u + 8 : 8 * u + P.half;
+    const int32_t pos = P.positions[t];
+    const bool known = pos >= 0 && (uint32_t)pos < P.n_pos;
+    const uint64_t at = (uint64_t)(known ? pos : 0) * P.half + 8 * u;
+    load8(in + ia, a);
+    load8(in + ib, b);
+    load8(P.cos + at, x);
+    load8(P.sin + at, y);
+    if (!known)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = __builtin_nanf("");
+    if (P.interleaved) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {   // pairs 0..3 in the first run, 4..7 in the second
+        float(&r)[8] = k < 4 ? a : b;
+        const float p = r[2 * k % 8], q = r[2 * k % 8 + 1];
+        r[2 * k % 8] = p * x[k] - q * y[k];
+        r[2 * k % 8 + 1] = p * y[k] + q * x[k];
+      }
     } else {
-      if (!keep) continue;
-      h -= P.n_head;
-      if (h < P.n_kv) {
-        in = (const T *)P.k + t * P.k_tok + h * P.k_head;
-        out = (C *)P.kc + page * P.kc_page + at * P.kc_token + h * P.kc_head;
-      } else {
-        h -= P.n_kv;
-        in = (const T *)P.v + t * P.v_tok + h * P.v_head;
-        out = (C *)P.vc + page * P.vc_page + at * P.vc_token + h * P.vc_head;
-        turn = false;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float p = a[k], q = b[k];
+        a[k] = p * x[k] - q * y[k];
+        b[k] = p * y[k] + q * x[k];
       }
     }
+    store8(out + ia, a);
+    store8(out + ib, b);
+    return;
+  }
+  const uint32_t e = 16 * u;
+  const bool two = e + 8 < P.d;
+  load8(in + e, a);
+  load8(in + (two ? e + 8 : e), b);
+  store8(out + e, a);
+  if (two) store8(out + e + 8, b);
+}
+
+// Rows of any size and alignment: one workgroup per token, one pair or copied
+// element per thread and turn.
+template <typename T, typename C>
+__global__ void __launch_bounds__(256) append_any_kernel(AppendParams P) {
+  const uint32_t t = blockIdx.x, rot = 2 * P.half, units = P.d - P.half;   // pairs, then copied elements
+  const int32_t pos = P.half ? P.positions[t] : 0;
+  const bool known = pos >= 0 && (uint32_t)pos < P.n_pos;
+  for (uint32_t i = threadIdx.x; i < (P.n_head + 2 * P.n_kv) * units; i += 256) {
+    const uint32_t u = i % units;
+    const T *in;
+    C *out;
+    bool turn;
+    if (!row_of(P, t, i / units, in, out, turn)) continue;
     if (u >= P.half) {
       out[rot + (u - P.half)] = (C)(float)in[rot + (u - P.half)];
       continue;
     }
     const uint32_t ia = P.interleaved ? 2 * u : u, ib = P.interleaved ? 2 * u + 1 : u + P.half;
     const float a = (float)in[ia], b = (float)in[ib];
-    if (!turn) {
-      out[ia] = (C)a;
-      out[ib] = (C)b;
-      continue;
-    }
-    const float c = known ? P.cos[(uint64_t)pos * P.half + u] : __builtin_nanf("");
-    const float s = known ? P.sin[(uint64_t)pos * P.half + u] : __builtin_nanf("");
-    out[ia] = (C)(a * c - b * s);
-    out[ib] = (C)(a * s + b * c);
+    const float c = !turn ? 1.f : known ? P.cos[(uint64_t)pos * P.half + u] : __builtin_nanf("");
+    const float s = !turn ? 0.f : known ? P.sin[(uint64_t)pos * P.half + u] : 0.f;
+    out[ia] = (C)(turn ? a * c - b * s : a);
+    out[ib] = (C)(turn ? a * s + b * c : b);
   }
 }
 
@@ -128,9 +217,21 @@ extern "C" int fiona_kv_append(const fiona_kv_cache *cache, const fiona_append_a
   P.n_tok = A.n_tok, P.n_head = A.n_head, P.n_kv = K.n_kv, P.d = K.head_dim, P.half = A.rot_dim / 2, P.n_pos = A.n_pos;
   P.interleaved = A.interleaved != 0, P.page_size = K.page_size;
   P.n_slot = (int64_t)K.n_pages * K.page_size;
+  page_divisor(K.page_size, P.page_mul, P.page_shift);
+  // 16-byte pieces where every row and its halves hold whole ones.
+  const bool pieces = d % 8 == 0 && P.half % 8 == 0 && rows_aligned16(in[0]) && rows_aligned16(in[1]) &&
+                      rows_aligned16(out[0]) && rows_aligned16(out[1]) &&
+                      (!A.n_head || (rows_aligned16(in[2]) && rows_aligned16(out[2]))) &&
+                      (!A.rot_dim || (rows_aligned16(in[5]) && rows_aligned16(in[6])));
+  const uint32_t items = (A.n_head + 2 * K.n_kv) * ((uint32_t)(d + 15) / 16);
+  P.tokens = std::max(1u, 256 / items);
+  const dim3 grid = pieces ? dim3((A.n_tok + P.tokens - 1) / P.tokens, (P.tokens * items + 255) / 256) : dim3(A.n_tok);
   with_type(A.rows_type, [&](auto t) {
     with_type(K.type, [&](auto c) {
-      hipLaunchKernelGGL((fiona::append_kernel<decltype(t), decltype(c)>), dim3(A.n_tok), dim3(256), 0, stream, P);
+      using T = decltype(t);
+      using C = decltype(c);
+      if (pieces) hipLaunchKernelGGL((fiona::append_kernel<T, C>), grid, dim3(256), 0, stream, P);
+      else hipLaunchKernelGGL((fiona::append_any_kernel<T, C>), grid, dim3(256), 0, stream, P);
     });
   });
   return hipGetLastError() == hipSuccess ? FIONA_OK : FIONA_ERR_HIP;

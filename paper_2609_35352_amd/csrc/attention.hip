@@ -140,11 +140,7 @@ int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cach
   P.page_size = D.page_size, P.n_pages = K.n_pages, P.window = A.window;
   P.scale = A.scale * fiona::kLog2e;
   if (A.softcap > 0) P.cap_in = 2.f * fiona::kLog2e * A.scale / A.softcap, P.cap_out = A.softcap * fiona::kLog2e;
-  if (D.page_size > 1) {
-    const uint32_t s = 32 - __builtin_clz(D.page_size - 1);   // 2^(s - 1) < page_size <= 2^s
-    P.page_mul = (uint32_t)((((uint64_t)1 << (31 + s)) + D.page_size - 1) / D.page_size);
-    P.page_shift = s - 1;
-  }
+  page_divisor(D.page_size, P.page_mul, P.page_shift);
   P.max_length = (uint32_t)std::min<uint64_t>(D.max_length, (uint64_t)A.table_width * D.page_size);
   if (K.n_pages == 0) P.max_length = 0;
   // A window's keys start anywhere in a tile.

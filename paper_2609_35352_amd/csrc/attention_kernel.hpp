@@ -51,9 +51,7 @@ struct AttendParams {
   float cap_in, cap_out;                        // 2 log2(e) scale / softcap, softcap log2(e); 0 without one
 };
 
-// token / page_size for token < 2^31: (token * page_mul) >> (32 + page_shift)
-// with page_mul = ceil(2^(32 + page_shift) / page_size), 2^page_shift <=
-// page_size / 2 < 2^(page_shift + 1); pages of one token have page_mul 0.
+// token / page_size for token < 2^31 (see page_divisor).
 __device__ __forceinline__ uint32_t page_of(const AttendParams &P, uint32_t token) {
   return P.page_mul ? __umulhi(token, P.page_mul) >> P.page_shift : token;
 }

@@ -92,6 +92,17 @@ inline bool rows_aligned16(const Rows &r) {
   return true;
 }
 
+// Division by a page size: token / page_size = umulhi(token, mul) >> shift for
+// token < 2^31, with 2^shift < page_size <= 2^(shift + 1) and
+// mul = ceil(2^(32 + shift) / page_size) (whose error, below page_size, times the
+// token stays below 2^(32 + shift)); mul 0 for pages of one token.
+inline void page_divisor(uint32_t page_size, uint32_t &mul, uint32_t &shift) {
+  mul = shift = 0;
+  if (page_size <= 1) return;
+  shift = 31 - __builtin_clz(page_size - 1);
+  mul = (uint32_t)((((uint64_t)1 << (32 + shift)) + page_size - 1) / page_size);
+}
+
 inline bool misaligned(const void *p, uint64_t elem) { return ((uint64_t)p & (elem - 1)) != 0; }
 
 }  // namespace fiona_host
