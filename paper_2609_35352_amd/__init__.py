@@ -472,6 +472,7 @@ _ADAPTERS_DESC = struct.Struct("@7I")
 _ADAPTER_ARGS = struct.Struct("@I6PQ2P2Q5P3Q")
 
 _DTYPES = {}   # torch dtype -> fiona_type
+_raw_stream = []
 _INT = {}      # bytes -> torch dtype, and "f32"
 
 
@@ -487,9 +488,18 @@ def _lm_lib():
             getattr(L, name).restype, getattr(L, name).argtypes = ctypes.c_int, args
         for name in ("fiona_attention_destroy", "fiona_adapters_destroy"):
             getattr(L, name).restype, getattr(L, name).argtypes = None, [p]
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (without the stream object: 2 us a call)
+        _raw_stream.append(raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream))
         _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
         _INT.update({4: torch.int32, 8: torch.int64, "f32": torch.float32})
     return L
+
+
+def _stream_of(stream, dev: int) -> int:
+    """The stream's handle; by default the current stream of the tensors' device."""
+    if stream is None:
+        return _raw_stream[0](dev)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _type_code(dtype) -> int:
@@ -568,7 +578,7 @@ def kv_append(k, v, slots, k_cache, v_cache, positions=None, cos=None, sin=None,
         pp = _packed(positions, "positions", _INT[4], (n,), dev)
     args = _APPEND_ARGS.pack(n, H, code, rot, n_pos, 1 if interleaved else 0, k.data_ptr(), v.data_ptr(), qp, qop,
                              ks[0], ks[1], vs[0], vs[1], qs[0], qs[1], qos[0], qos[1], at, pp, cp, sp)
-    rc = lib().fiona_kv_append(cache, args, _stream_handle(stream))
+    rc = lib().fiona_kv_append(cache, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_kv_append")
 
@@ -617,7 +627,7 @@ def paged_attention(att: Attention, q, k_cache, v_cache, page_table, lengths, ou
                                 float(softcap), q.data_ptr(), out.data_ptr(), lp, qs[0], qs[1], os_[0], os_[1],
                                 ts[0] if n > 1 else max(ts[0], width), page_table.data_ptr(),
                                 _packed(lengths, "lengths", _INT[4], (n,), dev))
-    rc = lib().fiona_paged_attention(att.handle, cache, args, _stream_handle(stream))
+    rc = lib().fiona_paged_attention(att.handle, cache, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_paged_attention")
 
@@ -670,7 +680,7 @@ def adapter_linear(ad: Adapters, x, ids, A, B, base, y, ranks=None, scaling=None
     bp, bs = (base.data_ptr(), _rows(base, "base", ad.dtype, shape, dev)[0]) if base is not None else (0, 0)
     ys = _rows(y, "y", ad.dtype, shape, dev)
     args = _ADAPTER_ARGS.pack(*head, bp, y.data_ptr(), bs, ys[0], 0, 0, 0, 0, 0, 0, 0, 0)
-    rc = lib().fiona_adapter_linear(ad.handle, args, _stream_handle(stream))
+    rc = lib().fiona_adapter_linear(ad.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_adapter_linear")
 
@@ -686,6 +696,6 @@ def adapter_backward(ad: Adapters, x, ids, A, B, dy, dx_base, dx, dA, dB, ranks=
     args = _ADAPTER_ARGS.pack(*head, 0, 0, 0, 0, dy.data_ptr(), bp, dx.data_ptr(),
                               _packed(dA, "dA", dt, (ad.n_adapter, ad.max_rank, ad.d_in), dev),
                               _packed(dB, "dB", dt, (ad.n_adapter, ad.d_out, ad.max_rank), dev), gs[0], bs, xs[0])
-    rc = lib().fiona_adapter_backward(ad.handle, args, _stream_handle(stream))
+    rc = lib().fiona_adapter_backward(ad.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_adapter_backward")
