@@ -182,8 +182,10 @@ void launch_shrink(const fiona_adapters *H, const fiona::AdapterIds &I, const fi
   P.I = I, P.splits = splits, P.slots = slots_of(I.n_tok, I.n_adapter);
   for (uint32_t i = 0; i < n_sides; ++i) P.side[i] = sides[i];
   with_tiles(H->RP, [&](auto rt) {
-    hipLaunchKernelGGL((fiona::shrink_kernel<T, decltype(rt)::value>), dim3(blocks_of(I.n_tok), splits, P.slots * n_sides),
-                       dim3(256), 0, stream, P);
+    constexpr int RT = decltype(rt)::value;
+    const dim3 grid(blocks_of(I.n_tok), splits, P.slots * n_sides);
+    if (n_sides == 1) hipLaunchKernelGGL((fiona::shrink_kernel<T, RT, true>), grid, dim3(256), 0, stream, P);
+    else hipLaunchKernelGGL((fiona::shrink_kernel<T, RT, false>), grid, dim3(256), 0, stream, P);
   });
 }
 

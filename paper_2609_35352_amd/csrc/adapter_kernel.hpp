@@ -73,10 +73,11 @@ struct ShrinkParams {
   uint32_t splits, slots;
 };
 
+// ONCE: the rows are read by this pass alone (the forward call).
 // Row pieces of 256 bytes pass through LDS to become fragments: rows are read
 // whole (16 lanes to a piece) and the factor's rows are shared by the
 // workgroup's four wavefronts, 16 tokens each.
-template <typename T, int RT>
+template <typename T, int RT, bool ONCE>
 __global__ void __launch_bounds__(256) shrink_kernel(ShrinkParams P) {
   constexpr uint32_t E = kLaneElems<T>, CE = 16 * E, RP = 16 * RT;
   __shared__ alignas(16) uint8_t sx[kRows][272], sw[RP][272];
@@ -105,7 +106,7 @@ __global__ void __launch_bounds__(256) shrink_kernel(ShrinkParams P) {
     auto load = [&](uint32_t c) {
       const uint32_t at = c * CE + pc * E;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) xv[i] = load_once<T>(piece_at<T>(xr[i], at, S.K));
+      for (int i = 0; i < 4; ++i) xv[i] = ONCE ? load_once<T>(piece_at<T>(xr[i], at, S.K)) : load_shared<T>(piece_at<T>(xr[i], at, S.K));
 #pragma unroll
       for (int j = 0; j < RT; ++j) wv[j] = load_shared<T>(piece_at<T>(wr[j], at, S.K));
     };
@@ -389,19 +390,22 @@ __global__ void __launch_bounds__(256) transpose_kernel(TransposeParams P) {
   const uint32_t n = of_b ? P.d_out : P.d_in, k0 = (blockIdx.x - (of_b ? nb_in : 0)) * 64;
   for (uint32_t r0 = 0; r0 < P.RP; r0 += 64) {
     if (r0) __syncthreads();
-    for (uint32_t i = q; i < 64; i += 4) {
-      const uint32_t k = k0 + (of_b ? i : c), r = r0 + (of_b ? c : i);
-      T v = (T)0.f;
-      if (k < n && r < rank)
-        v = of_b ? ((const T *)P.B)[((uint64_t)a * n + k) * P.I.R + r] : ((const T *)P.A)[((uint64_t)a * P.I.R + r) * n + k];
-      tile[i][c] = v;
+    T v[16];
+#pragma unroll
+    for (uint32_t i = 0; i < 16; ++i) {
+      const uint32_t k = k0 + (of_b ? 4 * i + q : c), r = r0 + (of_b ? c : 4 * i + q);
+      const uint32_t ki = k < n ? k : n - 1, ri = r < P.I.R ? r : P.I.R - 1;
+      v[i] = of_b ? ((const T *)P.B)[((uint64_t)a * n + ki) * P.I.R + ri] : ((const T *)P.A)[((uint64_t)a * P.I.R + ri) * n + ki];
     }
+#pragma unroll
+    for (uint32_t i = 0; i < 16; ++i) tile[4 * i + q][c] = r0 + (of_b ? c : 4 * i + q) < rank ? v[i] : (T)0.f;
     __syncthreads();
-    for (uint32_t i = q; i < 64; i += 4) {
-      const uint32_t k = k0 + (of_b ? c : i), r = r0 + (of_b ? i : c);
+#pragma unroll
+    for (uint32_t i = 0; i < 16; ++i) {
+      const uint32_t k = k0 + (of_b ? c : 4 * i + q), r = r0 + (of_b ? 4 * i + q : c);
       if (k >= n || r >= P.RP) continue;
-      if (of_b) ((T *)P.BT)[((uint64_t)a * P.RP + r) * n + k] = tile[c][i];
-      else ((T *)P.AT)[((uint64_t)a * n + k) * P.RP + r] = tile[c][i];
+      if (of_b) ((T *)P.BT)[((uint64_t)a * P.RP + r) * n + k] = tile[c][4 * i + q];
+      else ((T *)P.AT)[((uint64_t)a * n + k) * P.RP + r] = tile[c][4 * i + q];
     }
   }
 }
@@ -555,11 +559,11 @@ __global__ void __launch_bounds__(256) grad_kernel(GradParams P) {
       const char *p = (const char *)S.x + (uint64_t)row * row_bytes +
                       (row + grp * SP < P.I.n_tok ? lane_at : cat * (uint32_t)sizeof(T));
       if constexpr (W == 4) {
-        const u4 v = load_once<T>((const T *)p);
+        const u4 v = load_shared<T>((const T *)p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) r.x[j][i] = v[i];
       } else {
-        const u2 v = __builtin_nontemporal_load((const u2_any *)p);
+        const u2 v = *(const u2_any *)p;
         r.x[j][0] = v[0], r.x[j][1] = v[1];
       }
     }

@@ -115,6 +115,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
 #pragma unroll
   for (int t = 0; t < OT; ++t) o[t] = (f4){0, 0, 0, 0};
   float m = -INFINITY, l = 0;
+  const float unit = P.cap_out > 0 ? 1.f : P.scale;   // of a score, in powers of two
   const int32_t *table = P.table + seq * P.table_stride;
   const T *kb = (const T *)P.kc + kv * P.k_head, *vb = (const T *)P.vc + kv * P.v_head;
 
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
         sc[j] = P.cap_out * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(P.cap_in * acc[j / 4][j % 4]) + 1.f));
     } else {
 #pragma unroll
-      for (int j = 0; j < SP; ++j) sc[j] = acc[j / 4][j % 4] * P.scale;
+      for (int j = 0; j < SP; ++j) sc[j] = acc[j / 4][j % 4];
     }
     if (!whole) {   // places that do not count hold anything: no score, and no value that zero would not silence
 #pragma unroll
@@ -240,7 +241,9 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
 #pragma unroll
     for (int j = 1; j < SP; ++j) top = fmaxf(top, sc[j]);
 
-    const float mn = fmaxf(m, column_max(top)), ms = mn == -INFINITY ? 0.f : mn;
+    // The maximum is rounded once and taken from the exact scaled scores, so that
+    // its rounding is common to all weights and leaves with their sum.
+    const float mn = fmaxf(m, column_max(top) * unit), ms = mn == -INFINITY ? 0.f : mn;
     if (__any(mn > m)) {
       const float keep = __builtin_amdgcn_exp2f(m - ms);
       l *= keep;
@@ -250,7 +253,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
     }
 #pragma unroll
     for (int j = 0; j < SP; ++j) {
-      sc[j] = __builtin_amdgcn_exp2f(sc[j] - ms);
+      sc[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j], unit, -ms));
       l += sc[j];
     }
     if constexpr (sizeof(T) == 4) {
