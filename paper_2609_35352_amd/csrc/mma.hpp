@@ -110,10 +110,6 @@ __device__ __forceinline__ u4 first_mask(int valid) {
 // 32-bit values for a contraction with rows of T: in 16 bits as the sum of two
 // bfloat16 parts (an error of 2^-16 of the value, and its whole range; one part
 // would lose 2^-8, binary16 its range as well).
-template <typename T, int KF>
-struct Wide {
-  u4 hi[KF], lo[sizeof(T) == 2 ? KF : 1];
-};
 __device__ __forceinline__ uint32_t split_pair(float a, float b, uint32_t &lo) {
   typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
   const bf2 h = {(__bf16)a, (__bf16)b};
