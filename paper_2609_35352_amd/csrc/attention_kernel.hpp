@@ -122,9 +122,11 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
   // Loads are issued without branches, so that the waits between them are for
   // the data that is used next: a token that does not count is read from its
   // page all the same, or from page 0 where the table has none.
-  // The page and place of token `tok`, which lies in the table up to `end`.
+  // The page and place of token `tok`, or past `end` of the last one before it
+  // (SPAN: of the last span's first, as a whole span is read from there on).
+  const int32_t last = SPAN ? (end - 1) / SP * SP : end - 1;
   auto locate = [&](int32_t tok, int32_t &page, uint32_t &place) {
-    tok = tok < end ? tok : end - 1;
+    tok = tok < last ? tok : last;
     const uint32_t p = page_of(P, (uint32_t)tok);
     page = table[p];
     place = (uint32_t)tok - p * P.page_size;
