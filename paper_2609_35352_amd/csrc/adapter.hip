@@ -25,8 +25,9 @@ struct fiona_adapters {
   int32_t *ids = nullptr;
 };
 
-// Rows below kMinWidth elements, too short for 16-byte pieces: one value per
-// wavefront or thread.
+// Rows below kMinWidth elements can be shorter than a lane's 16 bytes, which the
+// tiled kernels may always read: one value per wavefront or thread, bound by
+// latency (for what is this narrow, no more than the launches: 3 or 4).
 constexpr uint32_t kMinWidth = 8;
 
 namespace fiona {
@@ -138,18 +139,22 @@ bool narrow(const fiona_adapters_desc &D) { return D.d_in < kMinWidth || D.d_out
 
 uint32_t blocks_of(uint64_t n) { return (uint32_t)((n + fiona::kRows - 1) / fiona::kRows); }
 
-// Workgroups that share the adapters among 64 tokens: many where there are few
-// tokens, as each may have its own; two in any case, for the blocks in which
-// one request ends and the next begins (8192 tokens of 12 requests, shrink and
-// expand: 16 and 26 us with two, 19 and 33 with one).
+// Workgroups that share the adapters among 64 tokens: 256 over the blocks, as
+// with few tokens each may have its own; two at least, for the blocks in which
+// one request ends and the next begins.  Calls of 4096 x 4096 at rank 16, us, with
+// 128 / 256 / 512 over the blocks: 8192 tokens of 12 requests 51.2 / 46.0 / 59.3, of
+// 400 118 / 81 / 99; 16384 of 30 131 with one at least, 117 with two.
 uint32_t slots_of(uint32_t n, uint32_t adapters) {
   const uint32_t want = std::max(2u, 256 / blocks_of(n));
   return std::min({want, adapters, std::min(n, fiona::kRows)});
 }
 
-constexpr uint32_t kMaxSplits = 8, kWorkgroups = 512, kGradWorkgroups = 512;
-
-// Parts of a row's contraction: enough workgroups to fill the GPU.
+// Parts of a row's contraction: enough workgroups to fill the GPU, and not so
+// many that adding them up costs more (us with 256 / 512 / 1024 workgroups: 8192
+// tokens of 4096, rank 16, 48.2 / 46.0 / 49.5; 613 of 1000, 20, 23.5 / 22.2 / 22.3;
+// a training step of 8192 of 4096, 64, 170.9 / 158.1 / 159.4; with at most 1 / 2 /
+// 4 / 8 parts: 16 of 4096 21.3 / 15.7 / 12.6 / 11.6).
+constexpr uint32_t kMaxSplits = 8, kWorkgroups = 512;
 uint32_t splits_of(uint32_t n, uint32_t adapters) {
   const uint32_t slots = slots_of(n, adapters), wgs = blocks_of(n) * (slots > 2 ? slots : 1);
   return std::max(1u, std::min(kMaxSplits, (kWorkgroups + wgs - 1) / wgs));
@@ -160,7 +165,10 @@ uint32_t grad_slices(uint32_t n, uint32_t type, uint32_t RP) {
   return (n + cols - 1) / cols;
 }
 
-// Parts of the tokens in the gradients' sums, where their columns alone do not fill the GPU.
+// Parts of the tokens in the gradients' sums, where their columns alone do not
+// fill the GPU (us with 256 / 512 / 1024 workgroups: 2048 tokens of 768, rank 8,
+// 41.7 / 41.6 / 42.5; 8192 of 4096, 64, 158.2 / 158.1 / 176.6).
+constexpr uint32_t kGradWorkgroups = 512;
 uint32_t grad_splits_of(const fiona_adapters_desc &D, uint32_t RP, uint32_t n) {
   const uint64_t wgs = (uint64_t)(grad_slices(D.d_in, D.type, RP) + grad_slices(D.d_out, D.type, RP)) * D.n_adapter * ((RP + 63) / 64);
   const uint64_t want = (kGradWorkgroups + wgs - 1) / wgs;
@@ -193,10 +201,9 @@ template <typename T>
 void launch_expand(const fiona_adapters *H, fiona::ExpandParams P, hipStream_t stream) {
   const uint32_t n = P.I.n_tok, steps = (P.O + 255) / 256;
   P.slots = slots_of(n, P.I.n_adapter + 1);
-  // (512 / 1024 / 2048 workgroups, us of the whole call: 8192 tokens of 4096, rank 16, 42.7 / 49.0 / 53.0;
-  // a training step at rank 64 217.8 / 209.9 / 209.9)
-  const uint32_t wgs = blocks_of(n), want = H->RP <= 32 ? 512 : 1024;
-  const uint32_t slices = std::max(1u, std::min(steps, (want + wgs - 1) / wgs));
+  // (512 / 1024 / 2048 workgroups, us of the whole call: 8192 tokens of 4096, rank 16, 46.0 / 47.4 / 50.7;
+  // a training step at rank 64 158.5 / 158.0 / 163.4)
+  const uint32_t wgs = blocks_of(n), slices = std::max(1u, std::min(steps, (kWorkgroups + wgs - 1) / wgs));
   P.slice = (steps + slices - 1) / slices * 256;
   with_tiles(H->RP, [&](auto rt) {
     hipLaunchKernelGGL((fiona::expand_kernel<T, decltype(rt)::value>), dim3((P.O + P.slice - 1) / P.slice, blocks_of(n), P.slots),
