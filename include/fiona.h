@@ -563,6 +563,9 @@ int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cach
  * projection); dA and dB are overwritten whole, with zeros for adapters no
  * token has and from an adapter's rank on.  The gradient of base is dy.
  * Sums run in a fixed order: the same call gives the same bits.
+ * Rows of other tokens never reach a token's outputs, whatever they hold; a
+ * token's own infinities reach them (and its adapter's gradients) as infinities
+ * or NaN.
  *
  * Both: asynchronous on stream, kernel launches only, allocate nothing.  The
  * workspace is shared by the handle's calls: one handle must not be used by

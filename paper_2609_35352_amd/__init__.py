@@ -503,8 +503,10 @@ def _stream_of(stream, dev: int) -> int:
 
 
 def _type_code(dtype) -> int:
-    _lm_lib()
     code = _DTYPES.get(dtype)
+    if code is None:
+        _lm_lib()
+        code = _DTYPES.get(dtype)
     if code is None:
         raise ValueError("%s is not float32, float16 or bfloat16" % (dtype,))
     return code
@@ -554,7 +556,7 @@ def kv_append(k, v, slots, k_cache, v_cache, positions=None, cos=None, sin=None,
     [n_tok]; outside the cache: not written), keys rotated at positions (int32 [n_tok]) with cos, sin float32
     [n_pos][rot_dim / 2], and q [n_tok][n_head][d] rotated into q_out (the caches' type)."""
     cache, dtype, dev, n_kv, d = _cache_desc(k_cache, v_cache)
-    n, rows = len(k), k.dtype
+    n, rows = k.shape[0], k.dtype
     code = _type_code(rows)
     ks, vs = _rows(k, "k", rows, (n, n_kv, d), dev), _rows(v, "v", rows, (n, n_kv, d), dev)
     at = _packed(slots, "slots", _INT[8], (n,), dev)
@@ -617,7 +619,7 @@ def paged_attention(att: Attention, q, k_cache, v_cache, page_table, lengths, ou
     [n_seq][table_width], lengths int32 [n_seq] -> out [n_seq][n_head][d] and lse float32 [n_seq][n_head].
     scale: default head_dim ** -0.5."""
     cache, _, dev, _, _ = _cache_desc(k_cache, v_cache)
-    n = len(q)
+    n = q.shape[0]
     shape = (n, att.n_head, att.head_dim)
     qs, os_ = _rows(q, "q", att.dtype, shape, dev), _rows(out, "out", att.dtype, shape, dev)
     width = page_table.shape[-1]
@@ -663,7 +665,7 @@ class Adapters:
 
 def _adapter_args(ad: Adapters, x, ids, A, B, ranks, scaling):
     """(the shared fields' values, n_tok, device)"""
-    n, dev, dt = len(x), x.get_device(), ad.dtype
+    n, dev, dt = x.shape[0], x.get_device(), ad.dtype
     xs = _rows(x, "x", dt, (n, ad.d_in), dev)
     return (n, x.data_ptr(), _packed(A, "A", dt, (ad.n_adapter, ad.max_rank, ad.d_in), dev),
             _packed(B, "B", dt, (ad.n_adapter, ad.d_out, ad.max_rank), dev), _packed(ids, "ids", _INT[4], (n,), dev),
