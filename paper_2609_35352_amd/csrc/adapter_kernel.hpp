@@ -599,7 +599,9 @@ __global__ void __launch_bounds__(256) grad_kernel(GradParams P) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) r.x[j][i] = v[i];
       } else {
-        const u2 v = *(const u2_any *)p;
+        // (the rows' last reading; past the caches a training step of 8192 tokens took 150.6 us instead
+        // of 154.2 at rank 64, 124.3 for 130.5 at 20; the wider pieces of small ranks gained nothing)
+        const u2 v = __builtin_nontemporal_load((const u2_any *)p);
         r.x[j][0] = v[0], r.x[j][1] = v[1];
       }
     }
