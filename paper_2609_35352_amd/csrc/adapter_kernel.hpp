@@ -150,6 +150,103 @@ __global__ void __launch_bounds__(256) shrink_kernel(ShrinkParams P) {
 }
 
 // ---------------------------------------------------------------------------
+// inner: parts of h and g summed and scaled, as columns of tokens for the
+// gradients, in two bfloat16 parts for 16-bit types; with a launch of its own g
+// whole as well, for expand.  8192 tokens of rank 64, four parts (23 MB): 7.4 us,
+// latency of ids, ranks and parts in turn.
+// ---------------------------------------------------------------------------
+// Tokens of one step of the gradients: a fragment's.
+template <typename T>
+constexpr uint32_t kGradTokens = sizeof(T) == 2 ? 32 : 16;
+// The lane's 16 bytes of the fragment of a step's tokens and 16 ranks: ranks by
+// lane % 16, tokens by lane / 16; bfloat16 has a second fragment for the rest.
+template <typename T>
+__device__ __forceinline__ char *column_at(const void *column, uint32_t RP, uint64_t step, uint32_t tile, uint32_t part, uint32_t lane) {
+  return (char *)column + (((step * (RP / 16) + tile) * (sizeof(T) == 2 ? 2 : 1) + part) * 64 + lane) * 16;
+}
+
+struct InnerParams {
+  AdapterIds I;
+  const float *part[2], *scaling;   // of h, of g
+  float *g;                         // [n_tok][RP], or null
+  int32_t *ids;                     // [n_pad]: the tokens' adapters, -1 for none
+  void *column[2];                  // h and g as fragments of the gradients' steps (see column_at)
+  uint32_t RP, n_pad, splits;
+};
+// 64 tokens from row0 and 32 ranks from r0 on of h (side 0) or g.
+template <typename T>
+__device__ __forceinline__ void inner_tile(const InnerParams &P, uint32_t side, uint32_t row0, uint32_t r0, float (*tile)[65]) {
+  if (side == 0 && r0 == 0 && threadIdx.x < 64) {
+    const uint32_t t = row0 + threadIdx.x;
+    const int32_t a = t < P.I.n_tok ? P.I.ids[t] : -1;
+    P.ids[t] = adapter_rank(P.I, a) ? a : -1;
+  }
+  // A thread takes one rank of eight tokens; their ids, ranks and parts are each
+  // asked for together, without branches.
+  constexpr uint32_t M = 8;
+  const uint32_t q = threadIdx.x / 32, r = r0 + threadIdx.x % 32, rc = r < P.RP ? r : P.RP - 1;
+  uint32_t a[M], at[M];
+  bool live[M];
+  float x[M];
+#pragma unroll
+  for (uint32_t i = 0; i < M; ++i) {
+    const uint32_t t = row0 + q + 8 * i;
+    at[i] = t < P.I.n_tok ? t : P.I.n_tok - 1;
+    const int32_t id = P.I.ids[at[i]];
+    live[i] = (int)(t < P.I.n_tok) & (int)((uint32_t)id < P.I.n_adapter);
+    a[i] = live[i] ? (uint32_t)id : 0;
+    x[i] = 0;
+  }
+  if (P.I.ranks) {
+#pragma unroll
+    for (uint32_t i = 0; i < M; ++i) live[i] &= P.I.ranks[a[i]] > 0;
+  }
+#pragma unroll 2
+  for (uint32_t s = 0; s < P.splits; ++s)
+#pragma unroll
+    for (uint32_t i = 0; i < M; ++i) x[i] += P.part[side][((uint64_t)s * P.I.n_tok + at[i]) * P.RP + rc];
+  if (P.scaling) {
+#pragma unroll
+    for (uint32_t i = 0; i < M; ++i) x[i] *= P.scaling[a[i]];
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < M; ++i) {
+    if (!live[i] || r >= P.RP) x[i] = 0;   // (nothing is written there)
+    if (side == 1 && P.g && r < P.RP && row0 + q + 8 * i < P.I.n_tok) P.g[(uint64_t)at[i] * P.RP + r] = x[i];
+    tile[threadIdx.x % 32][q + 8 * i] = x[i];
+  }
+  __syncthreads();
+  if constexpr (sizeof(T) == 4) {   // 4 steps of 16 tokens, 2 tiles of 16 ranks, 64 lanes of 4 tokens
+    for (uint32_t e = threadIdx.x; e < 512; e += 256) {
+      const uint32_t lane = e % 64, j = e / 64 % 2, step = e / 128, t = 16 * step + lane / 16 * 4;
+      if (r0 + 16 * j >= P.RP) continue;
+      f4 x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = tile[16 * j + lane % 16][t + i];
+      *(f4 *)column_at<T>(P.column[side], P.RP, row0 / 16 + step, r0 / 16 + j, 0, lane) = x;
+    }
+  } else {                          // 2 steps of 32 tokens, 2 tiles of 16 ranks, 64 lanes of 8 tokens
+    const uint32_t lane = threadIdx.x % 64, j = threadIdx.x / 64 % 2, step = threadIdx.x / 128, t = 32 * step + lane / 16 * 8;
+    if (r0 + 16 * j >= P.RP) return;
+    u4 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t l;
+      hi[i] = split_pair(tile[16 * j + lane % 16][t + 2 * i], tile[16 * j + lane % 16][t + 2 * i + 1], l);
+      lo[i] = l;
+    }
+    *(u4 *)column_at<T>(P.column[side], P.RP, row0 / 32 + step, r0 / 16 + j, 0, lane) = hi;
+    *(u4 *)column_at<T>(P.column[side], P.RP, row0 / 32 + step, r0 / 16 + j, 1, lane) = lo;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) inner_kernel(InnerParams P) {
+  __shared__ float tile[32][65];
+  inner_tile<T>(P, blockIdx.z, blockIdx.x * 64, blockIdx.y * 32, tile);
+}
+
+// ---------------------------------------------------------------------------
 // expand: out_t[o] = base_t[o] + c_a sum_r w_a[o][r] h_t[r],  h = sum of parts
 // ---------------------------------------------------------------------------
 struct ExpandParams {
@@ -159,6 +256,8 @@ struct ExpandParams {
   void *out;
   uint64_t base_row, out_row;
   uint32_t O, w_cols, splits, slots, slice;   // slice: columns of a workgroup, a multiple of 256
+  uint32_t inner_z;              // INNER: of the grid's z, the first ones for inner
+  InnerParams inner;
 };
 
 // The workgroup first adds up its tokens' parts of h and keeps them in LDS as
@@ -169,7 +268,8 @@ struct ExpandParams {
 // 8192 tokens of 4096 in bfloat16 with a base (134 MB), 31 us at rank 16 (4.3 TB/s;
 // a copy takes 26), 40 at rank 64, where eight times the products pass through LDS.
 // For few tokens, by its chain of loads (ids, ranks, parts, factor): 6.3 us for 16.
-template <typename T, int RT>
+// INNER: the launch's first workgroups are inner's.
+template <typename T, int RT, bool INNER>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 && RT <= 2 ? 3 : (sizeof(T) == 2 ? RT <= 4 : RT <= 2) ? 2 : 1) expand_kernel(ExpandParams P) {
   constexpr uint32_t E = kLaneElems<T>, FK = kFragElems<T>, RP = 16 * RT;
   constexpr int KF = (RP + FK - 1) / FK, PARTS = sizeof(T) == 2 ? 2 : 1;
@@ -179,9 +279,19 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && RT <= 2 ? 3 : (sizeof(T
   __shared__ alignas(16) uint8_t sh[kRows][PARTS * HB + 16];
   const uint32_t lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, grp = lane >> 4;
   const uint32_t row0 = blockIdx.y * kRows, tr = lane / LP, pc = lane % LP;
+  uint32_t slot = blockIdx.z;
+  if constexpr (INNER) {
+    if (slot < P.inner_z) {
+      const uint32_t i = slot * gridDim.x + blockIdx.x;
+      static_assert(sizeof(so) >= sizeof(float[32][65]), "inner's tile");
+      if (i / 2 * 32 < P.inner.RP) inner_tile<T>(P.inner, i % 2, row0, i / 2 * 32, (float(*)[65])so);
+      return;
+    }
+    slot -= P.inner_z;
+  }
   const uint32_t end = blockIdx.x * P.slice + P.slice < P.O ? blockIdx.x * P.slice + P.slice : P.O;
   const uint32_t here = P.I.n_tok - row0 < kRows ? P.I.n_tok - row0 : kRows;   // tokens of this workgroup
-  for_adapters(P.I, row0, lane, blockIdx.z, P.slots, true, [&](int32_t a, uint32_t rank, uint64_t rows, uint32_t lead) {
+  for_adapters(P.I, row0, lane, slot, P.slots, true, [&](int32_t a, uint32_t rank, uint64_t rows, uint32_t lead) {
     if (rank == 0 && P.base == P.out) return;
     u4 mask[KF];
     // The adapter's factor and the elements from there to the table's end (rows
@@ -421,98 +531,6 @@ __global__ void __launch_bounds__(256) transpose_kernel(TransposeParams P) {
 }
 
 // ---------------------------------------------------------------------------
-// inner: parts of h and g summed and scaled; g as rows for dx, both as columns
-// of tokens for the gradients, in two bfloat16 parts for 16-bit types.  8192 tokens
-// of rank 64, four parts (23 MB): 7.4 us, latency of ids, ranks and parts in turn
-// (10.6 with a branch at each).
-// ---------------------------------------------------------------------------
-// Tokens of one step of the gradients: a fragment's.
-template <typename T>
-constexpr uint32_t kGradTokens = sizeof(T) == 2 ? 32 : 16;
-// The lane's 16 bytes of the fragment of a step's tokens and 16 ranks: ranks by
-// lane % 16, tokens by lane / 16; bfloat16 has a second fragment for the rest.
-template <typename T>
-__device__ __forceinline__ char *column_at(const void *column, uint32_t RP, uint64_t step, uint32_t tile, uint32_t part, uint32_t lane) {
-  return (char *)column + (((step * (RP / 16) + tile) * (sizeof(T) == 2 ? 2 : 1) + part) * 64 + lane) * 16;
-}
-
-struct InnerParams {
-  AdapterIds I;
-  const float *part[2], *scaling;   // of h, of g
-  float *g;                         // [n_tok][RP]
-  int32_t *ids;                     // [n_pad]: the tokens' adapters, -1 for none
-  void *column[2];                  // h and g as fragments of the gradients' steps (see column_at)
-  uint32_t RP, n_pad, splits;
-};
-template <typename T>
-__global__ void __launch_bounds__(256) inner_kernel(InnerParams P) {
-  __shared__ float tile[32][65];
-  const uint32_t side = blockIdx.z, row0 = blockIdx.x * 64, r0 = blockIdx.y * 32;
-  if (side == 0 && r0 == 0 && threadIdx.x < 64) {
-    const uint32_t t = row0 + threadIdx.x;
-    const int32_t a = t < P.I.n_tok ? P.I.ids[t] : -1;
-    P.ids[t] = adapter_rank(P.I, a) ? a : -1;
-  }
-  // A thread takes one rank of eight tokens; their ids, ranks and parts are each
-  // asked for together, without branches.
-  constexpr uint32_t M = 8;
-  const uint32_t q = threadIdx.x / 32, r = r0 + threadIdx.x % 32, rc = r < P.RP ? r : P.RP - 1;
-  uint32_t a[M], at[M];
-  bool live[M];
-  float x[M];
-#pragma unroll
-  for (uint32_t i = 0; i < M; ++i) {
-    const uint32_t t = row0 + q + 8 * i;
-    at[i] = t < P.I.n_tok ? t : P.I.n_tok - 1;
-    const int32_t id = P.I.ids[at[i]];
-    live[i] = (int)(t < P.I.n_tok) & (int)((uint32_t)id < P.I.n_adapter);
-    a[i] = live[i] ? (uint32_t)id : 0;
-    x[i] = 0;
-  }
-  if (P.I.ranks) {
-#pragma unroll
-    for (uint32_t i = 0; i < M; ++i) live[i] &= P.I.ranks[a[i]] > 0;
-  }
-#pragma unroll 2
-  for (uint32_t s = 0; s < P.splits; ++s)
-#pragma unroll
-    for (uint32_t i = 0; i < M; ++i) x[i] += P.part[side][((uint64_t)s * P.I.n_tok + at[i]) * P.RP + rc];
-  if (P.scaling) {
-#pragma unroll
-    for (uint32_t i = 0; i < M; ++i) x[i] *= P.scaling[a[i]];
-  }
-#pragma unroll
-  for (uint32_t i = 0; i < M; ++i) {
-    if (!live[i] || r >= P.RP) x[i] = 0;   // (nothing is written there)
-    if (side == 1 && r < P.RP && row0 + q + 8 * i < P.I.n_tok) P.g[(uint64_t)at[i] * P.RP + r] = x[i];
-    tile[threadIdx.x % 32][q + 8 * i] = x[i];
-  }
-  __syncthreads();
-  if constexpr (sizeof(T) == 4) {   // 4 steps of 16 tokens, 2 tiles of 16 ranks, 64 lanes of 4 tokens
-    for (uint32_t e = threadIdx.x; e < 512; e += 256) {
-      const uint32_t lane = e % 64, j = e / 64 % 2, step = e / 128, t = 16 * step + lane / 16 * 4;
-      if (r0 + 16 * j >= P.RP) continue;
-      f4 x;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = tile[16 * j + lane % 16][t + i];
-      *(f4 *)column_at<T>(P.column[side], P.RP, row0 / 16 + step, r0 / 16 + j, 0, lane) = x;
-    }
-  } else {                          // 2 steps of 32 tokens, 2 tiles of 16 ranks, 64 lanes of 8 tokens
-    const uint32_t lane = threadIdx.x % 64, j = threadIdx.x / 64 % 2, step = threadIdx.x / 128, t = 32 * step + lane / 16 * 8;
-    if (r0 + 16 * j >= P.RP) return;
-    u4 hi, lo;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t l;
-      hi[i] = split_pair(tile[16 * j + lane % 16][t + 2 * i], tile[16 * j + lane % 16][t + 2 * i + 1], l);
-      lo[i] = l;
-    }
-    *(u4 *)column_at<T>(P.column[side], P.RP, row0 / 32 + step, r0 / 16 + j, 0, lane) = hi;
-    *(u4 *)column_at<T>(P.column[side], P.RP, row0 / 32 + step, r0 / 16 + j, 1, lane) = lo;
-  }
-}
-
-// ---------------------------------------------------------------------------
 // grad: dA_a[r] = sum_t g_t[r] x_t and dB_a[.][r] = sum_t c h_t[r] dy_t
 // ---------------------------------------------------------------------------
 struct GradSide {
@@ -525,7 +543,7 @@ struct GradSide {
 struct GradParams {
   AdapterIds I;
   GradSide side[2];
-  const int32_t *ids;        // [n_pad], -1 for tokens without an adapter and past the last (inner_kernel)
+  const int32_t *ids;        // [n_pad], -1 for tokens without an adapter and past the last (inner_tile)
   uint32_t RP, n_pad, splits, per_split, r_chunks;   // per_split: tokens, a multiple of 64
 };
 // Columns of a lane and of a workgroup: 16 bytes of 16 lanes, or 8 from 32 ranks
