@@ -88,7 +88,7 @@ __device__ __forceinline__ void store8(C *p, const float (&x)[8]) {
 // and written once: what bounds it is memory (16384 tokens of 32 + 8 + 8 heads of
 // 128 in bfloat16, 411 MB: 69 us, 6.0 TB/s; stores that pass the caches by reach
 // more than a plain copy's 5.1), or for a few tokens the launch (8 of 12 + 12 + 12
-// heads of 64: 3.5 us on the GPU, 9.7 a call).
+// heads of 64: 3.5 us on the GPU, 9.4 a call).
 template <typename T, typename C>
 __global__ void __launch_bounds__(256) append_kernel(AppendParams P) {
   const uint32_t units = (P.d + 15) / 16, items = (P.n_head + 2 * P.n_kv) * units;
