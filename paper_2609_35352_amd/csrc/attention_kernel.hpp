@@ -4,7 +4,9 @@
 //     m_J = max s_j,  l_J = sum exp(s_j - m_J),  o_J = sum exp(s_j - m_J) v_j,
 // and two parts join as m = max(m_1, m_2), l = sum_i l_i exp(m_i - m), o alike;
 // so every key and value is read once, by whichever wavefront holds its part.
-// Exponentials are to base 2, with log2(e) in the scale.
+// Exponentials are to base 2, with log2(e) in the scale, and of the difference of
+// two scores, taken before it is scaled: never above zero, whatever the scores' size
+// (a scaled maximum of 2^33, rounded, is off by up to 2^9 powers of two).
 //
 // A workgroup takes one chunk of one sequence's keys for one key head and up
 // to 16 of the query heads that share it; its four wavefronts take tiles of
@@ -52,7 +54,7 @@ struct AttendParams {
   uint32_t n_head, group, head_blocks, d, page_size, n_pages, window, max_length;
   uint32_t page_mul, page_shift;                // token / page_size (see page_of)
   uint32_t chunk, splits;
-  float scale;                                  // of a score, times log2(e)
+  float unit;                                   // of a product q k in powers of two, scale log2(e); 1 with a softcap
   float cap_in, cap_out;                        // 2 log2(e) scale / softcap, softcap log2(e); 0 without one
 };
 
@@ -123,7 +125,6 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
 #pragma unroll
   for (int t = 0; t < OT; ++t) o[t] = (f4){0, 0, 0, 0};
   float m = -INFINITY, l = 0;
-  const float unit = P.cap_out > 0 ? 1.f : P.scale;   // of a score, in powers of two
   const int32_t *table = P.table + seq * P.table_stride;
   const T *kb = (const T *)P.kc + kv * P.k_head, *vb = (const T *)P.vc + kv * P.v_head;
 
@@ -251,11 +252,9 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
 #pragma unroll
     for (int j = 1; j < SP; ++j) top = fmaxf(top, sc[j]);
 
-    // The maximum is rounded once and taken from the exact scaled scores, so that
-    // its rounding is common to all weights and leaves with their sum.
-    const float mn = fmaxf(m, column_max(top) * unit), ms = mn == -INFINITY ? 0.f : mn;
+    const float mn = fmaxf(m, column_max(top)), ms = mn == -INFINITY ? 0.f : mn;
     if (__any(mn > m)) {
-      const float keep = __builtin_amdgcn_exp2f(m - ms);
+      const float keep = __builtin_amdgcn_exp2f((m - ms) * P.unit);
       l *= keep;
 #pragma unroll
       for (int t = 0; t < OT; ++t) o[t] *= keep;
@@ -263,7 +262,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
     }
 #pragma unroll
     for (int j = 0; j < SP; ++j) {
-      sc[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j], unit, -ms));
+      sc[j] = __builtin_amdgcn_exp2f((sc[j] - ms) * P.unit);
       l += sc[j];
     }
     if constexpr (sizeof(T) == 4) {
@@ -313,7 +312,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
     const float ms = mt == -INFINITY ? 0.f : mt;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      f[i] = __builtin_amdgcn_exp2f(sm[i][oh] - ms);
+      f[i] = __builtin_amdgcn_exp2f((sm[i][oh] - ms) * P.unit);
       lt += sl[i][oh] * f[i];
     }
     if (oh >= heads) continue;
@@ -333,7 +332,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
     }
     if (oc == 0 && c0 == 0) {
       if (P.splits > 1) P.part_ml[2 * at] = mt, P.part_ml[2 * at + 1] = lt;
-      else if (P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms + __builtin_amdgcn_logf(lt));
+      else if (P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms * P.unit + __builtin_amdgcn_logf(lt));
     }
   }
 }
@@ -358,7 +357,7 @@ __global__ void __launch_bounds__(256 * G) attend_join_kernel(AttendParams P) {
     if (t < used) m = P.part_ml[2 * (at + t)], l = P.part_ml[2 * (at + t) + 1];
     float top = m;
     for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-    const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
+    const float f = __builtin_amdgcn_exp2f((m - (top == -INFINITY ? 0.f : top)) * P.unit);
     sw[t] = f;
     l *= f;
     for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
@@ -381,7 +380,7 @@ __global__ void __launch_bounds__(256 * G) attend_join_kernel(AttendParams P) {
 #pragma unroll
   for (int i = 1; i < G; ++i) x += so[i][t];
   ((T *)P.out)[seq * P.out_seq + head * P.out_head + t] = (T)(lt == 0 ? 0.f : x / lt);
-  if (t == 0 && P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms + __builtin_amdgcn_logf(lt));
+  if (t == 0 && P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms * P.unit + __builtin_amdgcn_logf(lt));
 }
 
 }  // namespace fiona
