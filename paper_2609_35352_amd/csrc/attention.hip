@@ -140,7 +140,10 @@ int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cach
   P.n_head = D.n_head, P.group = D.n_head / D.n_kv, P.head_blocks = head_blocks(D), P.d = D.head_dim;
   P.page_size = D.page_size, P.n_pages = K.n_pages, P.window = A.window;
   P.unit = (float)std::min<double>((double)A.scale * fiona::kLog2e, FLT_MAX);
-  if (A.softcap > 0) P.unit = 1, P.cap_in = 2.f * fiona::kLog2e * A.scale / A.softcap, P.cap_out = A.softcap * fiona::kLog2e;
+  if (A.softcap > 0) {
+    P.unit = fiona::kLog2e, P.scale = A.scale, P.cap = A.softcap;
+    P.cap_in = (float)std::min<double>(2. * fiona::kLog2e * A.scale / A.softcap, FLT_MAX);
+  }
   page_divisor(D.page_size, P.page_mul, P.page_shift);
   P.max_length = (uint32_t)std::min<uint64_t>(D.max_length, (uint64_t)A.table_width * D.page_size);
   if (K.n_pages == 0) P.max_length = 0;

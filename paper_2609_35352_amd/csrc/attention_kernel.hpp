@@ -54,8 +54,8 @@ struct AttendParams {
   uint32_t n_head, group, head_blocks, d, page_size, n_pages, window, max_length;
   uint32_t page_mul, page_shift;                // token / page_size (see page_of)
   uint32_t chunk, splits;
-  float unit;                                   // of a product q k in powers of two, scale log2(e); 1 with a softcap
-  float cap_in, cap_out;                        // 2 log2(e) scale / softcap, softcap log2(e); 0 without one
+  float unit;                                   // of a product q k in powers of two, scale log2(e); log2(e) with a softcap
+  float scale, cap, cap_in;                     // with a softcap: scale, the cap (0 without) and 2 log2(e) scale / cap
 };
 
 // token / page_size for token < 2^31 (see page_divisor).
@@ -68,6 +68,19 @@ __device__ __forceinline__ void key_range(const AttendParams &P, uint32_t s, int
   n = P.lengths[s];
   n = n < 0 ? 0 : (uint32_t)n > P.max_length ? (int32_t)P.max_length : n;
   first = P.window && (uint32_t)n > P.window ? n - (int32_t)P.window : 0;
+}
+
+// cap tanh(s / cap), s = scale x, with an error relative to s whatever the cap:
+// y = 2 log2(e) s / cap; below |s / cap| = 1/2 tanh(r) = r + r y^2 p(y^2) (p: least
+// largest relative error there, 2^-26), above it 1 - 2 / (2^|y| + 1), where what is
+// taken from 1 is at most 0.54.
+__device__ __forceinline__ float capped(const AttendParams &P, float x) {
+  const float s = x * P.scale, y = x * P.cap_in, z = y * y;
+  float p = __builtin_fmaf(z, 3.5919381389248883e-06f, -9.193531150231138e-05f);
+  p = __builtin_fmaf(z, p, 0.0019225659780204296f);
+  p = __builtin_fmaf(z, p, -0.040037527680397034f);
+  const float t = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(__builtin_fabsf(y)) + 1.f);
+  return __builtin_fabsf(y) < kLog2e ? __builtin_fmaf(s * z, p, s) : __builtin_copysignf(P.cap * t, y);
 }
 
 template <typename T>
@@ -230,10 +243,9 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
     }
 
     float sc[SP];
-    if (P.cap_out > 0) {
+    if (P.cap > 0) {
 #pragma unroll
-      for (int j = 0; j < SP; ++j)   // cap tanh(s / cap) = cap (1 - 2 / (exp(2 s / cap) + 1)), in units of log2(e)
-        sc[j] = P.cap_out * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(P.cap_in * acc[j / 4][j % 4]) + 1.f));
+      for (int j = 0; j < SP; ++j) sc[j] = capped(P, acc[j / 4][j % 4]);
     } else {
 #pragma unroll
       for (int j = 0; j < SP; ++j) sc[j] = acc[j / 4][j % 4];
