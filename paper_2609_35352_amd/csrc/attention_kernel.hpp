@@ -21,8 +21,12 @@
 // words in registers.  Key `row` of S^T's tile s stands for token (row / 4) *
 // kSpan + 4 s + row % 4 of the tile, so that the kSpan tokens whose weights a
 // lane ends up with are consecutive, and are the tokens whose rows it loads.
-// Softmax weights are rounded to the values' type (at most 1, so an error of at
-// most half a unit of the sum); their sum l uses them unrounded.
+// Softmax weights are rounded to the values' type, each by at most half a unit of
+// itself; their sum l uses them unrounded.  binary16, whose normal numbers end at
+// 2^-14, takes them times 2^15, so that this holds down to 2^-29 of the largest, and
+// below it to within 2^-40 of the largest (a key that outweighs the rest by 2^25 may
+// hold no value); l and o carry that factor to the end, where it leaves with their
+// quotient.
 //
 // What bounds it: the cache is read once, and 2 or 4 operations per byte and
 // query head are far below the matrix cores' rate.  Two sequences of 100000 and
@@ -89,6 +93,8 @@ template <typename T>
 constexpr int32_t kTiles = kTileKeys<T> / 16;     // score tiles of 16 keys
 template <typename T>
 constexpr int32_t kSpan = 4 * kTiles<T>;          // consecutive tokens of a lane
+template <typename T>
+constexpr float kShift = __is_same(T, _Float16) ? 15.f : 0.f;   // of the weights, in powers of two
 
 // D: head size rounded up.  VEC: rows in 16-byte pieces.  SPAN: pages are
 // multiples of kSpan tokens, so that a span lies in one page and takes one look
@@ -274,7 +280,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
     }
 #pragma unroll
     for (int j = 0; j < SP; ++j) {
-      sc[j] = __builtin_amdgcn_exp2f((sc[j] - ms) * P.unit);
+      sc[j] = __builtin_amdgcn_exp2f(kShift<T> > 0 ? __builtin_fmaf(sc[j] - ms, P.unit, kShift<T>) : (sc[j] - ms) * P.unit);
       l += sc[j];
     }
     if constexpr (sizeof(T) == 4) {
@@ -344,7 +350,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) attend_kernel(AttendPar
     }
     if (oc == 0 && c0 == 0) {
       if (P.splits > 1) P.part_ml[2 * at] = mt, P.part_ml[2 * at + 1] = lt;
-      else if (P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms * P.unit + __builtin_amdgcn_logf(lt));
+      else if (P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms * P.unit + (__builtin_amdgcn_logf(lt) - kShift<T>));
     }
   }
 }
@@ -392,7 +398,7 @@ __global__ void __launch_bounds__(256 * G) attend_join_kernel(AttendParams P) {
 #pragma unroll
   for (int i = 1; i < G; ++i) x += so[i][t];
   ((T *)P.out)[seq * P.out_seq + head * P.out_head + t] = (T)(lt == 0 ? 0.f : x / lt);
-  if (t == 0 && P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms * P.unit + __builtin_amdgcn_logf(lt));
+  if (t == 0 && P.lse) P.lse[(uint64_t)seq * P.n_head + head] = lt == 0 ? -INFINITY : kLn2 * (ms * P.unit + (__builtin_amdgcn_logf(lt) - kShift<T>));
 }
 
 }  // namespace fiona
