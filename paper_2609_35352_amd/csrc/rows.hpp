@@ -55,33 +55,48 @@ inline bool rows_distinct(const Rows &r) {
   return true;
 }
 
-// Whether two sets of rows may share a byte.  Where their ranges overlap they
-// are still apart if both step by the same largest stride and what they hold
-// of one step does not meet (queries, keys and values side by side in the
-// rows of one projection; keys and values side by side in one page).
+// Two sets of rows axis by axis, in bytes: axes from the largest step down, what a
+// whole set reaches, and how far b starts after a.  At the largest step the sets
+// split into copies of what is left; a copy of a and one of b whose steps differ by
+// i can meet only where their reaches do, for one or two i in sets that nest.
+struct Axis {
+  uint64_t step, n;
+};
+inline bool axes_meet(const Axis *a, int na, __int128 reach_a, const Axis *b, int nb, __int128 reach_b, __int128 delta) {
+  if (delta >= reach_a || -delta >= reach_b) return false;
+  if (!na && !nb) return true;
+  const __int128 s = std::max(na ? a->step : 0, nb ? b->step : 0);
+  const bool in_a = na && a->step == (uint64_t)s, in_b = nb && b->step == (uint64_t)s;
+  const __int128 most = in_a ? a->n - 1 : 0, least = in_b ? -(__int128)(b->n - 1) : 0;
+  reach_a -= most * s, reach_b += least * s;
+  // -reach_b < delta - i s < reach_a
+  auto floor_div = [&](__int128 x) { return x >= 0 ? x / s : -((-x + s - 1) / s); };
+  const __int128 first = std::max(least, floor_div(delta - reach_a) + 1), last = std::min(most, -floor_div(-delta - reach_b) - 1);
+  if (last - first > 3) return true;   // (rows over each other, or no common steps: taken to meet)
+  for (__int128 i = first; i <= last; ++i)
+    if (axes_meet(a + in_a, na - in_a, reach_a, b + in_b, nb - in_b, reach_b, delta - i * s)) return true;
+  return false;
+}
+
+// Whether two sets of rows may share a byte: exact where their steps nest (queries,
+// keys and values side by side in the rows of one projection; keys and values side by
+// side in a page, in a token or in a head), true in doubt.
 inline bool may_overlap(const Rows &a, const Rows &b) {
   if (empty(a) || empty(b)) return false;
   uint64_t ea, eb;
   if (!span(a, ea) || !span(b, eb)) return true;
-  const uint64_t a0 = (uint64_t)a.base, b0 = (uint64_t)b.base;
-  const uint64_t sa = ea * a.elem, sb = eb * b.elem;
-  if (a0 + sa <= b0 || b0 + sb <= a0) return false;
-  uint64_t step[2] = {0, 0}, window[2];
+  const __int128 delta = (__int128)(uint64_t)b.base - (__int128)(uint64_t)a.base;
+  const uint64_t bytes[2] = {ea * a.elem, eb * b.elem};
+  if (delta >= (__int128)bytes[0] || -delta >= (__int128)bytes[1]) return false;
+  Axis ax[2][3];
+  int n[2] = {0, 0};
   const Rows *rs[2] = {&a, &b};
-  const uint64_t bytes[2] = {sa, sb};
   for (int k = 0; k < 2; ++k) {
-    uint64_t count = 1;
     for (int i = 0; i < 3; ++i)
-      if (rs[k]->n[i] > 1 && rs[k]->stride[i] * rs[k]->elem > step[k]) {
-        step[k] = rs[k]->stride[i] * rs[k]->elem;
-        count = rs[k]->n[i];
-      }
-    window[k] = bytes[k] - (count - 1) * step[k];
+      if (rs[k]->n[i] > 1 && rs[k]->stride[i]) ax[k][n[k]++] = {rs[k]->stride[i] * rs[k]->elem, rs[k]->n[i]};
+    std::sort(ax[k], ax[k] + n[k], [](const Axis &x, const Axis &y) { return x.step > y.step; });
   }
-  if (step[0] != step[1] || step[0] == 0) return true;
-  const uint64_t s = step[0];
-  const uint64_t delta = b0 >= a0 ? (b0 - a0) % s : (s - (a0 - b0) % s) % s;
-  return !(delta >= window[0] && delta + window[1] <= s);
+  return axes_meet(ax[0], n[0], bytes[0], ax[1], n[1], bytes[1], delta);
 }
 
 // Whether every row starts at a multiple of 16 bytes.
