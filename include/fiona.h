@@ -465,8 +465,8 @@ typedef struct fiona_kv_cache {
  *               whose slot lies outside the cache is not written (padding: -1).
  *               Slots of one call are distinct, or which token is kept is unspecified
  *   positions   device, [n_tok], with rot_dim > 0
- *   cos, sin    device, [n_pos][rot_dim / 2]; a token whose position lies
- *               outside [0, n_pos) gets NaN in its rotated elements
+ *   cos, sin    device, [n_pos][rot_dim / 2] (not read with n_pos 0); a token whose
+ *               position lies outside [0, n_pos) gets NaN in its rotated elements
  * Asynchronous on stream; one kernel launch, allocates nothing.  Errors
  * (nothing is launched): FIONA_ERR_ARG, FIONA_ERR_UNSUPPORTED (a type or size
  * outside its range), FIONA_ERR_ALIGN, FIONA_ERR_ALIAS (an output overlaps an

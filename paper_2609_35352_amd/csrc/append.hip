@@ -182,7 +182,7 @@ extern "C" int fiona_kv_append(const fiona_kv_cache *cache, const fiona_append_a
   if (A.n_tok == 0) return FIONA_OK;
   if (!A.k || !A.v || !A.slots || (K.n_pages && (!K.k || !K.v))) return FIONA_ERR_ARG;
   if (A.n_head && (!A.q || !A.q_out)) return FIONA_ERR_ARG;
-  if (A.rot_dim && (!A.positions || !A.cos || !A.sin)) return FIONA_ERR_ARG;
+  if (A.rot_dim && (!A.positions || (A.n_pos && (!A.cos || !A.sin)))) return FIONA_ERR_ARG;
   const uint64_t es = type_size(A.rows_type), ec = type_size(K.type), d = K.head_dim;
   if (misaligned(A.k, es) || misaligned(A.v, es) || misaligned(K.k, ec) || misaligned(K.v, ec) ||
       misaligned(A.slots, 8) || (A.n_head && (misaligned(A.q, es) || misaligned(A.q_out, ec))) ||
@@ -225,11 +225,12 @@ extern "C" int fiona_kv_append(const fiona_kv_cache *cache, const fiona_append_a
   P.n_slot = (int64_t)K.n_pages * K.page_size;
   page_divisor(K.page_size, P.page_mul, P.page_shift);
   // 16-byte pieces where every row and its halves hold whole ones (1531 tokens of
-  // 25 heads of 80, 11.1 us, of 81 by elements 11.2; with 16384 of 48 6.0 and 1.9 TB/s).
+  // 25 heads of 80, 11.1 us, of 81 by elements 11.2; with 16384 of 48 6.0 and 1.9 TB/s),
+  // and the tables have a row, as a position outside them reads the first, unused.
   const bool pieces = d % 8 == 0 && P.half % 8 == 0 && rows_aligned16(in[0]) && rows_aligned16(in[1]) &&
                       rows_aligned16(out[0]) && rows_aligned16(out[1]) &&
                       (!A.n_head || (rows_aligned16(in[2]) && rows_aligned16(out[2]))) &&
-                      (!A.rot_dim || (rows_aligned16(in[5]) && rows_aligned16(in[6])));
+                      (!A.rot_dim || (A.n_pos && rows_aligned16(in[5]) && rows_aligned16(in[6])));
   const uint32_t items = (A.n_head + 2 * K.n_kv) * ((uint32_t)(d + 15) / 16);
   P.tokens = std::max(1u, 256 / items);
   const dim3 grid = pieces ? dim3((A.n_tok + P.tokens - 1) / P.tokens, (P.tokens * items + 255) / 256) : dim3(A.n_tok);
