@@ -511,8 +511,8 @@ void fiona_attention_destroy(fiona_attention *att);
  *   q, out      device, [n_seq][n_head][head_dim], of the handle's type
  *   lse         device, [n_seq][n_head] float32, or NULL
  *   page_table  device, [n_seq] rows of table_width entries, table_stride
- *               apart.  A key whose entry lies outside [0, n_pages) is left
- *               out, as if it were masked
+ *               apart (0: one row for all).  A key whose entry lies outside
+ *               [0, n_pages) is left out, as if it were masked
  *   lengths     device, [n_seq]; clamped to [0, min(max_length,
  *               table_width * page_size)]
  *   scale > 0; window 0: none; softcap 0: none, else > 0

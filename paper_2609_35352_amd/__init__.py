@@ -627,8 +627,7 @@ def paged_attention(att: Attention, q, k_cache, v_cache, page_table, lengths, ou
     lp = _packed(lse, "lse", _INT["f32"], (n, att.n_head), dev) if lse is not None else 0
     args = _ATTENTION_ARGS.pack(n, width, int(window), float(scale) if scale is not None else att.head_dim ** -0.5,
                                 float(softcap), q.data_ptr(), out.data_ptr(), lp, qs[0], qs[1], os_[0], os_[1],
-                                ts[0] if n > 1 else max(ts[0], width), page_table.data_ptr(),
-                                _packed(lengths, "lengths", _INT[4], (n,), dev))
+                                ts[0], page_table.data_ptr(), _packed(lengths, "lengths", _INT[4], (n,), dev))
     rc = lib().fiona_paged_attention(att.handle, cache, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_paged_attention")

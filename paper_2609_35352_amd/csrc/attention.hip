@@ -106,8 +106,7 @@ int fiona_paged_attention(const fiona_attention *att, const fiona_kv_cache *cach
     return FIONA_ERR_ARG;
   if ((uint64_t)K.n_pages * K.page_size >= (1u << 31)) return FIONA_ERR_UNSUPPORTED;
   if (A.n_seq == 0) return FIONA_OK;
-  if (!A.q || !A.out || !A.lengths || (A.table_width && !A.page_table) || A.table_stride < A.table_width ||
-      (K.n_pages && (!K.k || !K.v)))
+  if (!A.q || !A.out || !A.lengths || (A.table_width && !A.page_table) || (K.n_pages && (!K.k || !K.v)))
     return FIONA_ERR_ARG;
   const uint64_t e = type_size(D.type), d = D.head_dim, n = A.n_seq;
   if (misaligned(A.q, e) || misaligned(A.out, e) || misaligned(K.k, e) || misaligned(K.v, e) ||
