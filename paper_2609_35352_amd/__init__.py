@@ -458,8 +458,8 @@ def hybrid_linear_static(plan: Plan, in_t, pt_t, sign_t, scale_t, out_t, stream=
 #     adapter_linear(ad, x, ids, A, B, base, y)
 #     adapter_backward(ad, x, ids, A, B, dy, dx_base, dx, dA, dB)
 #
-# Tensors are float32, float16 or bfloat16 device tensors whose last axis is
-# contiguous; the other axes may have any stride.
+# Tensors are float32, float16 or bfloat16 tensors of the current device whose last
+# axis is contiguous; the other axes may have any stride.
 # ----------------------------------------------------------------------------
 
 # The header's structs, fields in order with native alignment; packed in one go, as a
@@ -472,7 +472,7 @@ _ADAPTERS_DESC = struct.Struct("@7I")
 _ADAPTER_ARGS = struct.Struct("@I6PQ2P2Q5P3Q")
 
 _DTYPES = {}   # torch dtype -> fiona_type
-_raw_stream = []
+_raw_stream, _device_now = [], []
 _INT = {}      # bytes -> torch dtype, and "f32"
 
 
@@ -490,15 +490,21 @@ def _lm_lib():
             getattr(L, name).restype, getattr(L, name).argtypes = None, [p]
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (without the stream object: 2 us a call)
         _raw_stream.append(raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream))
+        _device_now.append(getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device)
         _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
         _INT.update({4: torch.int32, 8: torch.int64, "f32": torch.float32})
     return L
 
 
 def _stream_of(stream, dev: int) -> int:
-    """The stream's handle; by default the current stream of the tensors' device."""
+    """The stream's handle; by default the current stream of the tensors' device, which has to be the current one:
+    that is where a launch goes, whatever its pointers are."""
+    if _device_now[0]() != dev:
+        raise ValueError("the tensors are on device %d, the current device is %d" % (dev, _device_now[0]()))
     if stream is None:
         return _raw_stream[0](dev)
+    if getattr(stream, "device_index", dev) != dev:
+        raise ValueError("the stream is on device %d, the tensors are on device %d" % (stream.device_index, dev))
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
