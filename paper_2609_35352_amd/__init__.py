@@ -459,7 +459,8 @@ def hybrid_linear_static(plan: Plan, in_t, pt_t, sign_t, scale_t, out_t, stream=
 #     adapter_backward(ad, x, ids, A, B, dy, dx_base, dx, dA, dB)
 #
 # Tensors are float32, float16 or bfloat16 tensors of the current device whose last
-# axis is contiguous; the other axes may have any stride.
+# axis is contiguous; the other axes may have any stride.  Nothing is recorded for
+# autograd: tensors that require a gradient are refused in grad mode.
 # ----------------------------------------------------------------------------
 
 # The header's structs, fields in order with native alignment; packed in one go, as a
@@ -519,6 +520,7 @@ def _type_code(dtype) -> int:
 
 
 def _refuse(t, name, dtype, shape, dev, packed=False):
+    """Raises for what is wrong with t; returns where nothing is, for a tensor with requires_grad outside grad mode."""
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
     if t.get_device() != dev:
@@ -527,20 +529,30 @@ def _refuse(t, name, dtype, shape, dev, packed=False):
         raise ValueError("%s must be %s, is %s" % (name, dtype, t.dtype))
     if t.shape != shape:
         raise ValueError("%s must have shape %s, has %s" % (name, tuple(shape), tuple(t.shape)))
-    raise ValueError("%s must be contiguous" % name if packed else "%s: its last axis must be contiguous" % name)
+    if packed and not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    if not packed and t.stride()[-1] != 1 and shape[-1] > 1:
+        raise ValueError("%s: its last axis must be contiguous" % name)
+    import torch
+
+    if torch.is_grad_enabled():
+        raise ValueError("%s requires a gradient, which this call does not record (torch.no_grad() or detach() where that "
+                         "is meant)" % name)
 
 
 def _rows(t, name, dtype, shape, dev):
     """The strides of a tensor whose last axis is contiguous, after checking type, shape and device."""
     st = t.stride()
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or dev < 0 or (st[-1] != 1 and shape[-1] > 1):
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or dev < 0 or (st[-1] != 1 and shape[-1] > 1) \
+            or t.requires_grad:
         _refuse(t, name, dtype, shape, dev)
     return st
 
 
 def _packed(t, name, dtype, shape, dev):
     """The address of a contiguous tensor, after the same checks."""
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or dev < 0 or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or dev < 0 or not t.is_contiguous() \
+            or t.requires_grad:
         _refuse(t, name, dtype, shape, dev, True)
     return t.data_ptr()
 
