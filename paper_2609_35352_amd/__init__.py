@@ -460,7 +460,8 @@ def hybrid_linear_static(plan: Plan, in_t, pt_t, sign_t, scale_t, out_t, stream=
 #
 # Tensors are float32, float16 or bfloat16 tensors of the current device whose last
 # axis is contiguous; the other axes may have any stride.  Nothing is recorded for
-# autograd: tensors that require a gradient are refused in grad mode.
+# autograd: tensors that require a gradient are refused in grad mode, and what a call
+# writes counts as modified in place.
 # ----------------------------------------------------------------------------
 
 # The header's structs, fields in order with native alignment; packed in one go, as a
@@ -473,7 +474,7 @@ _ADAPTERS_DESC = struct.Struct("@7I")
 _ADAPTER_ARGS = struct.Struct("@I6PQ2P2Q5P3Q")
 
 _DTYPES = {}   # torch dtype -> fiona_type
-_raw_stream, _device_now = [], []
+_raw_stream, _device_now, _modified = [], [], []
 _INT = {}      # bytes -> torch dtype, and "f32"
 
 
@@ -491,6 +492,7 @@ def _lm_lib():
             getattr(L, name).restype, getattr(L, name).argtypes = None, [p]
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (without the stream object: 2 us a call)
         _raw_stream.append(raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream))
+        _modified.append(torch.autograd.graph.increment_version)   # (a tensor or several)
         _device_now.append(getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device)
         _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
         _INT.update({4: torch.int32, 8: torch.int64, "f32": torch.float32})
@@ -601,6 +603,7 @@ def kv_append(k, v, slots, k_cache, v_cache, positions=None, cos=None, sin=None,
     rc = lib().fiona_kv_append(cache, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_kv_append")
+    _modified[0]((k_cache, v_cache) if q_out is None else (k_cache, v_cache, q_out))
 
 
 class Attention:
@@ -649,6 +652,7 @@ def paged_attention(att: Attention, q, k_cache, v_cache, page_table, lengths, ou
     rc = lib().fiona_paged_attention(att.handle, cache, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_paged_attention")
+    _modified[0](out if lse is None else (out, lse))
 
 
 class Adapters:
@@ -702,6 +706,7 @@ def adapter_linear(ad: Adapters, x, ids, A, B, base, y, ranks=None, scaling=None
     rc = lib().fiona_adapter_linear(ad.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_adapter_linear")
+    _modified[0](y)
 
 
 def adapter_backward(ad: Adapters, x, ids, A, B, dy, dx_base, dx, dA, dB, ranks=None, scaling=None, stream=None) -> None:
@@ -718,3 +723,4 @@ def adapter_backward(ad: Adapters, x, ids, A, B, dy, dx_base, dx, dA, dB, ranks=
     rc = lib().fiona_adapter_backward(ad.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_adapter_backward")
+    _modified[0]((dx, dA, dB))
