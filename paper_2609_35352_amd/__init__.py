@@ -18,6 +18,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
+import threading
 
 import numpy as np
 
@@ -66,12 +67,21 @@ class _Stats(ctypes.Structure):
 
 
 _lib = None
+_first_use = threading.RLock()
 
 
 def lib():
     """The loaded HIP library; raises if it has not been built."""
-    global _lib
     if _lib is None:
+        _load()
+    return _lib
+
+
+def _load():
+    global _lib
+    with _first_use:
+        if _lib is not None:
+            return
         if not os.path.exists(LIB_PATH):
             raise RuntimeError("libfiona.so is not built (run __graft_entry__.build()); "
                                "there is no fallback path")
@@ -95,7 +105,6 @@ def lib():
         L.fiona_status_string.restype = ctypes.c_char_p
         L.fiona_status_string.argtypes = [ctypes.c_int]
         _lib = L
-    return _lib
 
 
 def _check(rc: int, where: str):
@@ -480,7 +489,9 @@ _INT = {}      # bytes -> torch dtype, and "f32"
 
 def _lm_lib():
     L = lib()
-    if not _DTYPES:
+    if _DTYPES:
+        return L
+    with _first_use:
         import torch
 
         p = ctypes.c_void_p
@@ -494,8 +505,8 @@ def _lm_lib():
         _raw_stream.append(raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream))
         _modified.append(torch.autograd.graph.increment_version)   # (a tensor or several)
         _device_now.append(getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device)
-        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
         _INT.update({4: torch.int32, 8: torch.int64, "f32": torch.float32})
+        _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})   # (last: who finds a type finds all else)
     return L
 
 
