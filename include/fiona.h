@@ -426,7 +426,11 @@ int fiona_hoisted_rotate(const fiona_rotator *rotator, const uint64_t *ct, uint3
  *
  * Elements are IEEE binary32, binary16 or bfloat16.  Whatever the type, every
  * product is summed in 32 bits, softmax statistics are held in 32 bits, and a
- * result is rounded to its type once.  Strides count elements; the last axis
+ * result is rounded to its type once.  Two intermediate values are multiplied in
+ * fewer bits where the type has 16: fiona_paged_attention's softmax weights, in the
+ * type itself (half a unit of each weight; their sum is not rounded), and the
+ * adapters' h and g, as two bfloat16 parts (2^-16 of the value).  Every launch goes
+ * to the current device.  Strides count elements; the last axis
  * of every array is contiguous.  Device pointers need the alignment of their
  * elements; where pointers and strides are multiples of 16 bytes and rows are
  * multiples of 8 elements the kernels read and write 16 bytes per lane.
@@ -504,7 +508,8 @@ void fiona_attention_destroy(fiona_attention *att);
  * With n the sequence's length (the new token included), first = n - window
  * (0 without a window, or below it), and key j in page page_table[j / page_size]
  * at place j mod page_size,
- *     s_j = scale q . k_j,  or softcap tanh(s_j / softcap) with a softcap,
+ *     s_j = scale q . k_j,  or softcap tanh(s_j / softcap) with a softcap
+ *           (its error is relative to s_j, whatever the softcap),
  *     out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   first <= j < n
  *     lse = m + log sum_j exp(s_j - m),                    m = max_j s_j.
  *   n_seq       at most the handle's max_seq
@@ -516,7 +521,8 @@ void fiona_attention_destroy(fiona_attention *att);
  *   lengths     device, [n_seq]; clamped to [0, min(max_length,
  *               table_width * page_size)]
  *   scale > 0; window 0: none; softcap 0: none, else > 0
- * A sequence with no key gets out = 0 and lse = -inf.  Cache places past a
+ * A sequence with no key, or none whose score is above -inf, gets out = 0 and
+ * lse = -inf.  Cache places past a
  * sequence's length are never used, whatever they hold.
  * Asynchronous on stream; one or two kernel launches, allocates nothing.  The
  * workspace is shared by the handle's calls: one handle must not be used by

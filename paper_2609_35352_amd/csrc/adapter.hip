@@ -26,8 +26,10 @@ struct fiona_adapters {
 };
 
 // Rows below kMinWidth elements can be shorter than a lane's 16 bytes, which the
-// tiled kernels may always read: one value per wavefront or thread, bound by
-// latency (for what is this narrow, no more than the launches: 3 or 4).
+// tiled kernels may always read: one value per wavefront or thread.  Right, and slow
+// where the other side is wide or the tokens are many: a gradient's thread goes
+// through all of them (bfloat16, rank 16: 8192 tokens of 4096 x 4 325 us, a training
+// step of them 3.3 ms, of 512 182 us).
 constexpr uint32_t kMinWidth = 8;
 
 namespace fiona {
@@ -142,8 +144,9 @@ uint32_t blocks_of(uint64_t n) { return (uint32_t)((n + fiona::kRows - 1) / fion
 // Workgroups that share the adapters among 64 tokens: 256 over the blocks, as
 // with few tokens each may have its own; two at least, for the blocks in which
 // one request ends and the next begins.  Calls of 4096 x 4096 at rank 16, us, with
-// 128 / 256 / 512 over the blocks: 8192 tokens of 12 requests 51.2 / 46.0 / 59.3, of
-// 400 118 / 81 / 99; 16384 of 30 131 with one at least, 117 with two.
+// 128 / 256 / 512 over the blocks: 1024 tokens of 64 requests 20.6 / 20.5 / 20.7; 4096
+// of 200 44.2 / 51.3 / 54.1; 8192 of 12 46.9 / 46.9 / 59.3, of 400 81 / 81 / 99; 16384
+// of 30 131 with one at least, 118 with two.
 uint32_t slots_of(uint32_t n, uint32_t adapters) {
   const uint32_t want = std::max(2u, 256 / blocks_of(n));
   return std::min({want, adapters, std::min(n, fiona::kRows)});
@@ -151,9 +154,9 @@ uint32_t slots_of(uint32_t n, uint32_t adapters) {
 
 // Parts of a row's contraction: enough workgroups to fill the GPU, and not so
 // many that adding them up costs more (us with 256 / 512 / 1024 workgroups: 8192
-// tokens of 4096, rank 16, 48.2 / 46.0 / 49.5; 613 of 1000, 20, 23.5 / 22.2 / 22.3;
-// a training step of 8192 of 4096, 64, 170.9 / 158.1 / 159.4; with at most 1 / 2 /
-// 4 / 8 parts: 16 of 4096 21.3 / 15.7 / 12.6 / 11.6).
+// tokens of 4096, rank 16, 49.2 / 47.1 / 50.1; 613 of 1000, 20, 23.4 / 22.1 / 22.3;
+// a training step of 8192 of 4096, 64, 156.0 / 151.0 / 161.9; with at most 1 / 2 /
+// 4 / 8 parts: 16 of 4096, rank 16, 21.0 / 15.3 / 12.3 / 11.3).
 constexpr uint32_t kMaxSplits = 8, kWorkgroups = 512;
 uint32_t splits_of(uint32_t n, uint32_t adapters) {
   const uint32_t slots = slots_of(n, adapters), wgs = blocks_of(n) * (slots > 2 ? slots : 1);
@@ -167,7 +170,7 @@ uint32_t grad_slices(uint32_t n, uint32_t type, uint32_t RP) {
 
 // Parts of the tokens in the gradients' sums, where their columns alone do not
 // fill the GPU (us with 256 / 512 / 1024 workgroups: 2048 tokens of 768, rank 8,
-// 41.7 / 41.6 / 42.5; 8192 of 4096, 64, 158.2 / 158.1 / 176.6).
+// 34.9 / 34.7 / 35.7; 8192 of 4096, 64, 150.7 / 151.0 / 177.2).
 constexpr uint32_t kGradWorkgroups = 512;
 uint32_t grad_splits_of(const fiona_adapters_desc &D, uint32_t RP, uint32_t n) {
   const uint64_t wgs = (uint64_t)(grad_slices(D.d_in, D.type, RP) + grad_slices(D.d_out, D.type, RP)) * D.n_adapter * ((RP + 63) / 64);
@@ -199,18 +202,18 @@ void launch_shrink(const fiona_adapters *H, const fiona::AdapterIds &I, const fi
 
 // Whether the sums of h and g share a launch with expand, which then adds up g's
 // parts by itself in every slice of columns: for small ranks, where those are few.
-// A training step apart / together, us: rank 8 of 768, 13 tokens 24.4 / 19.6, 2048
-// 38.4 / 34.6; of 4096, rank 16, 8192 tokens 123.3 / 118.9; rank 32, 1024 tokens 48.0 /
-// 43.8, 8192 124.8 / 124.8; rank 64, 64 tokens 37.7 / 36.7, 512 46.9 / 46.5, 1024 59.8 /
-// 63.0, 8192 150.6 / 158.9; rank 128, 64 tokens 53.6 / 56.9, 512 75.6 / 88.4.
+// A training step apart / together, us: rank 8 of 768, 13 tokens 25.1 / 19.7, 2048
+// 38.5 / 34.6; of 4096, rank 16, 8192 tokens 122.8 / 118.4; rank 32, 1024 tokens 48.1 /
+// 43.6, 8192 125.1 / 125.0; rank 64, 64 tokens 37.5 / 36.7, 512 46.9 / 46.5, 1024 59.7 /
+// 62.8, 8192 150.7 / 158.1; rank 128, 64 tokens 53.7 / 56.8, 512 75.8 / 88.5.
 constexpr bool together(uint32_t RP) { return RP <= 32; }
 
 template <typename T, bool INNER>
 void launch_expand(const fiona_adapters *H, fiona::ExpandParams P, hipStream_t stream) {
   const uint32_t n = P.I.n_tok, steps = (P.O + 255) / 256;
   P.slots = slots_of(n, P.I.n_adapter + 1);
-  // (512 / 1024 / 2048 workgroups, us of the whole call: 8192 tokens of 4096, rank 16, 46.0 / 47.4 / 50.7;
-  // a training step at rank 64 158.5 / 158.0 / 163.4)
+  // (512 / 1024 / 2048 workgroups, us of the whole call: 8192 tokens of 4096, rank 16, 47.1 / 47.7 / 51.4;
+  // a training step at rank 64 151.0 / 150.4 / 156.0)
   const uint32_t wgs = blocks_of(n), slices = std::max(1u, std::min(steps, (kWorkgroups + wgs - 1) / wgs));
   P.slice = (steps + slices - 1) / slices * 256;
   const dim3 grid((P.O + P.slice - 1) / P.slice, blocks_of(n), P.slots);

@@ -347,7 +347,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && RT <= 2 ? 3 : (sizeof(T
     if (start >= end) return;
     // A tile's base rows are asked for two tiles ahead, the next columns'
     // factor as soon as the last tile's products are done (the call with one / two
-    // tiles ahead, us: 45.6 / 46.0 at rank 16, a training step at rank 64 160.9 / 158.2).
+    // tiles ahead, us: 45.6 / 47.1 at rank 16, a training step at rank 64 154.2 / 151.0).
     constexpr uint32_t SETS = 2;
     u4 b[SETS][NI], w[KF][4];
     auto load_w = [&](uint32_t o0) {
@@ -573,9 +573,9 @@ __device__ __forceinline__ u4 column_of(const uint32_t (&x)[SP][W], uint32_t u) 
 // eight tokens (four in 32 bits) to a lane; the transposed fragments (columns x tokens) are
 // picked from the tokens' words in registers, as values are in the attention.
 // 8192 tokens of 4096 + 4096 in bfloat16 at rank 64 (134 MB of rows and as much of
-// columns, the latter through the caches): 45 us, 3.0 TB/s of rows.  Bound by the
-// loads of both (41 us without the rows', 51 without the columns', 38 without
-// either, of 60 at the time); 8 wavefronts took 70, tokens in two parts 75.
+// columns, the latter through the caches): 47 us, 2.9 TB/s of rows.  Bound by the
+// loads of both (36 us without the rows', 39 without the columns', 32 without
+// either); with the tokens in two parts 61.
 template <typename T, int RT>
 __global__ void __launch_bounds__(256) grad_kernel(GradParams P) {
   constexpr uint32_t E = grad_width<T>(16 * RT), C = 16 * E, TB = kGradTokens<T>, SP = TB / 4, W = E * sizeof(T) / 4;

@@ -88,7 +88,7 @@ __device__ __forceinline__ void store8(C *p, const float (&x)[8]) {
 // and written once: what bounds it is memory (16384 tokens of 32 + 8 + 8 heads of
 // 128 in bfloat16, 411 MB: 69 us, 6.0 TB/s; stores that pass the caches by reach
 // more than a plain copy's 5.1), or for a few tokens the launch (8 of 12 + 12 + 12
-// heads of 64: 3.5 us on the GPU, 9.4 a call).
+// heads of 64: 3.4 us on the GPU, 10.2 a call from Python).
 template <typename T, typename C>
 __global__ void __launch_bounds__(256) append_kernel(AppendParams P) {
   const uint32_t units = (P.d + 15) / 16, items = (P.n_head + 2 * P.n_kv) * units;
@@ -224,8 +224,8 @@ extern "C" int fiona_kv_append(const fiona_kv_cache *cache, const fiona_append_a
   P.interleaved = A.interleaved != 0, P.page_size = K.page_size;
   P.n_slot = (int64_t)K.n_pages * K.page_size;
   page_divisor(K.page_size, P.page_mul, P.page_shift);
-  // 16-byte pieces where every row and its halves hold whole ones (1531 tokens of
-  // 25 heads of 80, 11.1 us, of 81 by elements 11.2; with 16384 of 48 6.0 and 1.9 TB/s),
+  // 16-byte pieces where every row and its halves hold whole ones (16384 tokens of 48
+  // heads 5.9 TB/s, by elements 1.9; 1531 of 25, 80 and 81 elements long, the same),
   // and the tables have a row, as a position outside them reads the first, unused.
   const bool pieces = d % 8 == 0 && P.half % 8 == 0 && rows_aligned16(in[0]) && rows_aligned16(in[1]) &&
                       rows_aligned16(out[0]) && rows_aligned16(out[1]) &&

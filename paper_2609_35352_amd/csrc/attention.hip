@@ -28,9 +28,10 @@ namespace {
 // table), none above kMaxChunk so that ragged lengths even out, at most
 // kMaxSplits parts to join, and no join for what one workgroup does as fast.
 // Chunks of 256 / 512 / 768 / 1024 / 2048 / 4096, us: 64 sequences of 100 to 8192
-// keys, 8 key heads of 128, 108 / 102 / 95 / 113 / 143 / 145; 19 of up to 3000,
-// 7 of 80, 20.7 / 25.0 / 25.3 / 26.2 / 30.1 / 35.2; 2 of 100000 and 131072, 8 of
-// 128, 164 / 165 / 165 / 165 / 159 / 157; 1 of 300, 12 of 64 in 32 bits, 19.7 / 17.1 whole.
+// keys, 8 key heads of 128, 106 / 101 / 95 / 111 / 142 / 143; 19 of up to 3000,
+// 7 of 80, 20.2 / 24.8 / 25.5 / 27.0 / 32.0 / 38.3; 2 of 100000 and 131072, 8 of
+// 128 (2048 at least for 64 parts), 159, at 4096 156; 1 of 300, 12 of 64 in 32 bits,
+// 11.2 in two parts, 8.8 whole.
 constexpr uint32_t kMinChunk = 256, kMaxChunk = 768, kNoSplit = 512, kWorkgroups = 2048;
 using fiona::kMaxSplits;
 uint32_t chunk_of(uint64_t keys, uint64_t units) {

@@ -153,7 +153,9 @@ __device__ __forceinline__ uint32_t pair_low(uint32_t a, uint32_t b) { return __
 __device__ __forceinline__ uint32_t pair_high(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
 // This wavefront's number in its workgroup, in a scalar register: branches and
-// addresses that depend on it need no lane masks.
+// addresses that depend on it need no lane masks.  grad_kernel's results need it too:
+// with the number in a vector register its loop over steps counts as divergent, and
+// the two sets of operands that take turns in it came out overwritten.
 __device__ __forceinline__ uint32_t wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // What one lane of a wavefront wrote to LDS another reads next.
