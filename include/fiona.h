@@ -608,6 +608,206 @@ void fiona_adapters_destroy(fiona_adapters *adapters);
 int fiona_adapter_linear(const fiona_adapters *adapters, const fiona_adapter_args *args, hipStream_t stream);
 int fiona_adapter_backward(const fiona_adapters *adapters, const fiona_adapter_args *args, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * The key holder's training step: a norm between projections, losses on the
+ * logits with their gradients, and the optimiser that applies fiona_adapter_backward's.
+ * Types, rounding, strides, alignment and streams as above: 32-bit sums and
+ * statistics, one rounding of each result, sums in a fixed order.
+ * ------------------------------------------------------------------------ */
+#define FIONA_MAX_NORM_WIDTH 32768u
+
+/*
+ * fiona_layer_norm: with s_t = x_t, or x_t + residual_t rounded to the type,
+ *     mean = sum s / width,  rstd = 1 / sqrt(sum (s - mean)^2 / width + eps),
+ *     y_t = weight (s_t - mean) rstd + bias
+ *   type, weight_type  fiona_type of the rows, and of weight and bias (the rows' type or FIONA_F32)
+ *   x, residual   device, [n][width]; residual NULL: none
+ *   weight, bias  device, [width], or NULL (one, zero)
+ *   y, total      device, [n][width]; total receives s, or is NULL.  y or total may be x or residual
+ *                 itself (same pointer and stride), but not both the same
+ *   mean, rstd    device, [n] float32, or NULL
+ *   eps > 0; width at most FIONA_MAX_NORM_WIDTH
+ * Asynchronous on stream; one kernel launch, allocates nothing.  Errors
+ * (nothing is launched): FIONA_ERR_ARG, FIONA_ERR_UNSUPPORTED, FIONA_ERR_ALIGN,
+ * FIONA_ERR_ALIAS, FIONA_ERR_HIP.
+ */
+typedef struct fiona_norm_args {
+  uint32_t n, width, type, weight_type;
+  float eps;
+  const void *x, *residual, *weight, *bias;
+  void *y, *total;
+  float *mean, *rstd;
+  uint64_t x_row, residual_row, y_row, total_row;
+} fiona_norm_args;
+
+int fiona_layer_norm(const fiona_norm_args *args, hipStream_t stream);
+
+/*
+ * fiona_layer_norm_backward: from dy, the gradient of y, with xh = (x - mean) rstd
+ * (x: what was normalised, s above) and u = weight dy,
+ *     dx_t = dx_base_t + rstd (u - sum u / width - xh sum (u xh) / width)
+ *     dweight = sum over the rows of dy xh,   dbias = sum of dy
+ *   dy, x, dx_base, dx  device, [n][width]; dx_base NULL: zero (else the gradient that
+ *                       reaches s by other ways); dx may be dx_base, dy or x itself
+ *   mean, rstd          device, [n] float32, as fiona_layer_norm wrote them
+ *   weight              device, [width], or NULL (one)
+ *   dweight, dbias      device, [width], of the weight's type, overwritten (zeros with n 0);
+ *                       NULL: not wanted
+ * fiona_norm_create: the workspace (the parts of dweight and dbias) for up to
+ * max_rows rows.  Asynchronous on stream; at most two kernel launches, allocates nothing.
+ * The workspace is shared by the handle's calls: one handle must not be used by
+ * two streams, or in two graphs that run, at the same time.  Errors: as above, and
+ * FIONA_ERR_NOMEM from fiona_norm_create.
+ */
+typedef struct fiona_norm_desc {
+  uint32_t type, weight_type, width, max_rows;
+} fiona_norm_desc;
+
+typedef struct fiona_norm_backward_args {
+  uint32_t n;
+  const void *dy, *x, *weight;
+  const float *mean, *rstd;
+  const void *dx_base;
+  void *dx, *dweight, *dbias;
+  uint64_t dy_row, x_row, dx_base_row, dx_row;
+} fiona_norm_backward_args;
+
+typedef struct fiona_norm fiona_norm;
+int fiona_norm_create(const fiona_norm_desc *desc, fiona_norm **out);
+void fiona_norm_destroy(fiona_norm *norm);
+int fiona_layer_norm_backward(const fiona_norm *norm, const fiona_norm_backward_args *args, hipStream_t stream);
+
+/*
+ * Losses on tokens' logits z, [n_tok][vocab], and the gradient with respect to
+ * them.  A token's log-probability is
+ *     l_t = z_t[targets[t]] - log sum_j exp(z_t[j]);
+ * a target outside [0, vocab) says that the token does not count (a prompt,
+ * padding): its logits are never used, whatever they hold, and its row of dlogits
+ * is zero.  A loss whose derivative with respect to l_t is g_t has
+ *     dlogits_t = g_t (onehot(targets[t]) - softmax(z_t)),
+ * zero where g_t is.  dlogits may be NULL (no gradient) or logits itself (same
+ * pointer and stride).
+ *
+ * fiona_token_loss_create: the workspace of calls of up to max_tokens tokens and
+ * max_pairs pairs (0: none) of vocab logits.  Limits: vocab, max_tokens and
+ * max_pairs at most 2^22.
+ *
+ * fiona_preference_loss: sequence s has tokens offsets[s] to offsets[s + 1] - 1;
+ * sequence 2 p is the preferred one of pair p, 2 p + 1 the other.  With L_s the sum
+ * of its tokens' log-probabilities and R_s = reference[s], the same of another model,
+ *     h = beta ((L_{2p} - R_{2p}) - (L_{2p+1} - R_{2p+1})),
+ *     loss_p = -w_p ((1 - label_smoothing) log sigmoid(h) + label_smoothing log sigmoid(-h))
+ * with w_p = weights[p], or 1 / n_pair without; logps receives L.
+ *   targets, offsets  device, [n_tok] and [2 n_pair + 1] (clamped to [0, n_tok]; not decreasing, or
+ *                     the gradients of tokens in several sequences are one of theirs);
+ *                     tokens of no sequence do not count
+ *   reference, logps  device, [2 n_pair]
+ *   loss, weights     device, [n_pair]; weights NULL: 1 / n_pair
+ *   beta > 0, label_smoothing in [0, 1)
+ * A pair of weight zero has no loss and no gradient, whatever its logits.
+ *
+ * fiona_policy_loss: with the ratio r = exp(l_t - old_t) to the policy that sampled
+ * the token, its advantage A and d = reference_t - l_t,
+ *     loss_t = w_t (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl (exp(d) - d - 1))
+ * with w_t = weights[t], or 1 / n_tok without; logps receives l.  Tokens that do not
+ * count get loss and logps 0.
+ *   old, advantages, loss, logps   device, [n_tok]
+ *   reference   device, [n_tok]; not read (NULL) with kl 0
+ *   weights     device, [n_tok], or NULL
+ *   clip_low in [0, 1], clip_high >= 0, kl >= 0
+ * Where the ratio stands at an end of the clip the free product's derivative is taken.  A token of weight
+ * zero has no loss and no gradient, whatever its logits.
+ *
+ * Both: asynchronous on stream, kernel launches only, allocate nothing.  The
+ * workspace is shared by the handle's calls: one handle must not be used by two
+ * streams, or in two graphs that run, at the same time.  Errors (nothing is launched): FIONA_ERR_ARG,
+ * FIONA_ERR_UNSUPPORTED, FIONA_ERR_ALIGN, FIONA_ERR_ALIAS, FIONA_ERR_HIP.
+ */
+typedef struct fiona_token_loss_desc {
+  uint32_t type, vocab, max_tokens, max_pairs;
+} fiona_token_loss_desc;
+
+typedef struct fiona_preference_args {
+  uint32_t n_tok, n_pair;
+  float beta, label_smoothing;
+  const void *logits;
+  void *dlogits;
+  uint64_t logits_row, dlogits_row;
+  const int32_t *targets, *offsets;
+  const float *reference, *weights;
+  float *loss, *logps;
+} fiona_preference_args;
+
+typedef struct fiona_policy_args {
+  uint32_t n_tok;
+  float clip_low, clip_high, kl;
+  const void *logits;
+  void *dlogits;
+  uint64_t logits_row, dlogits_row;
+  const int32_t *targets;
+  const float *old, *advantages, *reference, *weights;
+  float *loss, *logps;
+} fiona_policy_args;
+
+typedef struct fiona_token_loss fiona_token_loss;
+int fiona_token_loss_create(const fiona_token_loss_desc *desc, fiona_token_loss **out);
+void fiona_token_loss_destroy(fiona_token_loss *loss);
+int fiona_preference_loss(const fiona_token_loss *loss, const fiona_preference_args *args, hipStream_t stream);
+int fiona_policy_loss(const fiona_token_loss *loss, const fiona_policy_args *args, hipStream_t stream);
+
+/*
+ * fiona_adamw_step: one step over all tensors of a handle, each of n contiguous
+ * elements.  With g the gradient (times *grad_scale), t = *step and lr = *lr,
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *     p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ *   param, grad  device, of the desc's type; param is written
+ *   master       device, float32, or NULL.  With it p is the master, and param its value rounded
+ *   m, v         device: float32 (state_bits 32), or (8) e4m3 values c of blocks of
+ *                FIONA_ADAMW_BLOCK elements, counted from the tensor's first, that stand
+ *                for m = c m_scale and sqrt(v) = c v_scale of their block
+ *   m_scale, v_scale  device, float32, one to a block (a last short one as well); NULL with 32 bits
+ *   lr, step, grad_scale  device, one float32, int32 (from 1 on; less counts as 1) and float32 (NULL:
+ *                1): read when the step runs, so that a captured one follows them
+ * 8-bit states: the new m and v are used in 32 bits, then rounded to one of the two
+ * neighbouring values, up with the probability that keeps their mean (rounded to
+ * nearest, beta2 v would stay v for ever); sqrt(v) > 0 is never rounded to zero.  A
+ * block's scale is its largest magnitude / 448 (zero, as its values, below 2^-100).  The dither of
+ * element i is 16 bits for m (low) and 16 for v (high) of mix(i ^ mix(step 0x9E3779B1 + seed)) in
+ * 32-bit arithmetic, i counting from the first tensor on, every tensor from a multiple of the block;
+ *     mix(x): x ^= x >> 16; x *= 0xA3D8B167; x ^= x >> 15; x *= 0xC94F6E2B; x ^= x >> 16.
+ * A gradient that is not finite makes its element's states so, and with 8 bits its block's.
+ *
+ * fiona_adamw_create keeps the tensors' addresses, not the tensors: they have to
+ * live, where they are, as long as the handle is used.  What is written must not
+ * overlap anything else of any tensor (FIONA_ERR_ALIAS).
+ * fiona_adamw_step: asynchronous on stream; one kernel launch, allocates nothing.
+ * Errors: FIONA_ERR_ARG, FIONA_ERR_UNSUPPORTED, FIONA_ERR_ALIGN, FIONA_ERR_ALIAS,
+ * FIONA_ERR_NOMEM, FIONA_ERR_HIP.
+ */
+#define FIONA_ADAMW_BLOCK 256u
+
+typedef struct fiona_adamw_tensor {
+  void *param;
+  const void *grad;
+  float *master;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  uint64_t n;
+  double weight_decay;
+} fiona_adamw_tensor;
+
+typedef struct fiona_adamw_desc {
+  uint32_t type, state_bits, n_tensor, seed;
+  double beta1, beta2, eps;              /* betas in [0, 1), eps > 0 */
+  const fiona_adamw_tensor *tensors;     /* host, [n_tensor] */
+} fiona_adamw_desc;
+
+typedef struct fiona_adamw fiona_adamw;
+int fiona_adamw_create(const fiona_adamw_desc *desc, fiona_adamw **out);
+void fiona_adamw_destroy(fiona_adamw *opt);
+int fiona_adamw_step(const fiona_adamw *opt, const float *lr, const int32_t *step, const float *grad_scale,
+                     hipStream_t stream);
+
 /*
  * Measurement helper (not part of the weighted sum): the register-only rate
  * of the raw route's arithmetic, against which the hybrid kernel's

@@ -467,6 +467,18 @@ def hybrid_linear_static(plan: Plan, in_t, pt_t, sign_t, scale_t, out_t, stream=
 #     adapter_linear(ad, x, ids, A, B, base, y)
 #     adapter_backward(ad, x, ids, A, B, dy, dx_base, dx, dA, dB)
 #
+# The training step around them: a norm between projections, losses on the logits with
+# their gradients, and the optimiser.
+#
+#     layer_norm(x, weight, bias, y, residual=r, total=s, mean=mean, rstd=rstd)
+#     ln = LayerNorm(dtype, width, max_rows)
+#     layer_norm_backward(ln, dy, s, weight, mean, rstd, dx_base, dx, dweight, dbias)
+#     tl = TokenLoss(dtype, vocab, max_tokens, max_pairs)
+#     preference_loss(tl, logits, targets, offsets, reference, loss, logps, dlogits)
+#     policy_loss(tl, logits, targets, old, advantages, loss, logps, dlogits)
+#     opt = AdamW(params, grads, m, v)
+#     adamw_step(opt, lr, step)
+#
 # Tensors are float32, float16 or bfloat16 tensors of the current device whose last
 # axis is contiguous; the other axes may have any stride.  Nothing is recorded for
 # autograd: tensors that require a gradient are refused in grad mode, and what a call
@@ -481,6 +493,14 @@ _ATTENTION_DESC = struct.Struct("@7I")
 _ATTENTION_ARGS = struct.Struct("@3I2f3P5Q2P")
 _ADAPTERS_DESC = struct.Struct("@7I")
 _ADAPTER_ARGS = struct.Struct("@I6PQ2P2Q5P3Q")
+_NORM_ARGS = struct.Struct("@4If8P4Q")
+_NORM_DESC = struct.Struct("@4I")
+_NORM_BACKWARD_ARGS = struct.Struct("@I9P4Q")
+_TOKEN_LOSS_DESC = struct.Struct("@4I")
+_PREFERENCE_ARGS = struct.Struct("@2I2f2P2Q6P")
+_POLICY_ARGS = struct.Struct("@I3f2P2Q7P")
+_ADAMW_TENSOR = struct.Struct("@7PQd")
+_ADAMW_DESC = struct.Struct("@4I3dP")
 
 _DTYPES = {}   # torch dtype -> fiona_type
 _raw_stream, _device_now, _modified = [], [], []
@@ -497,9 +517,14 @@ def _lm_lib():
         p = ctypes.c_void_p
         for name, args in (("fiona_kv_append", [p] * 3), ("fiona_attention_create", [p, ctypes.POINTER(p)]),
                            ("fiona_paged_attention", [p] * 4), ("fiona_adapters_create", [p, ctypes.POINTER(p)]),
-                           ("fiona_adapter_linear", [p] * 3), ("fiona_adapter_backward", [p] * 3)):
+                           ("fiona_adapter_linear", [p] * 3), ("fiona_adapter_backward", [p] * 3),
+                           ("fiona_layer_norm", [p] * 2), ("fiona_norm_create", [p, ctypes.POINTER(p)]),
+                           ("fiona_layer_norm_backward", [p] * 3), ("fiona_token_loss_create", [p, ctypes.POINTER(p)]),
+                           ("fiona_preference_loss", [p] * 3), ("fiona_policy_loss", [p] * 3),
+                           ("fiona_adamw_create", [p, ctypes.POINTER(p)]), ("fiona_adamw_step", [p] * 5)):
             getattr(L, name).restype, getattr(L, name).argtypes = ctypes.c_int, args
-        for name in ("fiona_attention_destroy", "fiona_adapters_destroy"):
+        for name in ("fiona_attention_destroy", "fiona_adapters_destroy", "fiona_norm_destroy", "fiona_token_loss_destroy",
+                     "fiona_adamw_destroy"):
             getattr(L, name).restype, getattr(L, name).argtypes = None, [p]
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (without the stream object: 2 us a call)
         _raw_stream.append(raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream))
@@ -735,3 +760,217 @@ def adapter_backward(ad: Adapters, x, ids, A, B, dy, dx_base, dx, dA, dB, ranks=
     if rc:
         raise FionaError(rc, "fiona_adapter_backward")
     _modified[0]((dx, dA, dB))
+
+
+def _shared(t, name, dtype, dev):
+    """The address of one value that a call reads on the device."""
+    return _packed(t, name, dtype, (1,), dev)
+
+
+def _write(t, name, dtype, shape, dev, packed, written):
+    """(address, row stride) of an output, which is noted as written; (0, 0) for None."""
+    if t is None:
+        return 0, 0
+    written.append(t)
+    if packed:
+        return _packed(t, name, dtype, shape, dev), 0
+    return t.data_ptr(), _rows(t, name, dtype, shape, dev)[0]
+
+
+def layer_norm(x, weight, bias, y, eps: float = 1e-5, residual=None, total=None, mean=None, rstd=None, stream=None) -> None:
+    """fiona_layer_norm: y [n][d] = the norm of x [n][d], or of x + residual, which total receives; weight, bias [d] (x's
+    type or float32, or None: one and zero); mean, rstd float32 [n].  y or total may be x or residual."""
+    shape, dt, dev = x.shape, x.dtype, x.get_device()
+    if len(shape) != 2:
+        raise ValueError("x must have shape [n][width]")
+    code = _type_code(dt)
+    n, d = shape
+    f32, written = _INT["f32"], []
+    w = weight if weight is not None else bias
+    wt = dt if w is None or w.dtype is dt else f32
+    xs = _rows(x, "x", dt, shape, dev)
+    rp, rs = (residual.data_ptr(), _rows(residual, "residual", dt, shape, dev)[0]) if residual is not None else (0, 0)
+    wp = _packed(weight, "weight", wt, (d,), dev) if weight is not None else 0
+    bp = _packed(bias, "bias", wt, (d,), dev) if bias is not None else 0
+    yp, ys = _write(y, "y", dt, shape, dev, False, written)
+    tp, ts = _write(total, "total", dt, shape, dev, False, written)
+    mp, _ = _write(mean, "mean", f32, (n,), dev, True, written)
+    qp, _ = _write(rstd, "rstd", f32, (n,), dev, True, written)
+    args = _NORM_ARGS.pack(n, d, code, code if wt is dt else 0, eps, x.data_ptr(), rp, wp, bp, yp, tp, mp, qp, xs[0], rs, ys, ts)
+    rc = _lm_lib().fiona_layer_norm(args, _stream_of(stream, dev))
+    if rc:
+        raise FionaError(rc, "fiona_layer_norm")
+    _modified[0](written)
+
+
+class _Handle:
+    """A handle of the library's, freed with the object."""
+
+    _destroy = ""
+
+    def _create(self, create, desc):
+        h = ctypes.c_void_p()
+        _check(getattr(_lm_lib(), create)(desc, ctypes.byref(h)), create)
+        self._h = h
+
+    @property
+    def handle(self):
+        return self._h
+
+    def close(self):
+        if getattr(self, "_h", None) and self._h.value:
+            getattr(lib(), self._destroy)(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class LayerNorm(_Handle):
+    """The workspace of layer_norm_backward (fiona_norm_create).  weight_dtype: dtype (default) or float32."""
+
+    _destroy = "fiona_norm_destroy"
+
+    def __init__(self, dtype, width: int, max_rows: int, weight_dtype=None):
+        self.dtype, self.width, self.max_rows = dtype, int(width), int(max_rows)
+        self.weight_dtype = dtype if weight_dtype is None else weight_dtype
+        self._create("fiona_norm_create", _NORM_DESC.pack(_type_code(dtype), _type_code(self.weight_dtype), self.width,
+                                                          self.max_rows))
+
+
+def layer_norm_backward(ln: LayerNorm, dy, x, weight, mean, rstd, dx_base, dx, dweight=None, dbias=None, stream=None) -> None:
+    """fiona_layer_norm_backward: dx [n][d] = dx_base (or None: zero) plus the gradient through the norm of x (layer_norm's
+    total, where it had a residual) from dy [n][d]; dweight, dbias [d].  dx may be dx_base, dy or x."""
+    n, dev, dt, wt, f32, written = x.shape[0], x.get_device(), ln.dtype, ln.weight_dtype, _INT["f32"], []
+    shape, row = (n, ln.width), (ln.width,)
+    gs, xs = _rows(dy, "dy", dt, shape, dev), _rows(x, "x", dt, shape, dev)
+    wp = _packed(weight, "weight", wt, row, dev) if weight is not None else 0
+    bp, bs = (dx_base.data_ptr(), _rows(dx_base, "dx_base", dt, shape, dev)[0]) if dx_base is not None else (0, 0)
+    dp, ds = _write(dx, "dx", dt, shape, dev, False, written)
+    args = _NORM_BACKWARD_ARGS.pack(n, dy.data_ptr(), x.data_ptr(), wp, _packed(mean, "mean", f32, (n,), dev),
+                                    _packed(rstd, "rstd", f32, (n,), dev), bp, dp,
+                                    _write(dweight, "dweight", wt, row, dev, True, written)[0],
+                                    _write(dbias, "dbias", wt, row, dev, True, written)[0], gs[0], xs[0], bs, ds)
+    rc = lib().fiona_layer_norm_backward(ln.handle, args, _stream_of(stream, dev))
+    if rc:
+        raise FionaError(rc, "fiona_layer_norm_backward")
+    _modified[0](written)
+
+
+class TokenLoss(_Handle):
+    """The workspace of preference_loss and policy_loss (fiona_token_loss_create)."""
+
+    _destroy = "fiona_token_loss_destroy"
+
+    def __init__(self, dtype, vocab: int, max_tokens: int, max_pairs: int = 0):
+        self.dtype, self.vocab, self.max_tokens, self.max_pairs = dtype, int(vocab), int(max_tokens), int(max_pairs)
+        self._create("fiona_token_loss_create", _TOKEN_LOSS_DESC.pack(_type_code(dtype), self.vocab, self.max_tokens,
+                                                                      self.max_pairs))
+
+
+def preference_loss(tl: TokenLoss, logits, targets, offsets, reference, loss, logps, dlogits=None, beta: float = 0.1,
+                    label_smoothing: float = 0.0, weights=None, stream=None) -> None:
+    """fiona_preference_loss: logits [n_tok][vocab], targets int32 [n_tok] (outside the vocabulary: not counted), offsets int32
+    [2 n_pair + 1], reference float32 [2 n_pair] -> loss float32 [n_pair], logps float32 [2 n_pair] and dlogits
+    [n_tok][vocab] (None: not wanted; it may be logits).  weights float32 [n_pair]: default 1 / n_pair."""
+    n, p, dev, i32, f32, written = logits.shape[0], loss.shape[0], logits.get_device(), _INT[4], _INT["f32"], []
+    shape = (n, tl.vocab)
+    zs = _rows(logits, "logits", tl.dtype, shape, dev)
+    dp, ds = _write(dlogits, "dlogits", tl.dtype, shape, dev, False, written)
+    args = _PREFERENCE_ARGS.pack(n, p, beta, label_smoothing, logits.data_ptr(), dp, zs[0], ds,
+                                 _packed(targets, "targets", i32, (n,), dev), _packed(offsets, "offsets", i32, (2 * p + 1,), dev),
+                                 _packed(reference, "reference", f32, (2 * p,), dev),
+                                 _packed(weights, "weights", f32, (p,), dev) if weights is not None else 0,
+                                 _write(loss, "loss", f32, (p,), dev, True, written)[0],
+                                 _write(logps, "logps", f32, (2 * p,), dev, True, written)[0])
+    rc = lib().fiona_preference_loss(tl.handle, args, _stream_of(stream, dev))
+    if rc:
+        raise FionaError(rc, "fiona_preference_loss")
+    _modified[0](written)
+
+
+def policy_loss(tl: TokenLoss, logits, targets, old, advantages, loss, logps, dlogits=None, reference=None,
+                clip_low: float = 0.2, clip_high: float = 0.2, kl: float = 0.0, weights=None, stream=None) -> None:
+    """fiona_policy_loss: logits [n_tok][vocab], targets int32 [n_tok] (outside the vocabulary: not counted), old, advantages
+    and, with kl > 0, reference float32 [n_tok] -> loss, logps float32 [n_tok] and dlogits [n_tok][vocab] (None: not
+    wanted; it may be logits).  weights float32 [n_tok]: default 1 / n_tok."""
+    n, dev, f32, written = logits.shape[0], logits.get_device(), _INT["f32"], []
+    shape, each = (n, tl.vocab), (n,)
+    zs = _rows(logits, "logits", tl.dtype, shape, dev)
+    dp, ds = _write(dlogits, "dlogits", tl.dtype, shape, dev, False, written)
+    args = _POLICY_ARGS.pack(n, clip_low, clip_high, kl, logits.data_ptr(), dp, zs[0], ds,
+                             _packed(targets, "targets", _INT[4], each, dev), _packed(old, "old", f32, each, dev),
+                             _packed(advantages, "advantages", f32, each, dev),
+                             _packed(reference, "reference", f32, each, dev) if reference is not None else 0,
+                             _packed(weights, "weights", f32, each, dev) if weights is not None else 0,
+                             _write(loss, "loss", f32, each, dev, True, written)[0],
+                             _write(logps, "logps", f32, each, dev, True, written)[0])
+    rc = lib().fiona_policy_loss(tl.handle, args, _stream_of(stream, dev))
+    if rc:
+        raise FionaError(rc, "fiona_policy_loss")
+    _modified[0](written)
+
+
+class AdamW(_Handle):
+    """An optimiser over many tensors (fiona_adamw_create), which it keeps: lists of contiguous tensors of the same shape at
+    the same place.  params, grads: float32, float16 or bfloat16; masters: float32, beside 16-bit parameters; m, v: float32,
+    or float8_e4m3fn with m_scales, v_scales float32 [ceil(n / 256)] (v then holds the root).  weight_decay: one for all or
+    a list.  Parameters may require a gradient: a step is not recorded."""
+
+    _destroy = "fiona_adamw_destroy"
+
+    def __init__(self, params, grads, m, v, masters=None, m_scales=None, v_scales=None, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay=0.01, seed: int = 0):
+        import torch
+
+        _lm_lib()
+        lists = {"params": params, "grads": grads, "m": m, "v": v, "masters": masters, "m_scales": m_scales, "v_scales": v_scales}
+        lists = {k: list(t) for k, t in lists.items() if t is not None}
+        n = len(lists["params"])
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+        for name, t in list(lists.items()) + [("weight_decay", decay)]:
+            if len(t) != n:
+                raise ValueError("%s has %d entries, params %d" % (name, len(t), n))
+        self.dtype = lists["params"][0].dtype if n else torch.float32
+        code, f32 = _type_code(self.dtype), torch.float32
+        small = n > 0 and lists["m"][0].dtype is torch.float8_e4m3fn
+        if small != ("m_scales" in lists) or small != ("v_scales" in lists):
+            raise ValueError("m_scales and v_scales go with states of 8 bits")
+        self.device = lists["params"][0].get_device() if n else None
+        packed = []
+        for i in range(n):
+            shape, count = lists["params"][i].shape, lists["params"][i].numel()
+            kinds = [("params", self.dtype, shape), ("grads", self.dtype, shape), ("masters", f32, shape),
+                     ("m", torch.float8_e4m3fn if small else f32, shape), ("v", torch.float8_e4m3fn if small else f32, shape),
+                     ("m_scales", f32, (-(-count // 256),)), ("v_scales", f32, (-(-count // 256),))]
+            at = []
+            for name, dtype, want in kinds:
+                t = lists[name][i] if name in lists else None
+                if t is not None and name == "params":
+                    t = t.detach()
+                at.append(_packed(t, "%s[%d]" % (name, i), dtype, want, self.device) if t is not None else 0)
+            packed.append(_ADAMW_TENSOR.pack(*at, count, decay[i]))
+        table = ctypes.create_string_buffer(b"".join(packed), max(1, n * _ADAMW_TENSOR.size))
+        if n:
+            _stream_of(None, self.device)      # (the current device is the tensors')
+        self._create("fiona_adamw_create", _ADAMW_DESC.pack(code, 8 if small else 32, n, int(seed), betas[0], betas[1], eps,
+                                                            ctypes.addressof(table)))
+        self._tensors = lists
+        # What a step writes, tensors that share a version counter once.
+        self._written = list({id(b): b for t in (lists[k] for k in lists if k != "grads") for x in t if x is not None
+                              for b in (x if x._base is None else x._base,)}.values())
+
+
+def adamw_step(opt: AdamW, lr, step, grad_scale=None, stream=None) -> None:
+    """fiona_adamw_step: one step over the handle's tensors; lr float32 [1], step int32 [1] (from 1 on) and grad_scale float32
+    [1] (default: one) are read on the device."""
+    dev = lr.get_device() if opt.device is None else opt.device
+    args = (_shared(lr, "lr", _INT["f32"], dev), _shared(step, "step", _INT[4], dev),
+            _shared(grad_scale, "grad_scale", _INT["f32"], dev) if grad_scale is not None else 0)
+    rc = lib().fiona_adamw_step(opt.handle, *args, _stream_of(stream, dev))
+    if rc:
+        raise FionaError(rc, "fiona_adamw_step")
+    _modified[0](opt._written)

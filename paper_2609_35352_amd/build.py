@@ -9,7 +9,9 @@ ROOT = os.path.dirname(HERE)
 SRCS = [os.path.join(HERE, "csrc", "fiona.hip"), os.path.join(HERE, "csrc", "rescale.hip"),
         os.path.join(HERE, "csrc", "rotate.hip"), os.path.join(HERE, "csrc", "microbench.hip"),
         os.path.join(HERE, "csrc", "ntt_check.hip"), os.path.join(HERE, "csrc", "append.hip"),
-        os.path.join(HERE, "csrc", "attention.hip"), os.path.join(HERE, "csrc", "adapter.hip")]
+        os.path.join(HERE, "csrc", "attention.hip"), os.path.join(HERE, "csrc", "adapter.hip"),
+        os.path.join(HERE, "csrc", "norm.hip"), os.path.join(HERE, "csrc", "token_loss.hip"),
+        os.path.join(HERE, "csrc", "adamw.hip")]
 OUT = os.path.join(HERE, "libfiona.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -133,10 +133,6 @@ int check_common(const fiona_adapters *H, const fiona_adapter_args *args, fiona:
   return FIONA_OK;
 }
 
-Rows matrix(const void *p, uint64_t e, uint64_t n, uint64_t width, uint64_t row) {
-  return Rows{p, e, width, {n, 1, 1}, {row, 0, 0}};
-}
-
 bool narrow(const fiona_adapters_desc &D) { return D.d_in < kMinWidth || D.d_out < kMinWidth; }
 
 uint32_t blocks_of(uint64_t n) { return (uint32_t)((n + fiona::kRows - 1) / fiona::kRows); }
@@ -225,31 +221,6 @@ void launch_expand(const fiona_adapters *H, fiona::ExpandParams P, hipStream_t s
   });
 }
 
-// FIONA_ERR_ALIAS where an output's rows overlap each other, another output
-// or an input; `own` pairs (an output that may be its base itself) are passed
-// over where pointer and row stride agree.
-int check_alias(const Rows *in, int n_in, const Rows *out, int n_out, const int *own) {
-  uint64_t elems;
-  for (int i = 0; i < n_in; ++i)
-    if (!empty(in[i]) && !span(in[i], elems)) return FIONA_ERR_ARG;
-  for (int o = 0; o < n_out; ++o) {
-    if (empty(out[o])) continue;
-    if (!span(out[o], elems) || !rows_distinct(out[o])) return FIONA_ERR_ALIAS;
-    for (int p = o + 1; p < n_out; ++p)
-      if (may_overlap(out[o], out[p])) return FIONA_ERR_ALIAS;
-    for (int i = 0; i < n_in; ++i) {
-      if (own[o] == i && in[i].base == out[o].base && (in[i].stride[0] == out[o].stride[0] || in[i].n[0] == 1)) continue;
-      if (may_overlap(out[o], in[i])) return FIONA_ERR_ALIAS;
-    }
-  }
-  return FIONA_OK;
-}
-
-bool on_device(const fiona_adapters *H) {
-  int dev = -1;
-  return hipGetDevice(&dev) == hipSuccess && dev == H->device;
-}
-
 }  // namespace
 
 extern "C" {
@@ -323,9 +294,9 @@ int fiona_adapter_linear(const fiona_adapters *H, const fiona_adapter_args *args
                      matrix(A.ranks, 4, 1, D.n_adapter, 0), matrix(A.scaling, 4, 1, D.n_adapter, 0),
                      matrix(A.base, e, n, D.d_out, A.base_row)};
   const Rows out[] = {matrix(A.y, e, n, D.d_out, A.y_row)};
-  const int own[] = {6};
+  const uint32_t own[] = {1u << 6};
   if ((rc = check_alias(in, 7, out, 1, own)) != FIONA_OK) return rc;
-  if (!on_device(H)) return FIONA_ERR_ARG;
+  if (!on_device(H->device)) return FIONA_ERR_ARG;
   P.base = A.base, P.y = A.y, P.base_row = A.base_row, P.y_row = A.y_row;
   with_type(D.type, [&](auto t) {
     using T = decltype(t);
@@ -363,9 +334,9 @@ int fiona_adapter_backward(const fiona_adapters *H, const fiona_adapter_args *ar
                      matrix(A.scaling, 4, 1, D.n_adapter, 0), matrix(A.dy, e, n, D.d_out, A.dy_row),
                      matrix(A.dx_base, e, n, D.d_in, A.dx_base_row)};
   const Rows out[] = {matrix(A.dx, e, n, D.d_in, A.dx_row), matrix(A.dA, e, 1, wa, 0), matrix(A.dB, e, 1, wb, 0)};
-  const int own[] = {7, -1, -1};
+  const uint32_t own[] = {1u << 7, 0, 0};
   if ((rc = check_alias(in, 8, out, 3, own)) != FIONA_OK) return rc;
-  if (!on_device(H)) return FIONA_ERR_ARG;
+  if (!on_device(H->device)) return FIONA_ERR_ARG;
   P.dy = A.dy, P.dx_base = A.dx_base, P.dx = A.dx, P.dA = A.dA, P.dB = A.dB;
   P.dy_row = A.dy_row, P.dx_base_row = A.dx_base_row, P.dx_row = A.dx_row;
   with_type(D.type, [&](auto t) {

@@ -1,0 +1,117 @@
+// fiona_layer_norm and fiona_layer_norm_backward (include/fiona.h).
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <new>
+
+#include "fiona.h"
+#include "norm_kernel.hpp"
+#include "rows.hpp"
+
+using namespace fiona_host;
+
+struct fiona_norm {
+  fiona_norm_desc desc{};
+  int device = -1;
+};
+
+namespace {
+
+// Calls f with values of the rows' type and of the weights'.
+template <typename F>
+void with_types(uint32_t type, uint32_t weight_type, F f) {
+  with_type(type, [&](auto t) {
+    if (weight_type == type) f(t, t);
+    else f(t, float{});
+  });
+}
+
+int check_types(uint32_t type, uint32_t weight_type, uint32_t width) {
+  if (!known_type(type) || (weight_type != type && weight_type != FIONA_F32)) return FIONA_ERR_UNSUPPORTED;
+  if (!width) return FIONA_ERR_ARG;
+  return width > FIONA_MAX_NORM_WIDTH ? FIONA_ERR_UNSUPPORTED : FIONA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int fiona_layer_norm(const fiona_norm_args *args, hipStream_t stream) {
+  if (!args) return FIONA_ERR_ARG;
+  const fiona_norm_args &A = *args;
+  int rc = check_types(A.type, A.weight_type, A.width);
+  if (rc != FIONA_OK) return rc;
+  if (!(A.eps > 0) || !std::isfinite(A.eps)) return FIONA_ERR_ARG;
+  if (!A.n) return FIONA_OK;
+  if (A.n > (1u << 30)) return FIONA_ERR_UNSUPPORTED;
+  if (!A.x || !A.y) return FIONA_ERR_ARG;
+  const uint64_t e = type_size(A.type), w = type_size(A.weight_type), n = A.n, d = A.width;
+  if (misaligned(A.x, e) || misaligned(A.residual, e) || misaligned(A.y, e) || misaligned(A.total, e) ||
+      misaligned(A.weight, w) || misaligned(A.bias, w) || misaligned(A.mean, 4) || misaligned(A.rstd, 4))
+    return FIONA_ERR_ALIGN;
+  const Rows in[] = {matrix(A.x, e, n, d, A.x_row), matrix(A.residual, e, n, d, A.residual_row), matrix(A.weight, w, 1, d, 0),
+                     matrix(A.bias, w, 1, d, 0)};
+  const Rows out[] = {matrix(A.y, e, n, d, A.y_row), matrix(A.total, e, n, d, A.total_row), matrix(A.mean, 4, 1, n, 0),
+                      matrix(A.rstd, 4, 1, n, 0)};
+  const uint32_t own[] = {3, 3, 0, 0};
+  if ((rc = check_alias(in, 4, out, 4, own)) != FIONA_OK) return rc;
+  const fiona::NormParams P{A.x, A.residual, A.weight, A.bias, A.y, A.total, A.mean, A.rstd,
+                            A.x_row, A.residual_row, A.y_row, A.total_row, A.n, A.width, A.eps};
+  with_types(A.type, A.weight_type, [&](auto t, auto v) {
+    hipLaunchKernelGGL((fiona::norm_kernel<decltype(t), decltype(v)>), dim3(A.n), dim3(256), 0, stream, P);
+  });
+  return hipGetLastError() == hipSuccess ? FIONA_OK : FIONA_ERR_HIP;
+}
+
+int fiona_norm_create(const fiona_norm_desc *desc, fiona_norm **out) {
+  if (!out) return FIONA_ERR_ARG;
+  *out = nullptr;
+  if (!desc) return FIONA_ERR_ARG;
+  const int rc = check_types(desc->type, desc->weight_type, desc->width);
+  if (rc != FIONA_OK) return rc;
+  if (!desc->max_rows) return FIONA_ERR_ARG;
+  if (desc->max_rows > (1u << 30)) return FIONA_ERR_UNSUPPORTED;
+  fiona_norm *H = new (std::nothrow) fiona_norm;
+  if (!H) return FIONA_ERR_NOMEM;
+  H->desc = *desc;
+  if (hipGetDevice(&H->device) != hipSuccess) {
+    delete H;
+    return FIONA_ERR_HIP;
+  }
+  *out = H;
+  return FIONA_OK;
+}
+
+void fiona_norm_destroy(fiona_norm *norm) { delete norm; }
+
+int fiona_layer_norm_backward(const fiona_norm *norm, const fiona_norm_backward_args *args, hipStream_t stream) {
+  if (!norm || !args) return FIONA_ERR_ARG;
+  const fiona_norm_desc &D = norm->desc;
+  const fiona_norm_backward_args &A = *args;
+  if (A.n > D.max_rows) return FIONA_ERR_ARG;
+  if (A.n && (!A.dy || !A.x || !A.mean || !A.rstd || !A.dx)) return FIONA_ERR_ARG;
+  const uint64_t e = type_size(D.type), w = type_size(D.weight_type), n = A.n, d = D.width;
+  if (misaligned(A.dy, e) || misaligned(A.x, e) || misaligned(A.weight, w) || misaligned(A.mean, 4) || misaligned(A.rstd, 4) ||
+      misaligned(A.dx_base, e) || misaligned(A.dx, e) || misaligned(A.dweight, w) || misaligned(A.dbias, w))
+    return FIONA_ERR_ALIGN;
+  const Rows in[] = {matrix(A.dy, e, n, d, A.dy_row), matrix(A.x, e, n, d, A.x_row), matrix(A.dx_base, e, n, d, A.dx_base_row),
+                     matrix(A.weight, w, 1, d, 0), matrix(A.mean, 4, 1, n, 0), matrix(A.rstd, 4, 1, n, 0)};
+  const Rows out[] = {matrix(A.dx, e, n, d, A.dx_row), matrix(A.dweight, w, 1, d, 0), matrix(A.dbias, w, 1, d, 0)};
+  const uint32_t own[] = {7, 0, 0};
+  const int rc = check_alias(in, 6, out, 3, own);
+  if (rc != FIONA_OK) return rc;
+  if (!on_device(norm->device)) return FIONA_ERR_ARG;
+  const fiona::NormGradParams P{A.dy, A.x, A.weight, A.dx_base, A.mean, A.rstd, A.dx, A.dweight, A.dbias,
+                                A.dy_row, A.x_row, A.dx_base_row, A.dx_row, A.n, D.width};
+  with_types(D.type, D.weight_type, [&](auto t, auto v) {
+    using T = decltype(t);
+    using W = decltype(v);
+    if (A.dweight || A.dbias)   // (before dx, which may be dy or x)
+      hipLaunchKernelGGL((fiona::norm_weight_grad_kernel<T, W>), dim3((D.width + 255) / 256), dim3(256), 0, stream, P);
+    if (A.n) hipLaunchKernelGGL((fiona::norm_grad_kernel<T, W>), dim3(A.n), dim3(256), 0, stream, P);
+  });
+  return hipGetLastError() == hipSuccess ? FIONA_OK : FIONA_ERR_HIP;
+}
+
+}  // extern "C"

@@ -120,4 +120,34 @@ inline void page_divisor(uint32_t page_size, uint32_t &mul, uint32_t &shift) {
 
 inline bool misaligned(const void *p, uint64_t elem) { return ((uint64_t)p & (elem - 1)) != 0; }
 
+inline Rows matrix(const void *p, uint64_t e, uint64_t n, uint64_t width, uint64_t row) {
+  return Rows{p, e, width, {n, 1, 1}, {row, 0, 0}};
+}
+
+// FIONA_ERR_ALIAS where an output's rows overlap each other, another output
+// or an input; inputs whose bit is set in own[o] may be output o itself: they are
+// passed over where pointer and row stride agree.
+inline int check_alias(const Rows *in, int n_in, const Rows *out, int n_out, const uint32_t *own) {
+  uint64_t elems;
+  for (int i = 0; i < n_in; ++i)
+    if (!empty(in[i]) && !span(in[i], elems)) return FIONA_ERR_ARG;
+  for (int o = 0; o < n_out; ++o) {
+    if (empty(out[o])) continue;
+    if (!span(out[o], elems) || !rows_distinct(out[o])) return FIONA_ERR_ALIAS;
+    for (int p = o + 1; p < n_out; ++p)
+      if (may_overlap(out[o], out[p])) return FIONA_ERR_ALIAS;
+    for (int i = 0; i < n_in; ++i) {
+      if (own[o] >> i & 1u && in[i].base == out[o].base && (in[i].stride[0] == out[o].stride[0] || in[i].n[0] == 1)) continue;
+      if (may_overlap(out[o], in[i])) return FIONA_ERR_ALIAS;
+    }
+  }
+  return FIONA_OK;
+}
+
+// Whether a handle's device is the current one, to which every launch goes.
+inline bool on_device(int device) {
+  int dev = -1;
+  return hipGetDevice(&dev) == hipSuccess && dev == device;
+}
+
 }  // namespace fiona_host

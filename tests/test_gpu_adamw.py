@@ -1,0 +1,267 @@
+"""fiona_adamw_step against plain forms: 32-bit states in 64 bits, 8-bit states bit for bit in 32-bit operations."""
+import pytest
+
+import paper_2609_35352_amd as fiona
+
+torch = pytest.importorskip("torch")
+import training_reference as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+F32, F16, BF16, F8 = torch.float32, torch.float16, torch.bfloat16, torch.float8_e4m3fn
+
+
+def _dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    fiona.lib()
+    return torch.device("cuda:0")
+
+
+def _tensors(sizes, dtype, master, bits, seed, shift=0):
+    """Lists on the CPU; the tensors lie `shift` elements behind an allocation's start once moved (see _move)."""
+    g = torch.Generator().manual_seed(seed)
+    c = dict(params=[], grads=[], masters=[], m=[], v=[], m_scales=[], v_scales=[])
+    for n in sizes:
+        p = 0.1 * torch.randn(n, generator=g)
+        c["masters"].append(p)
+        c["params"].append(p.to(dtype))
+        c["grads"].append((0.02 * torch.randn(n, generator=g)).to(dtype))
+        m, r = 0.01 * torch.randn(n, generator=g), (0.02 * torch.randn(n, generator=g)).abs()
+        if bits == 32:
+            c["m"].append(m)
+            c["v"].append(r * r)
+            continue
+        half = torch.full((n,), 0.5)
+        for key, x, positive in (("m", m, False), ("v", r, True)):
+            codes, scale = ref.to_codes(x, half, positive)
+            c[key].append(codes)
+            c[key + "_scales"].append(scale)
+    if not master:
+        del c["masters"]
+    if bits == 32:
+        del c["m_scales"], c["v_scales"]
+    return c
+
+
+def _move(c, dev, shift=0):
+    def one(t):
+        store = torch.zeros(t.numel() + shift + 3, dtype=t.dtype, device=dev)
+        out = store[shift:shift + t.numel()]
+        out.copy_(t)
+        return out
+
+    return {k: [one(t) for t in ts] for k, ts in c.items()}
+
+
+def _scalars(dev, lr=3e-3, step=3):
+    return torch.tensor([lr], device=dev), torch.tensor([step], dtype=torch.int32, device=dev)
+
+
+def _check(c, t, lr, step, decay, eps=1e-8, scale=1.0, betas=(0.9, 0.999), seed=0):
+    first = 0
+    for i, p0 in enumerate(c["params"]):
+        n = p0.numel()
+        start = c["masters"][i] if "masters" in c else p0
+        if "m_scales" in c:
+            cm, cv, sm, sv, m, v = ref.states8(c["grads"][i], c["m"][i], c["v"][i], c["m_scales"][i], c["v_scales"][i], *betas, step, seed,
+                                               first, scale)
+            for key, want in (("m", cm), ("v", cv)):
+                assert torch.equal(t[key][i].cpu().view(torch.uint8), want.view(torch.uint8)), (i, key)
+            assert torch.equal(t["m_scales"][i].cpu(), sm) and torch.equal(t["v_scales"][i].cpu(), sv), i
+            (p, bp), _, _ = ref.adamw(start, torch.zeros(n), m, v, lr, step, *betas, eps, decay, new=True)
+        else:
+            (p, bp), (m, bm), (v, bv) = ref.adamw(start, c["grads"][i], c["m"][i], c["v"][i], lr, step, *betas, eps, decay, scale)
+            ref.assert_close(t["m"][i], m, bm, "m %d" % i)
+            ref.assert_close(t["v"][i], v, bv, "v %d" % i)
+        dt = p0.dtype
+        if "masters" in c:
+            ref.assert_close(t["masters"][i], p, bp, "master %d" % i)
+            assert torch.equal(t["params"][i], t["masters"][i].to(dt)), i
+        else:
+            ref.assert_close(t["params"][i], p, bp + (2 * ref.U[dt] * p.abs() + ref.TINY[dt] if dt is not F32 else 0), "param %d" % i)
+        first += -(-n // 256) * 256
+
+
+KINDS = [(F32, False), (F16, False), (BF16, False), (F16, True), (BF16, True)]
+SIZES = [1, 2, 255, 256, 257, 1000, 0, 1024, 1373, 5000, 12289]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype,master", KINDS)
+@pytest.mark.parametrize("shift", [0, 1, 4])
+def test_step(dtype, master, bits, shift):
+    dev = _dev()
+    c = _tensors(SIZES, dtype, master, bits, seed=bits + shift)
+    t = _move(c, dev, shift)
+    opt = fiona.AdamW(**t, weight_decay=0.05, seed=99)
+    lr, step = _scalars(dev)
+    fiona.adamw_step(opt, lr, step)
+    torch.cuda.synchronize()
+    _check(c, t, 3e-3, 3, 0.05, seed=99)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_first_steps_scale_and_decay(bits):
+    dev = _dev()
+    for step_no, scale, betas, decay, eps in ((1, 0.25, (0.9, 0.999), 0.0, 1e-8), (1000000, 3.0, (0.95, 0.99), 0.3, 1e-3), (2, 1.0, (0.5, 0.5), 0.1, 1e-6)):
+        c = _tensors([700, 256, 3000], F32, False, bits, seed=step_no % 97)
+        t = _move(c, dev)
+        opt = fiona.AdamW(**t, betas=betas, eps=eps, weight_decay=decay)
+        lr, step = _scalars(dev, step=step_no)
+        fiona.adamw_step(opt, lr, step, grad_scale=torch.tensor([scale], device=dev))
+        torch.cuda.synchronize()
+        _check(c, t, 3e-3, step_no, decay, eps=eps, scale=scale, betas=betas)
+
+
+def test_decay_of_each_tensor():
+    dev = _dev()
+    c = _tensors([300, 600], F32, False, 32, seed=4)
+    t = _move(c, dev)
+    fiona.adamw_step(fiona.AdamW(**t, weight_decay=[0.5, 0.0]), *_scalars(dev))
+    torch.cuda.synchronize()
+    for i, decay in enumerate((0.5, 0.0)):
+        one = {k: v[i:i + 1] for k, v in c.items()}
+        _check(one, {k: v[i:i + 1] for k, v in t.items()}, 3e-3, 3, decay)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_from_nothing(bits):
+    """Zero states and zero gradients: nothing moves but the decay; then a first gradient moves each element by lr."""
+    dev = _dev()
+    c = _tensors([900], F32, False, bits, seed=5)
+    for k in ("m", "v", "grads") + (("m_scales", "v_scales") if bits == 8 else ()):
+        c[k][0].zero_()
+    t = _move(c, dev)
+    opt = fiona.AdamW(**t, weight_decay=0.0)
+    lr, step = _scalars(dev, step=1)
+    fiona.adamw_step(opt, lr, step)
+    assert torch.equal(t["params"][0].cpu(), c["params"][0]) and not t["m"][0].float().any() and not t["v"][0].float().any()
+    t["grads"][0].copy_(0.1 * torch.randn(900, generator=torch.Generator().manual_seed(6)).sign())
+    fiona.adamw_step(opt, lr, step)
+    moved = (t["params"][0].cpu() - c["params"][0]).abs()
+    assert torch.allclose(moved, torch.full((900,), 3e-3), rtol=1e-3)
+
+
+def test_small_variances_are_never_rounded_to_zero():
+    """A block with one large gradient: the others' root variances lie below e4m3's smallest value of that scale."""
+    dev = _dev()
+    g = torch.full((256,), 1e-9)
+    g[7] = 1e3
+    c = dict(params=[torch.ones(256)], grads=[g], m=[torch.zeros(256).to(F8)], v=[torch.zeros(256).to(F8)], m_scales=[torch.zeros(1)],
+             v_scales=[torch.zeros(1)])
+    t = _move(c, dev)
+    fiona.adamw_step(fiona.AdamW(**t, weight_decay=0.0), *_scalars(dev, step=1))
+    torch.cuda.synchronize()
+    assert bool((t["v"][0].float() > 0).all())
+    _check(c, t, 3e-3, 1, 0.0)
+
+
+def test_the_dither_keeps_the_mean():
+    """A variance that only decays, over 700 steps: to nearest it would stay; dithered it follows beta2^steps."""
+    dev = _dev()
+    n, steps = 256 * 40, 700
+    x = 0.5 + torch.rand(n, generator=torch.Generator().manual_seed(7))
+    codes, scale = ref.to_codes(x, torch.full((n,), 0.5), True)
+    t = _move(dict(params=[torch.zeros(n)], grads=[torch.zeros(n)], m=[torch.zeros(n).to(F8)], v=[codes], m_scales=[torch.zeros(40)],
+                   v_scales=[scale]), dev)
+    value = lambda: (t["v"][0].float().view(-1, 256) * t["v_scales"][0][:, None]).mean().item()
+    before = value()
+    opt = fiona.AdamW(**t, weight_decay=0.0)
+    lr = torch.zeros(1, device=dev)
+    at = torch.arange(1, steps + 1, dtype=torch.int32, device=dev)
+    for i in range(steps):
+        fiona.adamw_step(opt, lr, at[i:i + 1])
+    # sqrt(0.999)^700 = 0.7045.  One rounding moves a value by at most 2^-4 of it, with no mean: after 700 of them over 10240 elements
+    # the mean is off by about 2^-4 sqrt(700 / 10240) = 1.6% at most in a standard deviation; the root of a mean of squares
+    # (the update squares the values) is no issue, as each step's root is linear in the value
+    assert abs(value() / before / 0.999 ** (steps / 2) - 1) <= 0.065
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_gradient_that_is_no_number(bits):
+    dev = _dev()
+    c = _tensors([256 * 3], F32, False, bits, seed=8)
+    t = _move(c, dev)
+    c["grads"][0][300] = float("nan")
+    t["grads"][0][300] = float("nan")
+    fiona.adamw_step(fiona.AdamW(**t, weight_decay=0.05), *_scalars(dev))
+    torch.cuda.synchronize()
+    p = t["params"][0].cpu()
+    assert bool(torch.isnan(p[300])) and int(torch.isnan(p).sum()) == 1
+    m = t["m"][0].float().cpu()
+    if bits == 8:
+        m = m * t["m_scales"][0].cpu().repeat_interleave(256)
+        assert bool(torch.isnan(m[256:512]).all()) and int(torch.isnan(m).sum()) == 256
+    else:
+        assert bool(torch.isnan(m[300])) and int(torch.isnan(m).sum()) == 1
+
+
+def test_several_steps_other_stream_and_graph_replay():
+    dev = _dev()
+    for bits in (32, 8):
+        c = _tensors([513, 4096, 77], BF16, True, bits, seed=9)
+        eager, captured = _move(c, dev), _move(c, dev)
+        a, b = fiona.AdamW(**eager), fiona.AdamW(**captured)
+        lr, step = _scalars(dev, step=1)
+        graph = torch.cuda.CUDAGraph()
+        s = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            fiona.adamw_step(b, lr, step)
+        for i in range(3):
+            step.fill_(i + 1)
+            lr.fill_(1e-3 / (i + 1))
+            torch.cuda.synchronize()
+            with torch.cuda.stream(s):
+                fiona.adamw_step(a, lr, step)
+            s.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            for k in eager:
+                assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(eager[k], captured[k])), (bits, i, k)
+        # parameters that ask for a gradient are taken, as optimisers take them
+        w = torch.nn.Parameter(torch.ones(8, device=dev))
+        z = lambda: torch.zeros(8, device=dev)
+        fiona.adamw_step(fiona.AdamW([w], [torch.ones(8, device=dev)], [z()], [z()], weight_decay=0.0), lr, step)
+        assert bool((w < 1).all())
+
+
+def test_nothing_to_do():
+    dev = _dev()
+    fiona.adamw_step(fiona.AdamW([], [], [], []), *_scalars(dev))
+    e = torch.empty(0, device=dev)
+    fiona.adamw_step(fiona.AdamW([e], [e], [e], [e]), *_scalars(dev))
+
+
+def test_refusals():
+    dev = _dev()
+    z = lambda n=300, dtype=F32: torch.zeros(n, dtype=dtype, device=dev)
+
+    def status(**over):
+        a = dict(params=[z()], grads=[z()], m=[z()], v=[z()])
+        a.update(over)
+        with pytest.raises(fiona.FionaError) as e:
+            fiona.AdamW(**a)
+        return e.value.status
+
+    same = z()
+    assert status(params=[same], grads=[same]) == -5 and status(m=[same], v=[same]) == -5
+    two = z(600)
+    assert status(params=[two[:300], two[299:599]], grads=[z(), z()], m=[z(), z()], v=[z(), z()]) == -5
+    assert status(betas=(1.0, 0.9)) == -1 and status(betas=(0.9, -0.1)) == -1 and status(eps=0.0) == -1 and status(weight_decay=-1.0) == -1
+    assert status(masters=[z()]) == -1                                  # beside 32-bit parameters
+    s = z(2)
+    assert status(m=[z(dtype=F8)], v=[z(dtype=F8)], m_scales=[s], v_scales=[s]) == -5
+    # neighbours in one allocation, and one gradient for two tensors, are no overlap
+    fiona.AdamW([two[:300], two[300:]], [same, same], [z(), z()], [z(), z()])
+    for bad in (dict(m=[z(dtype=F8)], v=[z(dtype=F8)]), dict(grads=[z(299)]), dict(grads=[z(dtype=BF16)]), dict(grads=[]), dict(v=[z(dtype=BF16)]),
+                dict(params=[z(600)[::2]]), dict(m_scales=[s], v_scales=[s]), dict(weight_decay=[0.1, 0.2]), dict(m=[z().cpu()])):
+        a = dict(params=[z()], grads=[z()], m=[z()], v=[z()])
+        a.update(bad)
+        with pytest.raises(ValueError):
+            fiona.AdamW(**a)
+    opt = fiona.AdamW([z()], [z()], [z()], [z()])
+    lr, step = _scalars(dev)
+    for bad in ((lr.double(), step), (lr, step.long()), (lr.cpu(), step), (torch.zeros(2, device=dev), step)):
+        with pytest.raises(ValueError):
+            fiona.adamw_step(opt, *bad)
