@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdint>
 #include <new>
+#include <type_traits>
 
 #include "fiona.h"
 #include "norm_kernel.hpp"
@@ -14,6 +15,7 @@ using namespace fiona_host;
 struct fiona_norm {
   fiona_norm_desc desc{};
   int device = -1;
+  float *part = nullptr;     // parts of dweight and dbias
 };
 
 namespace {
@@ -31,6 +33,45 @@ int check_types(uint32_t type, uint32_t weight_type, uint32_t width) {
   if (!known_type(type) || (weight_type != type && weight_type != FIONA_F32)) return FIONA_ERR_UNSUPPORTED;
   if (!width) return FIONA_ERR_ARG;
   return width > FIONA_MAX_NORM_WIDTH ? FIONA_ERR_UNSUPPORTED : FIONA_OK;
+}
+
+// The wavefronts and pieces that hold rows of q pieces: f(waves, pieces a lane).
+template <int W, int NV>
+struct Shape {
+  static constexpr int kWaves = W, kPieces = NV;
+};
+template <typename F>
+void with_shape(uint32_t q, F f) {
+  if (q <= 64) f(Shape<1, 1>{});
+  else if (q <= 128) f(Shape<1, 2>{});
+  else if (q <= 256) f(Shape<1, 4>{});
+  else if (q <= 512) f(Shape<4, 2>{});
+  else if (q <= 1024) f(Shape<4, 4>{});
+  else if (q <= 2048) f(Shape<16, 2>{});
+  else if (q <= 4096) f(Shape<16, 4>{});
+  else f(Shape<16, 8>{});
+}
+
+// The same in the backward pass, where a lane holds at most 16 elements: it keeps their sums as well.
+template <typename T, typename F>
+void with_grad_shape(uint32_t q, F f) {
+  constexpr bool wide = sizeof(T) == 4;
+  if (q <= 64) f(Shape<1, 1>{});
+  else if (q <= 128) f(Shape<1, 2>{});
+  else if (q <= 256) f(std::conditional_t<wide, Shape<1, 4>, Shape<4, 1>>{});
+  else if (q <= 512) f(Shape<4, 2>{});
+  else if (q <= 1024) f(std::conditional_t<wide, Shape<4, 4>, Shape<16, 1>>{});
+  else if (q <= 2048) f(Shape<16, 2>{});
+  else f(Shape<16, 4>{});
+}
+constexpr uint32_t kMostSums = 16384;   // elements of a row that with_grad_shape's kernels keep sums of
+
+// Parts of the rows' sums.
+constexpr uint32_t kMostParts = 512;
+bool by_columns(uint32_t type, uint32_t d) { return d < 16 / type_size(type) || d > kMostSums; }
+uint32_t parts_of(uint32_t type, uint32_t d, uint32_t n) {
+  const uint32_t most = d > kMostSums ? 64 : kMostParts;
+  return std::max(1u, std::min(most, by_columns(type, d) ? (n + 15) / 16 : n));
 }
 
 }  // namespace
@@ -59,7 +100,19 @@ int fiona_layer_norm(const fiona_norm_args *args, hipStream_t stream) {
   const fiona::NormParams P{A.x, A.residual, A.weight, A.bias, A.y, A.total, A.mean, A.rstd,
                             A.x_row, A.residual_row, A.y_row, A.total_row, A.n, A.width, A.eps};
   with_types(A.type, A.weight_type, [&](auto t, auto v) {
-    hipLaunchKernelGGL((fiona::norm_kernel<decltype(t), decltype(v)>), dim3(A.n), dim3(256), 0, stream, P);
+    using T = decltype(t);
+    using W = decltype(v);
+    constexpr uint32_t E = fiona::kLaneElems<T>;
+    if (A.width < E) {
+      hipLaunchKernelGGL((fiona::norm_narrow_kernel<T, W>), dim3((A.n + 255) / 256), dim3(256), 0, stream, P);
+      return;
+    }
+    with_shape((A.width + E - 1) / E, [&](auto s) {
+      constexpr int WAVES = decltype(s)::kWaves, NV = decltype(s)::kPieces, threads = fiona::kNormThreads<WAVES>;
+      constexpr uint32_t rows = threads / 64 / WAVES;
+      if constexpr (WAVES * 64 * (NV / 2) * E < FIONA_MAX_NORM_WIDTH)
+        hipLaunchKernelGGL((fiona::norm_kernel<T, W, WAVES, NV>), dim3((A.n + rows - 1) / rows), dim3(threads), 0, stream, P);
+    });
   });
   return hipGetLastError() == hipSuccess ? FIONA_OK : FIONA_ERR_HIP;
 }
@@ -79,11 +132,21 @@ int fiona_norm_create(const fiona_norm_desc *desc, fiona_norm **out) {
     delete H;
     return FIONA_ERR_HIP;
   }
+  const uint64_t bytes = (uint64_t)parts_of(desc->type, desc->width, desc->max_rows) * 2 * desc->width * sizeof(float);
+  if (hipMalloc((void **)&H->part, bytes) != hipSuccess) {
+    (void)hipGetLastError();
+    delete H;
+    return FIONA_ERR_NOMEM;
+  }
   *out = H;
   return FIONA_OK;
 }
 
-void fiona_norm_destroy(fiona_norm *norm) { delete norm; }
+void fiona_norm_destroy(fiona_norm *norm) {
+  if (!norm) return;
+  if (norm->part) (void)hipFree(norm->part);
+  delete norm;
+}
 
 int fiona_layer_norm_backward(const fiona_norm *norm, const fiona_norm_backward_args *args, hipStream_t stream) {
   if (!norm || !args) return FIONA_ERR_ARG;
@@ -102,14 +165,32 @@ int fiona_layer_norm_backward(const fiona_norm *norm, const fiona_norm_backward_
   const int rc = check_alias(in, 6, out, 3, own);
   if (rc != FIONA_OK) return rc;
   if (!on_device(norm->device)) return FIONA_ERR_ARG;
-  const fiona::NormGradParams P{A.dy, A.x, A.weight, A.dx_base, A.mean, A.rstd, A.dx, A.dweight, A.dbias,
-                                A.dy_row, A.x_row, A.dx_base_row, A.dx_row, A.n, D.width};
+  const uint32_t parts = parts_of(D.type, D.width, A.n);
+  const fiona::NormGradParams P{A.dy, A.x, A.weight, A.dx_base, A.mean, A.rstd, A.dx, A.dweight, A.dbias, norm->part,
+                                A.dy_row, A.x_row, A.dx_base_row, A.dx_row, A.n, D.width, parts};
+  const bool sums = A.dweight || A.dbias, columns = by_columns(D.type, D.width);
   with_types(D.type, D.weight_type, [&](auto t, auto v) {
     using T = decltype(t);
     using W = decltype(v);
-    if (A.dweight || A.dbias)   // (before dx, which may be dy or x)
-      hipLaunchKernelGGL((fiona::norm_weight_grad_kernel<T, W>), dim3((D.width + 255) / 256), dim3(256), 0, stream, P);
-    if (A.n) hipLaunchKernelGGL((fiona::norm_grad_kernel<T, W>), dim3(A.n), dim3(256), 0, stream, P);
+    constexpr uint32_t E = fiona::kLaneElems<T>;
+    if (sums && columns)    // (before dx, which may be dy or x)
+      hipLaunchKernelGGL(fiona::norm_column_kernel<T>, dim3((D.width + 255) / 256, parts), dim3(256), 0, stream, P);
+    if (D.width < E) {
+      if (A.n) hipLaunchKernelGGL((fiona::norm_narrow_grad_kernel<T, W>), dim3((A.n + 255) / 256), dim3(256), 0, stream, P);
+    } else if (D.width > kMostSums) {
+      constexpr int NV = sizeof(T) == 4 ? 8 : 4;
+      if (A.n) hipLaunchKernelGGL((fiona::norm_grad_kernel<T, W, 16, NV, false>), dim3(std::min(A.n, 65536u)), dim3(1024), 0, stream, P);
+    } else {
+      with_grad_shape<T>((D.width + E - 1) / E, [&](auto s) {
+        constexpr int WAVES = decltype(s)::kWaves, NV = decltype(s)::kPieces, threads = fiona::kNormThreads<WAVES>;
+        constexpr uint32_t rows = threads / 64 / WAVES;
+        if constexpr (WAVES * 64 * NV * E <= kMostSums) {
+          if (sums) hipLaunchKernelGGL((fiona::norm_grad_kernel<T, W, WAVES, NV, true>), dim3(parts), dim3(threads), 0, stream, P);
+          else if (A.n) hipLaunchKernelGGL((fiona::norm_grad_kernel<T, W, WAVES, NV, false>), dim3(std::min((A.n + rows - 1) / rows, 65536u)), dim3(threads), 0, stream, P);
+        }
+      });
+    }
+    if (sums) hipLaunchKernelGGL(fiona::norm_sum_kernel<W>, dim3((2 * D.width + 63) / 64), dim3(1024), 0, stream, P);
   });
   return hipGetLastError() == hipSuccess ? FIONA_OK : FIONA_ERR_HIP;
 }
