@@ -40,7 +40,7 @@ template <int W, int NV>
 struct Shape {
   static constexpr int kWaves = W, kPieces = NV;
 };
-template <typename F>
+template <typename T, typename F>
 void with_shape(uint32_t q, F f) {
   if (q <= 64) f(Shape<1, 1>{});
   else if (q <= 128) f(Shape<1, 2>{});
@@ -49,10 +49,14 @@ void with_shape(uint32_t q, F f) {
   else if (q <= 1024) f(Shape<4, 4>{});
   else if (q <= 2048) f(Shape<16, 2>{});
   else if (q <= 4096) f(Shape<16, 4>{});
-  else f(Shape<16, 8>{});
+  else if constexpr (sizeof(T) == 4) f(Shape<16, 8>{});
 }
 
-// The same in the backward pass, where a lane holds at most 16 elements: it keeps their sums as well.
+// The same in the backward pass with the weights' gradients, where a lane holds at most
+// 16 elements: with their sums, weights and the next row that is a hundred registers
+// (32 elements, rows of 16384, spilled: 413 us for 2048 of them, 353 in 32 bits; a pass
+// over columns takes 38 beside 55 for dx).
+constexpr uint32_t kMostSums = 8192;
 template <typename T, typename F>
 void with_grad_shape(uint32_t q, F f) {
   constexpr bool wide = sizeof(T) == 4;
@@ -60,14 +64,13 @@ void with_grad_shape(uint32_t q, F f) {
   else if (q <= 128) f(Shape<1, 2>{});
   else if (q <= 256) f(std::conditional_t<wide, Shape<1, 4>, Shape<4, 1>>{});
   else if (q <= 512) f(Shape<4, 2>{});
-  else if (q <= 1024) f(std::conditional_t<wide, Shape<4, 4>, Shape<16, 1>>{});
-  else if (q <= 2048) f(Shape<16, 2>{});
-  else f(Shape<16, 4>{});
+  else if (q <= 1024) f(std::conditional_t<wide, Shape<4, 4>, Shape<8, 2>>{});
+  else if constexpr (wide) f(Shape<8, 4>{});
 }
-constexpr uint32_t kMostSums = 16384;   // elements of a row that with_grad_shape's kernels keep sums of
 
 // Parts of the rows' sums.
 constexpr uint32_t kMostParts = 512;
+constexpr uint32_t pitch_of(uint32_t d) { return (d + 3) / 4 * 4; }
 bool by_columns(uint32_t type, uint32_t d) { return d < 16 / type_size(type) || d > kMostSums; }
 uint32_t parts_of(uint32_t type, uint32_t d, uint32_t n) {
   const uint32_t most = d > kMostSums ? 64 : kMostParts;
@@ -107,11 +110,10 @@ int fiona_layer_norm(const fiona_norm_args *args, hipStream_t stream) {
       hipLaunchKernelGGL((fiona::norm_narrow_kernel<T, W>), dim3((A.n + 255) / 256), dim3(256), 0, stream, P);
       return;
     }
-    with_shape((A.width + E - 1) / E, [&](auto s) {
+    with_shape<T>((A.width + E - 1) / E, [&](auto s) {
       constexpr int WAVES = decltype(s)::kWaves, NV = decltype(s)::kPieces, threads = fiona::kNormThreads<WAVES>;
       constexpr uint32_t rows = threads / 64 / WAVES;
-      if constexpr (WAVES * 64 * (NV / 2) * E < FIONA_MAX_NORM_WIDTH)
-        hipLaunchKernelGGL((fiona::norm_kernel<T, W, WAVES, NV>), dim3((A.n + rows - 1) / rows), dim3(threads), 0, stream, P);
+      hipLaunchKernelGGL((fiona::norm_kernel<T, W, WAVES, NV>), dim3((A.n + rows - 1) / rows), dim3(threads), 0, stream, P);
     });
   });
   return hipGetLastError() == hipSuccess ? FIONA_OK : FIONA_ERR_HIP;
@@ -132,7 +134,7 @@ int fiona_norm_create(const fiona_norm_desc *desc, fiona_norm **out) {
     delete H;
     return FIONA_ERR_HIP;
   }
-  const uint64_t bytes = (uint64_t)parts_of(desc->type, desc->width, desc->max_rows) * 2 * desc->width * sizeof(float);
+  const uint64_t bytes = (uint64_t)parts_of(desc->type, desc->width, desc->max_rows) * 2 * pitch_of(desc->width) * sizeof(float);
   if (hipMalloc((void **)&H->part, bytes) != hipSuccess) {
     (void)hipGetLastError();
     delete H;
@@ -167,7 +169,7 @@ int fiona_layer_norm_backward(const fiona_norm *norm, const fiona_norm_backward_
   if (!on_device(norm->device)) return FIONA_ERR_ARG;
   const uint32_t parts = parts_of(D.type, D.width, A.n);
   const fiona::NormGradParams P{A.dy, A.x, A.weight, A.dx_base, A.mean, A.rstd, A.dx, A.dweight, A.dbias, norm->part,
-                                A.dy_row, A.x_row, A.dx_base_row, A.dx_row, A.n, D.width, parts};
+                                A.dy_row, A.x_row, A.dx_base_row, A.dx_row, A.n, D.width, parts, pitch_of(D.width)};
   const bool sums = A.dweight || A.dbias, columns = by_columns(D.type, D.width);
   with_types(D.type, D.weight_type, [&](auto t, auto v) {
     using T = decltype(t);
@@ -175,22 +177,22 @@ int fiona_layer_norm_backward(const fiona_norm *norm, const fiona_norm_backward_
     constexpr uint32_t E = fiona::kLaneElems<T>;
     if (sums && columns)    // (before dx, which may be dy or x)
       hipLaunchKernelGGL(fiona::norm_column_kernel<T>, dim3((D.width + 255) / 256, parts), dim3(256), 0, stream, P);
+    const uint32_t q = (D.width + E - 1) / E;
     if (D.width < E) {
       if (A.n) hipLaunchKernelGGL((fiona::norm_narrow_grad_kernel<T, W>), dim3((A.n + 255) / 256), dim3(256), 0, stream, P);
-    } else if (D.width > kMostSums) {
-      constexpr int NV = sizeof(T) == 4 ? 8 : 4;
-      if (A.n) hipLaunchKernelGGL((fiona::norm_grad_kernel<T, W, 16, NV, false>), dim3(std::min(A.n, 65536u)), dim3(1024), 0, stream, P);
-    } else {
-      with_grad_shape<T>((D.width + E - 1) / E, [&](auto s) {
+    } else if (sums && !columns) {
+      with_grad_shape<T>(q, [&](auto s) {
+        constexpr int WAVES = decltype(s)::kWaves, NV = decltype(s)::kPieces;
+        hipLaunchKernelGGL((fiona::norm_grads_kernel<T, W, WAVES, NV>), dim3(parts), dim3(fiona::kNormThreads<WAVES>), 0, stream, P);
+      });
+    } else if (A.n) {
+      with_shape<T>(q, [&](auto s) {
         constexpr int WAVES = decltype(s)::kWaves, NV = decltype(s)::kPieces, threads = fiona::kNormThreads<WAVES>;
         constexpr uint32_t rows = threads / 64 / WAVES;
-        if constexpr (WAVES * 64 * NV * E <= kMostSums) {
-          if (sums) hipLaunchKernelGGL((fiona::norm_grad_kernel<T, W, WAVES, NV, true>), dim3(parts), dim3(threads), 0, stream, P);
-          else if (A.n) hipLaunchKernelGGL((fiona::norm_grad_kernel<T, W, WAVES, NV, false>), dim3(std::min((A.n + rows - 1) / rows, 65536u)), dim3(threads), 0, stream, P);
-        }
+        hipLaunchKernelGGL((fiona::norm_grad_kernel<T, W, WAVES, NV>), dim3((A.n + rows - 1) / rows), dim3(threads), 0, stream, P);
       });
     }
-    if (sums) hipLaunchKernelGGL(fiona::norm_sum_kernel<W>, dim3((2 * D.width + 63) / 64), dim3(1024), 0, stream, P);
+    if (sums) hipLaunchKernelGGL(fiona::norm_sum_kernel<W>, dim3((2 * P.pitch + 63) / 64), dim3(1024), 0, stream, P);
   });
   return hipGetLastError() == hipSuccess ? FIONA_OK : FIONA_ERR_HIP;
 }

@@ -23,9 +23,9 @@ struct NormGradParams {
   const void *dy, *x, *weight, *dx_base;
   const float *mean, *rstd;
   void *dx, *dweight, *dbias;
-  float *part;               // [parts][2][d]: sums of dy xh and of dy
+  float *part;               // [parts][2][pitch]: sums of dy xh and of dy
   uint64_t dy_row, x_row, dx_base_row, dx_row;
-  uint32_t n, d, parts;
+  uint32_t n, d, parts, pitch;
 };
 
 // Workgroups: four wavefronts, or the sixteen of one group.
@@ -134,97 +134,163 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_kernel(NormParams P)
   }
 }
 
-// dx row by row, and with SUMS this workgroup's part of the weights' gradients, which
-// its lanes add up in registers over the rows they take.
-template <typename T, typename W, int WAVES, int NV, bool SUMS>
+// A lane's elements of u = weight dy and xh.
+template <typename T>
+__device__ __forceinline__ void unpack_grad(u4 x, u4 dy, uint32_t at, uint32_t d, float mean, float rstd, const float (&w)[kLaneElems<T>],
+                                            float (&u)[kLaneElems<T>], float (&xh)[kLaneElems<T>]) {
+  unpack<T>(piece_fix<T>(x, at, d), xh);
+  unpack<T>(piece_fix<T>(dy, at, d), u);
+#pragma unroll
+  for (int j = 0; j < (int)kLaneElems<T>; ++j) xh[j] = (xh[j] - mean) * rstd, u[j] *= w[j];
+}
+
+// A lane's piece of dx.
+template <typename T>
+__device__ __forceinline__ void store_grad(T *dx, uint32_t at, uint32_t d, bool based, u4 base, float rstd, float s1, float s2,
+                                           const float (&u)[kLaneElems<T>], const float (&xh)[kLaneElems<T>]) {
+  constexpr int E = kLaneElems<T>;
+  if (at >= d) return;
+  float v[E], more[E];
+  if (based) unpack<T>(piece_fix<T>(base, at, d), more);
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    v[j] = rstd * (u[j] - s1 - xh[j] * s2);
+    if (based) v[j] += more[j];
+  }
+  store_piece(dx, at, d, pack<T>(v));
+}
+
+// dx alone, a group to a row, which stays packed between the sums and the result.
+template <typename T, typename W, int WAVES, int NV>
 __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grad_kernel(NormGradParams P) {
+  constexpr int E = kLaneElems<T>, GROUPS = kNormThreads<WAVES> / 64 / WAVES;
+  const uint32_t lane = threadIdx.x % (64 * WAVES), d = P.d;
+  uint64_t t = (uint64_t)blockIdx.x * GROUPS + wave_index() / WAVES;
+  if (t >= P.n) return;      // (groups of one wavefront: the others fill their workgroup)
+  const T *x = (const T *)P.x + t * P.x_row, *dy = (const T *)P.dy + t * P.dy_row;
+  const T *base = (const T *)P.dx_base + (P.dx_base ? t * P.dx_base_row : 0);
+  u4 rx[NV], rg[NV], rb[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const uint32_t at = (k * 64 * WAVES + lane) * E;
+    rx[k] = load_once(piece_at(x, at, d)), rg[k] = load_once(piece_at(dy, at, d));
+    if (P.dx_base) rb[k] = load_once(piece_at(base, at, d));
+  }
+  const float mean = P.mean[t], rstd = P.rstd[t];
+  float s1 = 0, s2 = 0;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const uint32_t at = (k * 64 * WAVES + lane) * E;
+    float w[E], u[E], xh[E];
+    load_weights<T, W>(P.weight, at, d, 1.f, w);
+    unpack_grad<T>(rx[k], rg[k], at, d, mean, rstd, w, u, xh);
+#pragma unroll
+    for (int j = 0; j < E; ++j) s1 += u[j], s2 += u[j] * xh[j];
+  }
+  group_sum<WAVES>(s1, s2, 0);
+  s1 /= d, s2 /= d;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const uint32_t at = (k * 64 * WAVES + lane) * E;
+    float w[E], u[E], xh[E];
+    load_weights<T, W>(P.weight, at, d, 1.f, w);
+    unpack_grad<T>(rx[k], rg[k], at, d, mean, rstd, w, u, xh);
+    store_grad((T *)P.dx + t * P.dx_row, at, d, P.dx_base, rb[k], rstd, s1, s2, u, xh);
+  }
+}
+
+// dx of every gridDim-th group's row, and this workgroup's part of the weights'
+// gradients, which its lanes add up in registers over those rows.
+template <typename T, typename W, int WAVES, int NV>
+__global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grads_kernel(NormGradParams P) {
   constexpr int E = kLaneElems<T>, GROUPS = kNormThreads<WAVES> / 64 / WAVES;
   const uint32_t lane = threadIdx.x % (64 * WAVES), group = wave_index() / WAVES, d = P.d;
   const float per = 1.f / d;
-  float w[NV][E], dw[SUMS ? NV : 1][E], db[SUMS ? NV : 1][E];
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    load_weights<T, W>(P.weight, (k * 64 * WAVES + lane) * E, d, 1.f, w[k]);
-    if (SUMS)
-#pragma unroll
-      for (int j = 0; j < E; ++j) dw[k][j] = db[k][j] = 0;
-  }
   const uint64_t step = (uint64_t)gridDim.x * GROUPS;
-  uint32_t slot = 0;
-  // (a group without a row at the end goes along with the last one, for the barriers)
-  for (uint64_t first = (uint64_t)blockIdx.x * GROUPS; first < P.n; first += step, slot ^= 1) {
-    const bool live = first + group < P.n;
-    const uint64_t t = live ? first + group : P.n - 1;
+  // The next row is on its way while one is computed (a group without a row at the
+  // end goes along with the last one).
+  u4 rx[NV], rg[NV], rb[NV];
+  float mean = 0, rstd = 0;
+  auto load = [&](uint64_t t) {
+    t = t < P.n ? t : P.n - 1;
     const T *x = (const T *)P.x + t * P.x_row, *dy = (const T *)P.dy + t * P.dy_row;
     const T *base = (const T *)P.dx_base + (P.dx_base ? t * P.dx_base_row : 0);
-    u4 rx[NV], rg[NV], rb[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const uint32_t at = (k * 64 * WAVES + lane) * E;
       rx[k] = load_once(piece_at(x, at, d)), rg[k] = load_once(piece_at(dy, at, d));
       if (P.dx_base) rb[k] = load_once(piece_at(base, at, d));
     }
-    const float mean = P.mean[t], rstd = P.rstd[t];
+    mean = P.mean[t], rstd = P.rstd[t];
+  };
+  uint64_t first = (uint64_t)blockIdx.x * GROUPS;
+  if (first < P.n) load(first + group);
+  float w[NV][E], dw[NV][E], db[NV][E];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    load_weights<T, W>(P.weight, (k * 64 * WAVES + lane) * E, d, 1.f, w[k]);
+#pragma unroll
+    for (int j = 0; j < E; ++j) dw[k][j] = db[k][j] = 0;
+  }
+  for (uint32_t slot = 0; first < P.n; first += step, slot ^= 1) {
+    const bool live = first + group < P.n;
+    const uint64_t t = first + group;
+    const float m = mean, r = rstd;
     float s1 = 0, s2 = 0;
     float xh[NV][E], g[NV][E];
+    u4 add[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const uint32_t at = (k * 64 * WAVES + lane) * E;
       unpack<T>(piece_fix<T>(rx[k], at, d), xh[k]);
       unpack<T>(piece_fix<T>(rg[k], at, d), g[k]);
+      add[k] = rb[k];
+    }
+    if (first + step < P.n) load(t + step);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        xh[k][j] = (xh[k][j] - mean) * rstd;
-        if (SUMS && live) dw[k][j] += g[k][j] * xh[k][j], db[k][j] += g[k][j];
+        xh[k][j] = (xh[k][j] - m) * r;
+        if (live) dw[k][j] += g[k][j] * xh[k][j], db[k][j] += g[k][j];
         g[k][j] *= w[k][j];
         s1 += g[k][j], s2 += g[k][j] * xh[k][j];
       }
-    }
     group_sum<WAVES>(s1, s2, slot);
     if (!live) continue;
-    s1 *= per, s2 *= per;
-    T *dx = (T *)P.dx + t * P.dx_row;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const uint32_t at = (k * 64 * WAVES + lane) * E;
-      if (at >= d) continue;
-      float add[E];
-      if (P.dx_base) unpack<T>(piece_fix<T>(rb[k], at, d), add);
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        const float v = rstd * (g[k][j] - s1 - xh[k][j] * s2);
-        g[k][j] = P.dx_base ? add[j] + v : v;
-      }
-      store_piece(dx, at, d, pack<T>(g[k]));
-    }
+    for (int k = 0; k < NV; ++k)
+      store_grad((T *)P.dx + t * P.dx_row, (k * 64 * WAVES + lane) * E, d, P.dx_base, add[k], r, s1 * per, s2 * per, g[k], xh[k]);
   }
-  if constexpr (SUMS) {
-    // The groups' sums one after another through LDS, then this workgroup's part.
-    float *part = P.part + (uint64_t)blockIdx.x * 2 * d;
-    if constexpr (GROUPS > 1) {
-      __shared__ float sh[2][64 * WAVES * NV * E];
-      for (int q = 0; q < GROUPS; ++q) {
-        if (group == (uint32_t)q)
+  // This workgroup's part: its groups' sums, through LDS.
+  float *part = P.part + (uint64_t)blockIdx.x * 2 * P.pitch;
+  if constexpr (GROUPS > 1) {
+    __shared__ f4 sh[GROUPS][2][64 * WAVES * NV * E / 4];
 #pragma unroll
-          for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-              const uint32_t at = (k * 64 * WAVES + lane) * E + j;
-              sh[0][at] = q ? sh[0][at] + dw[k][j] : dw[k][j];
-              sh[1][at] = q ? sh[1][at] + db[k][j] : db[k][j];
-            }
-        __syncthreads();
+      for (int j = 0; j < E; j += 4) {
+        const uint32_t at = ((k * 64 * WAVES + lane) * E + j) / 4;
+        sh[group][0][at] = (f4){dw[k][j], dw[k][j + 1], dw[k][j + 2], dw[k][j + 3]};
+        sh[group][1][at] = (f4){db[k][j], db[k][j + 1], db[k][j + 2], db[k][j + 3]};
       }
-      for (uint32_t i = threadIdx.x; i < d; i += kNormThreads<WAVES>) part[i] = sh[0][i], part[d + i] = sh[1][i];
-    } else {
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < d; i += kNormThreads<WAVES>) {
+      float a = 0, b = 0;
 #pragma unroll
-      for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-          const uint32_t at = (k * 64 * WAVES + lane) * E + j;
-          if (at < d) part[at] = dw[k][j], part[d + at] = db[k][j];
-        }
+      for (int q = 0; q < GROUPS; ++q) a += ((const float *)sh[q][0])[i], b += ((const float *)sh[q][1])[i];
+      part[i] = a, part[P.pitch + i] = b;
     }
+  } else {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int j = 0; j < E; j += 4) {
+        const uint32_t at = (k * 64 * WAVES + lane) * E + j;
+        if (at >= d) continue;      // (the pitch is in whole steps of 4)
+        *(f4 *)(part + at) = (f4){dw[k][j], dw[k][j + 1], dw[k][j + 2], dw[k][j + 3]};
+        *(f4 *)(part + P.pitch + at) = (f4){db[k][j], db[k][j + 1], db[k][j + 2], db[k][j + 3]};
+      }
   }
 }
 
@@ -233,7 +299,7 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grad_kernel(NormGrad
 template <typename W>
 __global__ void __launch_bounds__(1024) norm_sum_kernel(NormGradParams P) {
   __shared__ float sh[16][64];
-  const uint32_t i = blockIdx.x * 64 + threadIdx.x % 64, w = wave_index(), columns = 2 * P.d;
+  const uint32_t i = blockIdx.x * 64 + threadIdx.x % 64, w = wave_index(), columns = 2 * P.pitch;
   float s = 0;
   if (i < columns) {
 #pragma unroll 8
@@ -245,8 +311,9 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(NormGradParams P) {
   s = 0;
 #pragma unroll
   for (int k = 0; k < 16; ++k) s += sh[k][threadIdx.x];
-  W *out = (W *)(i < P.d ? P.dweight : P.dbias);
-  if (out) out[i < P.d ? i : i - P.d] = (W)s;
+  W *out = (W *)(i < P.pitch ? P.dweight : P.dbias);
+  const uint32_t c = i < P.pitch ? i : i - P.pitch;
+  if (out && c < P.d) out[c] = (W)s;
 }
 
 // Rows shorter than a piece, or too long for their sums to stay in registers: a part of
@@ -261,8 +328,8 @@ __global__ void __launch_bounds__(256) norm_column_kernel(NormGradParams P) {
     dw += dy * (((float)((const T *)P.x)[t * P.x_row + i] - P.mean[t]) * P.rstd[t]);
     db += dy;
   }
-  float *part = P.part + (uint64_t)blockIdx.y * 2 * P.d;
-  part[i] = dw, part[P.d + i] = db;
+  float *part = P.part + (uint64_t)blockIdx.y * 2 * P.pitch;
+  part[i] = dw, part[P.pitch + i] = db;
 }
 
 // Rows shorter than a piece: a thread to a row.
