@@ -615,6 +615,7 @@ int fiona_adapter_backward(const fiona_adapters *adapters, const fiona_adapter_a
  * statistics, one rounding of each result, sums in a fixed order.
  * ------------------------------------------------------------------------ */
 #define FIONA_MAX_NORM_WIDTH 32768u
+#define FIONA_MAX_NORM_ROWS (1u << 22)
 
 /*
  * fiona_layer_norm: with s_t = x_t, or x_t + residual_t rounded to the type,
@@ -626,7 +627,7 @@ int fiona_adapter_backward(const fiona_adapters *adapters, const fiona_adapter_a
  *   y, total      device, [n][width]; total receives s, or is NULL.  y or total may be x or residual
  *                 itself (same pointer and stride), but not both the same
  *   mean, rstd    device, [n] float32, or NULL
- *   eps > 0; width at most FIONA_MAX_NORM_WIDTH
+ *   eps > 0; width at most FIONA_MAX_NORM_WIDTH, n at most FIONA_MAX_NORM_ROWS
  * Asynchronous on stream; one kernel launch, allocates nothing.  Errors
  * (nothing is launched): FIONA_ERR_ARG, FIONA_ERR_UNSUPPORTED, FIONA_ERR_ALIGN,
  * FIONA_ERR_ALIAS, FIONA_ERR_HIP.
@@ -690,7 +691,7 @@ int fiona_layer_norm_backward(const fiona_norm *norm, const fiona_norm_backward_
  *
  * fiona_token_loss_create: the workspace of calls of up to max_tokens tokens and
  * max_pairs pairs (0: none) of vocab logits.  Limits: vocab, max_tokens and
- * max_pairs at most 2^22.
+ * max_pairs at most 2^21.
  *
  * fiona_preference_loss: sequence s has tokens offsets[s] to offsets[s + 1] - 1;
  * sequence 2 p is the preferred one of pair p, 2 p + 1 the other.  With L_s the sum

@@ -62,7 +62,7 @@ int check_tensors(const fiona_adamw_desc &D, uint64_t &chunks) {
     add(T.m, T.n * s, true), add(T.v, T.n * s, true), add(T.m_scale, blocks * 4, true), add(T.v_scale, blocks * 4, true);
     chunks += (blocks + fiona::kChunkBlocks - 1) / fiona::kChunkBlocks;
   }
-  if (chunks >= (uint64_t)1 << 31) return FIONA_ERR_UNSUPPORTED;
+  if (chunks >= 1u << 24) return FIONA_ERR_UNSUPPORTED;   // (times 256 threads: below 2^32)
   return pieces_overlap(pieces) ? FIONA_ERR_ALIAS : FIONA_OK;
 }
 

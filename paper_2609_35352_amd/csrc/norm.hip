@@ -88,7 +88,7 @@ int fiona_layer_norm(const fiona_norm_args *args, hipStream_t stream) {
   if (rc != FIONA_OK) return rc;
   if (!(A.eps > 0) || !std::isfinite(A.eps)) return FIONA_ERR_ARG;
   if (!A.n) return FIONA_OK;
-  if (A.n > (1u << 30)) return FIONA_ERR_UNSUPPORTED;
+  if (A.n > FIONA_MAX_NORM_ROWS) return FIONA_ERR_UNSUPPORTED;
   if (!A.x || !A.y) return FIONA_ERR_ARG;
   const uint64_t e = type_size(A.type), w = type_size(A.weight_type), n = A.n, d = A.width;
   if (misaligned(A.x, e) || misaligned(A.residual, e) || misaligned(A.y, e) || misaligned(A.total, e) ||
@@ -126,7 +126,7 @@ int fiona_norm_create(const fiona_norm_desc *desc, fiona_norm **out) {
   const int rc = check_types(desc->type, desc->weight_type, desc->width);
   if (rc != FIONA_OK) return rc;
   if (!desc->max_rows) return FIONA_ERR_ARG;
-  if (desc->max_rows > (1u << 30)) return FIONA_ERR_UNSUPPORTED;
+  if (desc->max_rows > FIONA_MAX_NORM_ROWS) return FIONA_ERR_UNSUPPORTED;
   fiona_norm *H = new (std::nothrow) fiona_norm;
   if (!H) return FIONA_ERR_NOMEM;
   H->desc = *desc;

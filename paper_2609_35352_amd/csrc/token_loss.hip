@@ -2,9 +2,11 @@
 // logits and their gradients.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <new>
+#include <type_traits>
 
 #include "fiona.h"
 #include "rows.hpp"
@@ -15,12 +17,13 @@ using namespace fiona_host;
 struct fiona_token_loss {
   fiona_token_loss_desc desc{};
   int device = -1;
-  float *ws = nullptr;     // [3][max_tokens]: log sums, log-probabilities, derivatives
+  char *ws = nullptr;      // parts of rows, then [3][max_tokens]: logits, log sums, derivatives
+  uint64_t part_cap = 0;   // parts that fit
 };
 
 namespace {
 
-constexpr uint32_t kMost = 1u << 22;   // vocab, tokens, pairs
+constexpr uint32_t kMost = 1u << 21;   // vocab, tokens, pairs (times 1024 threads: below 2^32)
 
 // Checks what both calls share.
 int check_logits(const fiona_token_loss *H, uint32_t n, const void *logits, const void *dlogits, const int32_t *targets,
@@ -33,14 +36,65 @@ int check_logits(const fiona_token_loss *H, uint32_t n, const void *logits, cons
   return FIONA_OK;
 }
 
+// Parts of each of n rows of `pieces` pieces: enough workgroups to fill the GPU, none
+// below 256 pieces (one for each of its threads).
+constexpr uint32_t kWorkgroups = 1024;
+uint32_t splits_of(uint32_t n, uint32_t pieces) {
+  n = std::max(1u, n);
+  return std::max(1u, std::min({(kWorkgroups + n - 1) / n, (pieces + 255) / 256, fiona::kLossSplits}));
+}
+
+uint32_t pieces_of(const fiona_token_loss_desc &D) {
+  const uint32_t e = 16 / type_size(D.type);
+  return (D.vocab + e - 1) / e;
+}
+
 fiona::TokenParams params(const fiona_token_loss *H, uint32_t n, const void *logits, void *dlogits, const int32_t *targets,
                           uint64_t logits_row, uint64_t dlogits_row) {
   fiona::TokenParams P{};
   P.z = logits, P.dz = dlogits, P.targets = targets, P.z_row = logits_row, P.dz_row = dlogits_row;
   P.n_tok = n, P.vocab = H->desc.vocab;
-  P.lse = H->ws, P.logp = H->ws + H->desc.max_tokens, P.coef = P.logp + H->desc.max_tokens;
+  P.part = (float2 *)H->ws, P.at_target = (float *)(P.part + H->part_cap);
+  P.lse = P.at_target + H->desc.max_tokens, P.coef = P.lse + H->desc.max_tokens;
+  const uint32_t pieces = pieces_of(H->desc);
+  P.slice = (pieces + splits_of(n, pieces) - 1) / splits_of(n, pieces);
+  P.splits = (pieces + P.slice - 1) / P.slice;
   return P;
 }
+
+// Calls f with whether rows are shorter than a piece.
+template <typename T, typename F>
+void with_width(uint32_t vocab, F f) {
+  if (vocab < fiona::kLaneElems<T>) f(std::true_type{});
+  else f(std::false_type{});
+}
+
+template <typename T>
+void launch_stats(const fiona::TokenParams &P, hipStream_t stream) {
+  with_width<T>(P.vocab, [&](auto narrow) {
+    hipLaunchKernelGGL((fiona::token_stats_kernel<T, decltype(narrow)::value>), dim3(P.n_tok, P.splits), dim3(256), 0, stream, P);
+  });
+}
+
+template <typename T, bool POLICY>
+void launch_grad(const fiona::TokenParams &P, const fiona::PolicyParams &Q, hipStream_t stream) {
+  with_width<T>(P.vocab, [&](auto narrow) {
+    hipLaunchKernelGGL((fiona::token_grad_kernel<T, decltype(narrow)::value, POLICY>), dim3(P.n_tok, P.dz ? P.splits : 1), dim3(256), 0,
+                       stream, P, Q, P.slice);
+  });
+}
+
+// The policy loss with whole rows in registers.
+template <typename T>
+void launch_rows(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint32_t pieces, hipStream_t stream) {
+  const dim3 grid(P.n_tok);
+  if (pieces <= 256 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 256, 4>), grid, dim3(256), 0, stream, P, Q);
+  else if (pieces <= 512 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 512, 4>), grid, dim3(512), 0, stream, P, Q);
+  else if (pieces <= 1024 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 4>), grid, dim3(1024), 0, stream, P, Q);
+  else if (pieces <= 1024 * 8) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 8>), grid, dim3(1024), 0, stream, P, Q);
+  else hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 16>), grid, dim3(1024), 0, stream, P, Q);
+}
+constexpr uint32_t kRowPieces = 1024 * 16;
 
 }  // namespace
 
@@ -61,7 +115,8 @@ int fiona_token_loss_create(const fiona_token_loss_desc *desc, fiona_token_loss 
     delete H;
     return FIONA_ERR_HIP;
   }
-  if (hipMalloc((void **)&H->ws, (uint64_t)D.max_tokens * 3 * sizeof(float)) != hipSuccess) {
+  H->part_cap = (uint64_t)D.max_tokens + kWorkgroups;     // (n rounded-up quotients of kWorkgroups / n, or 64 of few rows)
+  if (hipMalloc((void **)&H->ws, H->part_cap * sizeof(float2) + (uint64_t)D.max_tokens * 3 * sizeof(float)) != hipSuccess) {
     (void)hipGetLastError();
     delete H;
     return FIONA_ERR_NOMEM;
@@ -99,9 +154,11 @@ int fiona_preference_loss(const fiona_token_loss *H, const fiona_preference_args
   const fiona::PairParams Q{A.offsets, A.reference, A.weights, A.loss, A.logps, A.beta, A.label_smoothing, A.n_pair};
   with_type(H->desc.type, [&](auto t) {
     using T = decltype(t);
-    if (A.n_tok) hipLaunchKernelGGL((fiona::token_stats_kernel<T, false>), dim3(A.n_tok), dim3(256), 0, stream, P, fiona::PolicyParams{});
-    if (A.n_pair) hipLaunchKernelGGL(fiona::pair_kernel, dim3(A.n_pair), dim3(256), 0, stream, P, Q);
-    if (A.n_tok && A.dlogits) hipLaunchKernelGGL(fiona::token_grad_kernel<T>, dim3(A.n_tok), dim3(256), 0, stream, P);
+    if (A.n_tok) launch_stats<T>(P, stream);
+    uint32_t lanes = 1;
+    while (lanes < P.splits) lanes *= 2;
+    if (A.n_pair) hipLaunchKernelGGL(fiona::pair_kernel, dim3(A.n_pair), dim3(1024), 0, stream, P, Q, lanes);
+    if (A.n_tok && A.dlogits) launch_grad<T, false>(P, fiona::PolicyParams{}, stream);
   });
   return hipGetLastError() == hipSuccess ? FIONA_OK : FIONA_ERR_HIP;
 }
@@ -132,8 +189,13 @@ int fiona_policy_loss(const fiona_token_loss *H, const fiona_policy_args *args, 
                               A.clip_low, A.clip_high, A.kl};
   with_type(H->desc.type, [&](auto t) {
     using T = decltype(t);
-    hipLaunchKernelGGL((fiona::token_stats_kernel<T, true>), dim3(A.n_tok), dim3(256), 0, stream, P, Q);
-    if (A.dlogits) hipLaunchKernelGGL(fiona::token_grad_kernel<T>, dim3(A.n_tok), dim3(256), 0, stream, P);
+    const uint32_t pieces = pieces_of(H->desc);
+    if (A.dlogits && pieces <= kRowPieces && P.vocab >= fiona::kLaneElems<T>) {
+      launch_rows<T>(P, Q, pieces, stream);
+      return;
+    }
+    launch_stats<T>(P, stream);
+    launch_grad<T, true>(P, Q, stream);
   });
   return hipGetLastError() == hipSuccess ? FIONA_OK : FIONA_ERR_HIP;
 }

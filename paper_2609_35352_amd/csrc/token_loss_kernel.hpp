@@ -1,17 +1,29 @@
 // Kernels of fiona_preference_loss and fiona_policy_loss.
+//
+// A row's log sum of exponentials in parts, as a softmax over a long axis: a part with
+// elements J has m_J = max z_j and s_J = sum exp(z_j - m_J), and two parts join as
+// m = max(m_1, m_2), s = sum_i s_i exp(m_i - m).  Exponentials are to base 2, of the
+// difference of two logits, taken before it is scaled.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "pieces.hpp"
+
 namespace fiona {
+
+constexpr float kLossLog2e = 1.4426950408889634f, kLossLn2 = 0.6931471805599453f;
+constexpr uint32_t kLossSplits = 64;   // parts of one row
 
 struct TokenParams {
   const void *z;
   void *dz;
   const int32_t *targets;
-  float *lse, *logp, *coef;       // [n_tok]: log sum of exponentials, log-probability, derivative of the loss
+  float2 *part;                   // [n_tok][splits]: maximum and sum of a part of a row
+  float *at_target, *lse, *coef;  // [n_tok]: the target's logit, log sum of exponentials, derivative of the loss
   uint64_t z_row, dz_row;
   uint32_t n_tok, vocab;
+  uint32_t splits, slice;         // parts of a row, and their pieces
 };
 
 struct PairParams {
@@ -28,24 +40,6 @@ struct PolicyParams {
   float clip_low, clip_high, kl;
 };
 
-__device__ __forceinline__ float max_256(float a) {
-  __shared__ float part[4];
-  for (int k = 32; k; k >>= 1) a = fmaxf(a, __shfl_xor(a, k));
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = a;
-  __syncthreads();
-  return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-}
-template <typename F>
-__device__ __forceinline__ F add_256(F a) {
-  __shared__ F part[4];
-  for (int k = 32; k; k >>= 1) a += __shfl_xor(a, k);
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = a;
-  __syncthreads();
-  return part[0] + part[1] + (part[2] + part[3]);
-}
-
 // The policy loss of a token with log-probability l, and its derivative.
 __device__ __forceinline__ float policy_of(const PolicyParams &Q, uint32_t n_tok, uint32_t t, float l, float &loss) {
   const float w = Q.weights ? Q.weights[t] : 1.f / n_tok, a = Q.advantages[t], r = expf(l - Q.old[t]);
@@ -61,55 +55,156 @@ __device__ __forceinline__ float policy_of(const PolicyParams &Q, uint32_t n_tok
   return w * c;
 }
 
-// A workgroup to a token: its log-probability, and with POLICY its loss.
-template <typename T, bool POLICY>
-__global__ void __launch_bounds__(256) token_stats_kernel(TokenParams P, PolicyParams Q) {
-  const uint32_t t = blockIdx.x;
-  const int32_t y = P.targets[t];
-  float l = 0, lse = 0;
-  const bool live = y >= 0 && (uint32_t)y < P.vocab;
-  const T *z = (const T *)P.z + t * P.z_row;
-  if (live) {
-    float m = -INFINITY, s = 0;
-    for (uint32_t i = threadIdx.x; i < P.vocab; i += 256) m = fmaxf(m, (float)z[i]);
-    m = max_256(m);
-    const float ms = m == -INFINITY ? 0.f : m;
-    for (uint32_t i = threadIdx.x; i < P.vocab; i += 256) s += expf((float)z[i] - ms);
-    lse = ms + logf(add_256(s));
-    l = (float)z[y] - lse;
-  }
-  if (threadIdx.x) return;
-  P.lse[t] = lse, P.logp[t] = l;
-  if (POLICY) {
-    float loss = 0;
-    P.coef[t] = live ? policy_of(Q, P.n_tok, t, l, loss) : 0.f;
-    Q.loss[t] = loss, Q.logps[t] = l;
+__device__ __forceinline__ bool counts(int32_t target, uint32_t vocab) { return target >= 0 && (uint32_t)target < vocab; }
+
+// A lane's piece of a row of n elements.  NARROW: rows shorter than a piece.
+template <typename T, bool NARROW>
+__device__ __forceinline__ u4 read_piece(const T *row, uint32_t at, uint32_t n) {
+  if constexpr (!NARROW) {
+    return load_shared(piece_at(row, at, n));
   } else {
-    P.coef[t] = 0;          // (of a token in no sequence)
+    uint32_t w[4];
+    load_row<T, kLaneElems<T>, false>(row, at ? 0 : (int)n, w);
+    return (u4){w[0], w[1], w[2], w[3]};
   }
 }
 
+// The elements of such a piece, -inf from the row's end on.  whole: it is known to end before.
+template <typename T, bool NARROW>
+__device__ __forceinline__ void logits_of(u4 v, uint32_t at, uint32_t n, float (&x)[kLaneElems<T>], bool whole = false) {
+  if (whole || at + kLaneElems<T> <= n) {
+    unpack<T>(v, x);
+    return;
+  }
+  unpack<T>(NARROW ? v : piece_fix<T>(v, at, n), x);
+#pragma unroll
+  for (int j = 0; j < (int)kLaneElems<T>; ++j)
+    if (at + j >= n) x[j] = -INFINITY;
+}
+
+// Adds elements to a running maximum and sum of exponentials.
+template <int N>
+__device__ __forceinline__ void gather(const float (&x)[N], float &m, float &s) {
+  float top = m;
+#pragma unroll
+  for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
+  const float ms = top == -INFINITY ? 0.f : top;
+  float more[4] = {s * __builtin_amdgcn_exp2f((m - ms) * kLossLog2e), 0, 0, 0};   // (four chains of additions)
+#pragma unroll
+  for (int j = 0; j < N; ++j) more[j % 4] += __builtin_amdgcn_exp2f((x[j] - ms) * kLossLog2e);
+  s = more[0] + more[1] + (more[2] + more[3]);
+  m = top;
+}
+
+// Four pieces of a row, 256 of them apart, for a lane whose first one starts at `at`.
+// Steps that end before the row does (`whole`, the same in the workgroup) need no checks.
+template <typename T, bool NARROW>
+__device__ __forceinline__ void read_step(const T *row, uint32_t at, uint32_t n, bool whole, u4 (&v)[4]) {
+  if (whole) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = load_shared(row + at + u * 256 * kLaneElems<T>);
+  } else {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = read_piece<T, NARROW>(row, at + u * 256 * kLaneElems<T>, n);
+  }
+}
+
+// Parts held by the lanes of a wavefront joined, the same in each.
+__device__ __forceinline__ void join_wave(float &m, float &s) {
+  const float top = wave_max(m), ms = top == -INFINITY ? 0.f : top;
+  s = wave_sum(s * __builtin_amdgcn_exp2f((m - ms) * kLossLog2e));
+  m = top;
+}
+__device__ __forceinline__ float log_sum(float m, float s) { return (m == -INFINITY ? 0.f : m) + kLossLn2 * __builtin_amdgcn_logf(s); }
+
+// A workgroup to a part of a token's row.
+template <typename T, bool NARROW>
+__global__ void __launch_bounds__(256) token_stats_kernel(TokenParams P) {
+  constexpr int E = kLaneElems<T>, U = 4;
+  const uint32_t t = blockIdx.x, split = blockIdx.y;
+  const int32_t y = P.targets[t];
+  if (split == 0 && threadIdx.x == 0) P.coef[t] = 0;          // (of a token in no sequence)
+  if (!counts(y, P.vocab)) return;
+  const T *z = (const T *)P.z + t * P.z_row;
+  constexpr uint32_t STEP = U * 256 * E;
+  const uint32_t start = split * P.slice * E, end = min(start + P.slice * E, P.vocab);
+  u4 v[U];
+  read_step<T, NARROW>(z, start + threadIdx.x * E, P.vocab, start + STEP <= end, v);
+  float zt = 0;
+  if (split == 0 && threadIdx.x == 0) zt = (float)z[y];
+  float m = -INFINITY, s = 0;
+  for (uint32_t base = start; base < end; base += STEP) {
+    const uint32_t at = base + threadIdx.x * E;
+    const bool whole = base + STEP <= end;
+    float x[U * E];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float e[E];
+      logits_of<T, NARROW>(v[u], at + u * 256 * E, end, e, whole);
+#pragma unroll
+      for (int j = 0; j < E; ++j) x[u * E + j] = e[j];
+    }
+    if (base + STEP < end) read_step<T, NARROW>(z, at + STEP, P.vocab, base + 2 * STEP <= end, v);
+    gather(x, m, s);
+  }
+  join_wave(m, s);
+  __shared__ float2 part[4];
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = {m, s};
+  __syncthreads();
+  if (threadIdx.x) return;
+  const float top = fmaxf(fmaxf(part[0].x, part[1].x), fmaxf(part[2].x, part[3].x)), ms = top == -INFINITY ? 0.f : top;
+  s = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s += part[i].y * __builtin_amdgcn_exp2f((part[i].x - ms) * kLossLog2e);
+  P.part[(uint64_t)t * P.splits + split] = {top, s};
+  if (split == 0) P.at_target[t] = zt;
+}
+
 // A workgroup to a pair: its sequences' sums, its loss, and their tokens' derivatives.
-__global__ void __launch_bounds__(256) pair_kernel(TokenParams P, PairParams Q) {
+// `lanes`, a power of two, share a token's parts.
+__global__ void __launch_bounds__(1024) pair_kernel(TokenParams P, PairParams Q, uint32_t lanes) {
+  const uint32_t lane = threadIdx.x % lanes;
+  __shared__ double sh[2][16];
   const uint32_t p = blockIdx.x;
   double sum[2];
   int32_t first[2], last[2];
+#pragma unroll
   for (int k = 0; k < 2; ++k) {
     first[k] = min(max(Q.offsets[2 * p + k], 0), (int32_t)P.n_tok);
     last[k] = min(max(Q.offsets[2 * p + k + 1], 0), (int32_t)P.n_tok);
-    double s = 0;
-    for (int32_t t = first[k] + (int32_t)threadIdx.x; t < last[k]; t += 256) s += P.logp[t];
-    sum[k] = add_256(s);
+    sum[k] = 0;
+    for (int32_t t = first[k] + (int32_t)(threadIdx.x / lanes); t < last[k]; t += 1024 / lanes) {
+      if (!counts(P.targets[t], P.vocab)) continue;
+      float m = -INFINITY, s = 0;
+      if (lane < P.splits) {
+        const float2 part = P.part[(uint64_t)t * P.splits + lane];
+        m = part.x, s = part.y;
+      }
+      const float zt = P.at_target[t];
+      float top = m;
+      for (uint32_t i = 1; i < lanes; i *= 2) top = fmaxf(top, __shfl_xor(top, i));
+      s *= __builtin_amdgcn_exp2f((m - (top == -INFINITY ? 0.f : top)) * kLossLog2e);
+      for (uint32_t i = 1; i < lanes; i *= 2) s += __shfl_xor(s, i);
+      const float lse = log_sum(top, s);
+      if (lane) continue;
+      P.lse[t] = lse;
+      sum[k] += zt - lse;
+    }
+    for (int i = 32; i; i >>= 1) sum[k] += __shfl_xor(sum[k], i);
+    if (threadIdx.x % 64 == 0) sh[k][threadIdx.x / 64] = sum[k];
   }
+  __syncthreads();
+  sum[0] = sum[1] = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sum[0] += sh[0][i], sum[1] += sh[1][i];
   const double h = Q.beta * ((sum[0] - Q.reference[2 * p]) - (sum[1] - Q.reference[2 * p + 1]));
   const double w = Q.weights ? Q.weights[p] : 1. / Q.n_pair, e = Q.smoothing, x = exp(-fabs(h)), big = 1 / (1 + x), small = x / (1 + x);
   const double up = h >= 0 ? big : small, down = h >= 0 ? small : big;      // sigmoid(h), sigmoid(-h)
   const float g = w == 0 ? 0.f : (float)(w * Q.beta * (e * up - (1 - e) * down));
+#pragma unroll
   for (int k = 0; k < 2; ++k)
-    for (int32_t t = first[k] + (int32_t)threadIdx.x; t < last[k]; t += 256) {
-      const int32_t y = P.targets[t];
-      P.coef[t] = y >= 0 && (uint32_t)y < P.vocab ? (k ? -g : g) : 0.f;
-    }
+    for (int32_t t = first[k] + (int32_t)threadIdx.x; t < last[k]; t += 1024)
+      if (counts(P.targets[t], P.vocab)) P.coef[t] = k ? -g : g;
   if (threadIdx.x) return;
   // -log sigmoid(h) = log(1 + exp(-|h|)) + max(-h, 0)
   const double loss = log1p(x) + (h < 0 ? (1 - e) * -h : e > 0 && h > 0 ? e * h : 0.);
@@ -117,17 +212,129 @@ __global__ void __launch_bounds__(256) pair_kernel(TokenParams P, PairParams Q) 
   Q.logps[2 * p] = (float)sum[0], Q.logps[2 * p + 1] = (float)sum[1];
 }
 
-// A workgroup to a token: its row of the gradient.
-template <typename T>
-__global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P) {
-  const uint32_t t = blockIdx.x;
-  const float c = P.coef[t], lse = P.lse[t];
+// c (onehot(y) - softmax(z)) of a lane's piece.
+template <typename T, bool NARROW>
+__device__ __forceinline__ u4 gradient_of(u4 v, uint32_t at, uint32_t n, int32_t y, float c, float lse, bool whole = false) {
+  constexpr int E = kLaneElems<T>;
+  float x[E];
+  logits_of<T, NARROW>(v, at, n, x, whole);
+#pragma unroll
+  for (int j = 0; j < E; ++j) x[j] = -c * __builtin_amdgcn_exp2f((x[j] - lse) * kLossLog2e);
+  if ((uint32_t)y - at < (uint32_t)E) {
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+      if (at + j == (uint32_t)y) x[j] += c;
+  }
+  return pack<T>(x);
+}
+
+// A workgroup to a part of a token's row of the gradient.  POLICY: the token's loss as
+// well, from the parts of its row.
+template <typename T, bool NARROW, bool POLICY>
+__global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyParams Q, uint32_t slice) {
+  constexpr int E = kLaneElems<T>, U = 4;
+  // From the last token on: its logits were read last.
+  const uint32_t t = P.n_tok - 1 - blockIdx.x, split = blockIdx.y, end = min((split + 1) * slice * E, P.vocab);
   const int32_t y = P.targets[t];
   const T *z = (const T *)P.z + t * P.z_row;
+  constexpr uint32_t STEP = U * 256 * E;
+  const uint32_t start = split * slice * E;
+  u4 v[U];
+  auto load = [&](uint32_t base) { read_step<T, NARROW>(z, base + threadIdx.x * E, P.vocab, base + STEP <= end, v); };
+  float c = 0, lse = 0;
+  if constexpr (POLICY) {
+    const bool live = counts(y, P.vocab);
+    float l = 0, loss = 0;
+    if (live) {
+      if (P.dz) load(start);
+      const uint32_t lane = threadIdx.x % 64;
+      float m = -INFINITY, s = 0;
+      if (lane < P.splits) m = P.part[(uint64_t)t * P.splits + lane].x, s = P.part[(uint64_t)t * P.splits + lane].y;
+      join_wave(m, s);
+      lse = log_sum(m, s);
+      l = P.at_target[t] - lse;
+      c = policy_of(Q, P.n_tok, t, l, loss);
+    }
+    if (split == 0 && threadIdx.x == 0) Q.loss[t] = loss, Q.logps[t] = l;
+    if (!P.dz) return;
+  } else {
+    c = P.coef[t], lse = P.lse[t];
+    if (c != 0) load(start);
+  }
   T *dz = (T *)P.dz + t * P.dz_row;
-  for (uint32_t i = threadIdx.x; i < P.vocab; i += 256) {
-    const float p = c == 0 ? 0.f : c * (expf((float)z[i] - lse));
-    dz[i] = (T)(c == 0 ? 0.f : (int32_t)i == y ? c - p : -p);
+  if (c == 0) {
+    for (uint32_t at = start + threadIdx.x * E; at < end; at += 256 * E) store_piece(dz, at, P.vocab, (u4){0, 0, 0, 0});
+    return;
+  }
+  for (uint32_t base = start; base < end; base += STEP) {
+    u4 g[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) g[u] = v[u];
+    if (base + STEP < end) load(base + STEP);
+    const uint32_t at = base + threadIdx.x * E;
+    const bool whole = base + STEP <= end;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t i = at + u * 256 * E;
+      if (whole) __builtin_nontemporal_store(gradient_of<T, NARROW>(g[u], i, P.vocab, y, c, lse, true), (u4_any *)(dz + i));
+      else if (i < end) store_piece(dz, i, P.vocab, gradient_of<T, NARROW>(g[u], i, P.vocab, y, c, lse));
+    }
+  }
+}
+
+// The policy loss with a workgroup's registers holding the whole row: read once.
+template <typename T, int THREADS, int NV>
+__global__ void __launch_bounds__(THREADS) policy_row_kernel(TokenParams P, PolicyParams Q) {
+  constexpr int E = kLaneElems<T>, WAVES = THREADS / 64;
+  const uint32_t t = blockIdx.x;
+  const int32_t y = P.targets[t];
+  T *dz = (T *)P.dz + t * P.dz_row;
+  if (!counts(y, P.vocab)) {
+    if (threadIdx.x == 0) Q.loss[t] = 0, Q.logps[t] = 0;
+    for (uint32_t at = threadIdx.x * E; at < P.vocab; at += THREADS * E) store_piece(dz, at, P.vocab, (u4){0, 0, 0, 0});
+    return;
+  }
+  const T *z = (const T *)P.z + t * P.z_row;
+  u4 v[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) v[k] = load_once(piece_at(z, (k * THREADS + threadIdx.x) * E, P.vocab));
+  // (by one thread, through LDS: where dlogits are the logits the element is overwritten after the barrier)
+  __shared__ float at_target;
+  if (threadIdx.x == 0) at_target = (float)z[y];
+  float m = -INFINITY, s = 0;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    if (k * THREADS * E >= P.vocab) continue;
+    float x[E];
+    logits_of<T, false>(v[k], (k * THREADS + threadIdx.x) * E, P.vocab, x, (k + 1) * THREADS * E <= P.vocab);
+    gather(x, m, s);
+    // (only the packed row stays: its elements kept as 32-bit values for the second pass spilled, 599 us for 200)
+    asm volatile("" : "+v"(v[k]));
+  }
+  __shared__ float2 part[WAVES];
+  join_wave(m, s);
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = {m, s};
+  __syncthreads();
+  const uint32_t lane = threadIdx.x % 64;
+  m = lane < WAVES ? part[lane].x : -INFINITY, s = lane < WAVES ? part[lane].y : 0.f;
+  join_wave(m, s);
+  const float lse = log_sum(m, s), l = at_target - lse;
+  float loss;
+  const float c = policy_of(Q, P.n_tok, t, l, loss);
+  if (c == 0) {
+    if (threadIdx.x == 0) Q.loss[t] = loss, Q.logps[t] = l;
+    for (uint32_t at = threadIdx.x * E; at < P.vocab; at += THREADS * E) store_piece(dz, at, P.vocab, (u4){0, 0, 0, 0});
+    return;
+  }
+  if (threadIdx.x == 0) Q.loss[t] = loss, Q.logps[t] = l;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const uint32_t at = (k * THREADS + threadIdx.x) * E;
+    if (k * THREADS * E >= P.vocab) continue;
+    const bool whole = (k + 1) * THREADS * E <= P.vocab;
+    const u4 g = gradient_of<T, false>(v[k], at, P.vocab, y, c, lse, whole);
+    if (whole) __builtin_nontemporal_store(g, (u4_any *)(dz + at));
+    else store_piece(dz, at, P.vocab, g);
   }
 }
 

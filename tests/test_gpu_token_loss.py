@@ -368,7 +368,7 @@ def test_a_larger_call_then_a_smaller_one_on_a_handle():
 
 def test_refusals():
     dev = _dev()
-    for desc, status in [((BF16, 0, 8, 1), -1), ((BF16, 8, 0, 1), -1), ((BF16, (1 << 22) + 1, 8, 1), -3), ((BF16, 8, (1 << 22) + 1, 1), -3)]:
+    for desc, status in [((BF16, 0, 8, 1), -1), ((BF16, 8, 0, 1), -1), ((BF16, (1 << 21) + 1, 8, 1), -3), ((BF16, 8, (1 << 21) + 1, 1), -3)]:
         with pytest.raises(fiona.FionaError) as e:
             fiona.TokenLoss(*desc)
         assert e.value.status == status, desc

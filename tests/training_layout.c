@@ -69,6 +69,8 @@ int main(void) {
   EXPECT(FIONA_ERR_ARG, fiona_layer_norm(&a, NULL));
   a = norm(), a.width = FIONA_MAX_NORM_WIDTH + 1;
   EXPECT(FIONA_ERR_UNSUPPORTED, fiona_layer_norm(&a, NULL));
+  a = norm(), a.n = FIONA_MAX_NORM_ROWS + 1;
+  EXPECT(FIONA_ERR_UNSUPPORTED, fiona_layer_norm(&a, NULL));
   a = norm(), a.eps = 0;
   EXPECT(FIONA_ERR_ARG, fiona_layer_norm(&a, NULL));
   a = norm(), a.y = NULL;
@@ -98,7 +100,7 @@ int main(void) {
   EXPECT(FIONA_ERR_ARG, fiona_layer_norm_backward(NULL, NULL, NULL));
   EXPECT(FIONA_ERR_ARG, fiona_token_loss_create(&ld, &loss));
   if (loss) return 1;
-  ld.max_tokens = (1u << 22) + 1;
+  ld.max_tokens = (1u << 21) + 1;
   EXPECT(FIONA_ERR_UNSUPPORTED, fiona_token_loss_create(&ld, &loss));
   EXPECT(FIONA_ERR_ARG, fiona_preference_loss(NULL, NULL, NULL));
   EXPECT(FIONA_ERR_ARG, fiona_policy_loss(NULL, NULL, NULL));
