@@ -3,11 +3,14 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fiona.h"
+#include "mma.hpp"
 
 namespace fiona {
 
-constexpr uint32_t kChunkBlocks = 4;   // blocks of a workgroup
+constexpr uint32_t kChunkBlocks = 16;   // most blocks of a workgroup
 
 // What a workgroup works on: part of one tensor, from a block's first element on.
 struct AdamwChunk {
@@ -33,71 +36,210 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   return x ^ x >> 16;
 }
 
-// y in [0, 448], times its neighbouring e4m3 values' spacing: rounded up or down by
-// the dither, in (0, 1).  With LEAST never down to zero.
-template <bool LEAST>
+// y in [0, 448] to one of its neighbouring e4m3 values, by the dither in (0, 1).
 __device__ __forceinline__ float to_code(float y, float dither) {
   const uint32_t e = __builtin_bit_cast(uint32_t, y) >> 23, u = (e > 121 ? e : 121) - 3;   // 2^-6: the smallest normal value
   const float unit = __builtin_bit_cast(float, u << 23), per = __builtin_bit_cast(float, (254 - u) << 23);
-  float k = __builtin_floorf(y * per + dither);
-  if (LEAST) k = fmaxf(k, 1.f);
-  return k * unit;
+  return __builtin_floorf(y * per + dither) * unit;
 }
 
+// Four consecutive elements of T, at any address that they may stand at.
+typedef uint32_t u1_any __attribute__((aligned(1)));
+template <typename T>
+struct Four {
+  u2 v;
+};
+template <>
+struct Four<float> {
+  u4 v;
+};
+template <>
+struct Four<uint8_t> {
+  uint32_t v;
+};
+
+// `valid` of them, in whole pieces where `whole` says so; the rest zero.
+template <typename T>
+__device__ __forceinline__ void load_four(const void *base, uint64_t at, bool whole, int valid, Four<T> &f) {
+  const T *p = (const T *)base + at;
+  if constexpr (sizeof(T) == 4) {
+    if (whole) f.v = __builtin_nontemporal_load((const u4_any *)p);
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f.v[j] = j < valid ? ((const uint32_t *)p)[j] : 0;
+  } else if constexpr (sizeof(T) == 2) {
+    if (whole) f.v = __builtin_nontemporal_load((const u2_any *)p);
+    else
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t lo = 2 * j < valid ? ((const uint16_t *)p)[2 * j] : 0, hi = 2 * j + 1 < valid ? ((const uint16_t *)p)[2 * j + 1] : 0;
+        f.v[j] = lo | hi << 16;
+      }
+  } else {
+    if (whole) f.v = __builtin_nontemporal_load((const u1_any *)p);
+    else {
+      f.v = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f.v |= j < valid ? (uint32_t)((const uint8_t *)p)[j] << 8 * j : 0;
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_four(void *base, uint64_t at, bool whole, int valid, Four<T> f) {
+  T *p = (T *)base + at;
+  if constexpr (sizeof(T) == 4) {
+    if (whole) __builtin_nontemporal_store(f.v, (u4_any *)p);
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < valid) ((uint32_t *)p)[j] = f.v[j];
+  } else if constexpr (sizeof(T) == 2) {
+    if (whole) __builtin_nontemporal_store(f.v, (u2_any *)p);
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < valid) ((uint16_t *)p)[j] = (uint16_t)(f.v[j / 2] >> 16 * (j % 2));
+  } else {
+    if (whole) __builtin_nontemporal_store(f.v, (u1_any *)p);
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < valid) ((uint8_t *)p)[j] = (uint8_t)(f.v >> 8 * j);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void floats_of(Four<T> f, float (&x)[4]) {
+  if constexpr (sizeof(T) == 4) {
+    const f4 y = __builtin_bit_cast(f4, f.v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = y[j];
+  } else if constexpr (__is_same(T, _Float16)) {
+    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+    const h4 y = __builtin_bit_cast(h4, f.v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = (float)y[j];
+  } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t word = j < 2 ? f.v[0] : f.v[1];
+      x[j] = __builtin_bit_cast(float, j % 2 ? word & 0xFFFF0000u : word << 16);
+    }
+  } else {
+    x[0] = __builtin_amdgcn_cvt_f32_fp8((int)f.v, 0), x[1] = __builtin_amdgcn_cvt_f32_fp8((int)f.v, 1);
+    x[2] = __builtin_amdgcn_cvt_f32_fp8((int)f.v, 2), x[3] = __builtin_amdgcn_cvt_f32_fp8((int)f.v, 3);
+  }
+}
+template <typename T>
+__device__ __forceinline__ Four<T> four_of(const float (&x)[4]) {
+  Four<T> f;
+  if constexpr (sizeof(T) == 4) f.v = __builtin_bit_cast(u4, (f4){x[0], x[1], x[2], x[3]});
+  else if constexpr (sizeof(T) == 2) f.v = (u2){pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
+  else f.v = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false), true);
+  return f;
+}
+
+// The largest of the lanes' magnitudes, as bits: a NaN is above all numbers.
+__device__ __forceinline__ uint32_t wave_top(uint32_t x) {
+  auto step = [&](auto ctrl) {
+    const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, decltype(ctrl)::value, 0xF, 0xF, true);
+    x = x > y ? x : y;
+  };
+  step(std::integral_constant<int, 0xB1>{}), step(std::integral_constant<int, 0x4E>{});
+  step(std::integral_constant<int, 0x141>{}), step(std::integral_constant<int, 0x140>{});
+  const auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  x = a[0] > a[1] ? a[0] : a[1];
+  const auto b = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return b[0] > b[1] ? b[0] : b[1];
+}
+
+// A block's values as codes, and its scale.
+template <bool LEAST>
+__device__ __forceinline__ float block_codes(float (&x)[4], const float (&dither)[4]) {
+#pragma clang fp contract(off)
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x[j]) & 0x7FFFFFFFu;
+    top = top > u ? top : u;
+  }
+  const float t = __builtin_bit_cast(float, wave_top(top)), most = t < 0x1p-100f ? 0.f : t;
+  const float per = most > 0 ? 448.f / most : 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float y = fminf(__builtin_fabsf(x[j]) * per, 448.f);
+    float c = to_code(y, dither[j]);
+    if (LEAST) c = x[j] > 0 ? fmaxf(c, 0x1p-9f) : 0.f;
+    x[j] = most > 0 ? __builtin_copysignf(c, x[j]) : 0.f;
+  }
+  return most / 448.f;
+}
+
+// A workgroup to a chunk, its wavefronts to blocks in turn, four elements to a lane.
 template <typename T, bool SMALL>
 __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams P) {
-  // Each operation rounded by itself: a state is the same wherever the same operations are done.
+  // Each operation of the states rounded by itself: they are the same wherever the same
+  // operations are done.
 #pragma clang fp contract(off)
+  using S = std::conditional_t<SMALL, uint8_t, float>;
+  constexpr int K = kChunkBlocks / 4;
   const AdamwChunk C = P.chunks[blockIdx.x];
+  const uint32_t w = wave_index(), lane = threadIdx.x % 64;
+  Four<T> rp[K], rg[K];
+  Four<float> rx[K];
+  Four<S> rm[K], rv[K];
+  float sm[K], sv[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const uint32_t b = w + 4 * k, i = b * FIONA_ADAMW_BLOCK + 4 * lane;
+    if (b * FIONA_ADAMW_BLOCK >= C.n) continue;
+    const bool whole = (b + 1) * FIONA_ADAMW_BLOCK <= C.n;
+    const int valid = (int)C.n - (int)i;
+    load_four<T>(C.grad, i, whole, valid, rg[k]);
+    load_four<S>(C.m, i, whole, valid, rm[k]);
+    load_four<S>(C.v, i, whole, valid, rv[k]);
+    if (C.master) load_four<float>(C.master, i, whole, valid, rx[k]);
+    else load_four<T>(C.param, i, whole, valid, rp[k]);
+    if (SMALL) sm[k] = C.m_scale[b], sv[k] = C.v_scale[b];
+  }
   const int32_t step = *P.step < 1 ? 1 : *P.step;
   // 1 - beta^t without the difference of two near numbers.
-  const float c1 = -expm1f(step * P.log_b1), c2 = sqrtf(-expm1f(step * P.log_b2)), lr = *P.lr;
-  const float gs = P.grad_scale ? *P.grad_scale : 1.f;
+  const float c1 = 1.f / -expm1f(step * P.log_b1), c2 = 1.f / sqrtf(-expm1f(step * P.log_b2)), lr = *P.lr;
+  const float gs = P.grad_scale ? *P.grad_scale : 1.f, keep = 1.f - lr * C.decay;
   const uint32_t key = mix((uint32_t)step * 0x9E3779B1u + P.seed);
-  __shared__ float top[2][4];
-  for (uint32_t b = 0; b < kChunkBlocks && b * FIONA_ADAMW_BLOCK < C.n; ++b) {
-    const uint32_t i = b * FIONA_ADAMW_BLOCK + threadIdx.x;
-    const bool in = i < C.n;
-    float m = 0, v = 0, r = 0;
-    if (in) {
-      const float g = (float)((const T *)C.grad)[i] * gs;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const uint32_t b = w + 4 * k, i = b * FIONA_ADAMW_BLOCK + 4 * lane;
+    if (b * FIONA_ADAMW_BLOCK >= C.n) continue;
+    const bool whole = (b + 1) * FIONA_ADAMW_BLOCK <= C.n;
+    const int valid = (int)C.n - (int)i;
+    float g[4], m[4], v[4], x[4];
+    floats_of(rg[k], g), floats_of(rm[k], m), floats_of(rv[k], v);
+    if (C.master) floats_of(rx[k], x);
+    else floats_of(rp[k], x);
+    float um[4], uv[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float gj = g[j] * gs;
+      if (SMALL) m[j] *= sm[k], v[j] *= sv[k], v[j] *= v[j];
+      m[j] = P.b1 * m[j] + P.a1 * gj;
+      v[j] = P.b2 * v[j] + P.a2 * (gj * gj);
+      const float r = __builtin_sqrtf(v[j]);   // (rounded once; the library function may be off by a unit)
+      x[j] = x[j] * keep - lr * (m[j] * c1 * __builtin_amdgcn_rcpf(r * c2 + P.eps));
       if (SMALL) {
-        m = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)C.m)[i], 0) * C.m_scale[b];
-        v = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)C.v)[i], 0) * C.v_scale[b];
-        v = v * v;
-      } else {
-        m = ((const float *)C.m)[i], v = ((const float *)C.v)[i];
+        v[j] = r;
+        const uint32_t h = mix((C.first + i + j) ^ key);
+        um[j] = ((float)(h & 0xFFFFu) + 0.5f) * 0x1p-16f, uv[j] = ((float)(h >> 16) + 0.5f) * 0x1p-16f;
       }
-      m = P.b1 * m + P.a1 * g;
-      v = P.b2 * v + P.a2 * (g * g);
-      r = __builtin_sqrtf(v);   // (rounded once; the library function may be off by a unit)
-      float p = C.master ? C.master[i] : (float)((const T *)C.param)[i];
-      p = p - lr * C.decay * p - lr * (m / c1) / (r / c2 + P.eps);
-      if (C.master) C.master[i] = p;
-      ((T *)C.param)[i] = (T)p;
-      if (!SMALL) ((float *)C.m)[i] = m, ((float *)C.v)[i] = v;
     }
+    if (C.master) store_four(C.master, i, whole, valid, four_of<float>(x));
+    store_four(C.param, i, whole, valid, four_of<T>(x));
     if constexpr (SMALL) {
-      // The block's largest magnitudes, as bits: a NaN is above all numbers.
-      uint32_t tm = __builtin_bit_cast(uint32_t, m) & 0x7FFFFFFFu, tv = __builtin_bit_cast(uint32_t, r) & 0x7FFFFFFFu;
-      for (int k = 32; k; k >>= 1) tm = max(tm, (uint32_t)__shfl_xor((int)tm, k)), tv = max(tv, (uint32_t)__shfl_xor((int)tv, k));
-      __syncthreads();
-      if (threadIdx.x % 64 == 0)
-        top[0][threadIdx.x / 64] = __builtin_bit_cast(float, tm), top[1][threadIdx.x / 64] = __builtin_bit_cast(float, tv);
-      __syncthreads();
-      for (int k = 0; k < 4; ++k)
-        tm = max(tm, __builtin_bit_cast(uint32_t, top[0][k])), tv = max(tv, __builtin_bit_cast(uint32_t, top[1][k]));
-      const float xm = __builtin_bit_cast(float, tm) < 0x1p-100f ? 0.f : __builtin_bit_cast(float, tm);
-      const float xv = __builtin_bit_cast(float, tv) < 0x1p-100f ? 0.f : __builtin_bit_cast(float, tv);
-      const uint32_t h = mix((C.first + i) ^ key);
-      const float um = ((float)(h & 0xFFFFu) + 0.5f) / 65536.f, uv = ((float)(h >> 16) + 0.5f) / 65536.f;
-      const float ym = xm > 0 ? fminf(fabsf(m) * (448.f / xm), 448.f) : 0.f, yv = xv > 0 ? fminf(r * (448.f / xv), 448.f) : 0.f;
-      const float km = xm > 0 ? __builtin_copysignf(to_code<false>(ym, um), m) : 0.f;
-      const float kv = xv > 0 && r > 0 ? to_code<true>(yv, uv) : 0.f;
-      const uint32_t codes = __builtin_amdgcn_cvt_pk_fp8_f32(km, kv, 0, false);
-      if (in) ((uint8_t *)C.m)[i] = (uint8_t)codes, ((uint8_t *)C.v)[i] = (uint8_t)(codes >> 8);
-      if (threadIdx.x == 0) C.m_scale[b] = xm / 448.f, C.v_scale[b] = xv / 448.f;
+      const float tm = block_codes<false>(m, um), tv = block_codes<true>(v, uv);
+      if (lane == 0) C.m_scale[b] = tm, C.v_scale[b] = tv;
     }
+    store_four(C.m, i, whole, valid, four_of<S>(m));
+    store_four(C.v, i, whole, valid, four_of<S>(v));
   }
 }
 
