@@ -772,11 +772,13 @@ int fiona_policy_loss(const fiona_token_loss *loss, const fiona_policy_args *arg
  * 8-bit states: the new m and v are used in 32 bits, then rounded to one of the two
  * neighbouring values, up with the probability that keeps their mean (rounded to
  * nearest, beta2 v would stay v for ever); sqrt(v) > 0 is never rounded to zero.  A
- * block's scale is its largest magnitude / 448 (zero, as its values, below 2^-100).  The dither of
+ * block's scale is its largest magnitude / 448 (zero, as its values, below 2^-100; v below 2^-126 counts
+ * as zero).  The dither of
  * element i is 16 bits for m (low) and 16 for v (high) of mix(i ^ mix(step 0x9E3779B1 + seed)) in
  * 32-bit arithmetic, i counting from the first tensor on, every tensor from a multiple of the block;
  *     mix(x): x ^= x >> 16; x *= 0xA3D8B167; x ^= x >> 15; x *= 0xC94F6E2B; x ^= x >> 16.
- * A gradient that is not finite makes its element's states so, and with 8 bits its block's.
+ * A gradient that is no number makes its element's states and parameter so, an infinite one with 8 bits
+ * the states of its block.
  *
  * fiona_adamw_create keeps the tensors' addresses, not the tensors: they have to
  * live, where they are, as long as the handle is used.  What is written must not

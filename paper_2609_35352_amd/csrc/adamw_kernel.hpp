@@ -6,7 +6,7 @@
 #include <type_traits>
 
 #include "fiona.h"
-#include "mma.hpp"
+#include "pieces.hpp"
 
 namespace fiona {
 
@@ -36,11 +36,14 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   return x ^ x >> 16;
 }
 
-// y in [0, 448] to one of its neighbouring e4m3 values, by the dither in (0, 1).
-__device__ __forceinline__ float to_code(float y, float dither) {
-  const uint32_t e = __builtin_bit_cast(uint32_t, y) >> 23, u = (e > 121 ? e : 121) - 3;   // 2^-6: the smallest normal value
-  const float unit = __builtin_bit_cast(float, u << 23), per = __builtin_bit_cast(float, (254 - u) << 23);
-  return __builtin_floorf(y * per + dither) * unit;
+// y in [0, 448] to one of the two neighbouring e4m3 values: up where what it is above
+// the lower one, in steps between them, and a dither in (0, 1) make one together.
+// one_and: the dither and one, as 24 bits hold it.  Exponents stay those of the value's
+// binade, from 2^-6 (the smallest normal value) on.
+__device__ __forceinline__ float to_code(float y, float one_and) {
+  const uint32_t e = __builtin_bit_cast(uint32_t, y) & 0x7F800000u, u = e > (121u << 23) ? e : 121u << 23;
+  const float step = __builtin_bit_cast(float, u - (3u << 23)), per = __builtin_bit_cast(float, (257u << 23) - u);
+  return __builtin_fmaf(__builtin_floorf(__builtin_fmaf(y, per, one_and)), step, -step);
 }
 
 // Four consecutive elements of T, at any address that they may stand at.
@@ -139,48 +142,23 @@ __device__ __forceinline__ Four<T> four_of(const float (&x)[4]) {
   return f;
 }
 
-// The largest of the lanes' magnitudes, as bits: a NaN is above all numbers.
-__device__ __forceinline__ uint32_t wave_top(uint32_t x) {
-  auto step = [&](auto ctrl) {
-    const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, decltype(ctrl)::value, 0xF, 0xF, true);
-    x = x > y ? x : y;
-  };
-  step(std::integral_constant<int, 0xB1>{}), step(std::integral_constant<int, 0x4E>{});
-  step(std::integral_constant<int, 0x141>{}), step(std::integral_constant<int, 0x140>{});
-  const auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-  x = a[0] > a[1] ? a[0] : a[1];
-  const auto b = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  return b[0] > b[1] ? b[0] : b[1];
-}
-
-// A block's values as codes, and its scale.
-template <bool LEAST>
-__device__ __forceinline__ float block_codes(float (&x)[4], const float (&dither)[4]) {
-#pragma clang fp contract(off)
-  uint32_t top = 0;
+// A block's values as codes, and its scale.  A value that is no number gets the code
+// for that; an infinity makes the scale one, and with it the block.
+template <bool ROOTS>
+__device__ __forceinline__ float block_codes(float (&x)[4], const float (&one_and)[4]) {
+  const float t = wave_max(fmaxf(fmaxf(__builtin_fabsf(x[0]), __builtin_fabsf(x[1])), fmaxf(__builtin_fabsf(x[2]), __builtin_fabsf(x[3]))));
+  const float most = t < 0x1p-100f ? 0.f : t, per = most > 0 ? 448.f * __builtin_amdgcn_rcpf(most) : 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, x[j]) & 0x7FFFFFFFu;
-    top = top > u ? top : u;
+    const float y = __builtin_fabsf(x[j]) * per, c = to_code(y > 448.f ? 448.f : y, one_and[j]);
+    x[j] = ROOTS ? x[j] > 0 && most > 0 ? fmaxf(c, 0x1p-9f) : c : __builtin_copysignf(c, x[j]);
   }
-  const float t = __builtin_bit_cast(float, wave_top(top)), most = t < 0x1p-100f ? 0.f : t;
-  const float per = most > 0 ? 448.f / most : 0.f;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float y = fminf(__builtin_fabsf(x[j]) * per, 448.f);
-    float c = to_code(y, dither[j]);
-    if (LEAST) c = x[j] > 0 ? fmaxf(c, 0x1p-9f) : 0.f;
-    x[j] = most > 0 ? __builtin_copysignf(c, x[j]) : 0.f;
-  }
-  return most / 448.f;
+  return most * (1 / 448.f);
 }
 
 // A workgroup to a chunk, its wavefronts to blocks in turn, four elements to a lane.
 template <typename T, bool SMALL>
 __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams P) {
-  // Each operation of the states rounded by itself: they are the same wherever the same
-  // operations are done.
-#pragma clang fp contract(off)
   using S = std::conditional_t<SMALL, uint8_t, float>;
   constexpr int K = kChunkBlocks / 4;
   const AdamwChunk C = P.chunks[blockIdx.x];
@@ -222,14 +200,16 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams P) {
     for (int j = 0; j < 4; ++j) {
       const float gj = g[j] * gs;
       if (SMALL) m[j] *= sm[k], v[j] *= sv[k], v[j] *= v[j];
-      m[j] = P.b1 * m[j] + P.a1 * gj;
-      v[j] = P.b2 * v[j] + P.a2 * (gj * gj);
-      const float r = __builtin_sqrtf(v[j]);   // (rounded once; the library function may be off by a unit)
+      m[j] = __builtin_fmaf(P.b1, m[j], P.a1 * gj);
+      v[j] = __builtin_fmaf(P.a2 * gj, gj, P.b2 * v[j]);
+      const float r = __builtin_amdgcn_sqrtf(v[j]);
       x[j] = x[j] * keep - lr * (m[j] * c1 * __builtin_amdgcn_rcpf(r * c2 + P.eps));
       if (SMALL) {
         v[j] = r;
         const uint32_t h = mix((C.first + i + j) ^ key);
-        um[j] = ((float)(h & 0xFFFFu) + 0.5f) * 0x1p-16f, uv[j] = ((float)(h >> 16) + 0.5f) * 0x1p-16f;
+        // one + (16 bits + 1/2) / 2^16, the bits below the leading one's seven places up
+        um[j] = __builtin_bit_cast(float, (h & 0xFFFFu) << 7 | 0x3F800040u);
+        uv[j] = __builtin_bit_cast(float, (h >> 9 & 0x7FFF80u) | 0x3F800040u);
       }
     }
     if (C.master) store_four(C.master, i, whole, valid, four_of<float>(x));

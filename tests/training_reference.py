@@ -185,39 +185,40 @@ def dither(step, seed, first, n):
 
 def _spread(x, n):
     """x [n] in blocks of 256, the last filled with zeros."""
-    out = torch.zeros(-(-n // 256) * 256)
+    out = torch.zeros(-(-n // 256) * 256, dtype=torch.float64)
     out[:n] = x
     return out.view(-1, 256)
 
 
 def to_codes(x, up, positive):
-    """x [n] float32 as e4m3 values in 32-bit operations: (codes [n], scales)."""
+    """x [n] as e4m3 values, in 64 bits: (codes [n], scales, and the other neighbour [n] where a value and its dither come within
+    2^-15 of a step to the border between the two)."""
     n = x.numel()
-    x, up = _spread(x, n), _spread(up, n)
+    x, up = _spread(x.double(), n).double(), _spread(up, n).double()
     top = x.abs().amax(1, keepdim=True)
-    top = torch.where(top < 2.0 ** -100, torch.zeros(()), top)
-    y = (x.abs() * torch.where(top > 0, 448.0 / top, torch.zeros(()))).clamp(max=448.0)
+    top = torch.where(top < 2.0 ** -100, torch.zeros((), dtype=torch.float64), top)
+    y = x.abs() * torch.where(top > 0, 448.0 / top, torch.zeros((), dtype=torch.float64))
     e = torch.frexp(y)[1].clamp(min=-5)
     unit = torch.ldexp(torch.ones_like(y), e - 4)
-    k = torch.floor(y / unit + up)
-    if positive:
-        k = torch.where(x > 0, k.clamp(min=1.0), torch.zeros(()))
-    k = torch.where(top > 0, k, torch.zeros(()))
-    return (torch.sign(x) * k * unit).flatten()[:n].to(torch.float8_e4m3fn), (top / 448.0)[:, 0]
+
+    def values(k):
+        if positive:
+            k = torch.where(x > 0, k.clamp(min=1.0), torch.zeros((), dtype=torch.float64))
+        k = torch.where(top > 0, k, torch.zeros((), dtype=torch.float64))
+        return (torch.sign(x) * k * unit).clamp(-448, 448).flatten()[:n].float().to(torch.float8_e4m3fn)
+
+    # 32 bits leave y / unit, below 16, off by a few 2^-24 of itself: by 16 * 16 * 2^-24 = 2^-16 of a step at most, and the sum by
+    # half of 2^-20; y just below a power of two may count as that power, whose steps are twice as long: the same values
+    at = y / unit + up
+    return values(torch.floor(at)), (top / 448.0)[:, 0].float(), torch.stack([values(torch.floor(at + s * 2.0 ** -15)).float() for s in (-1, 1)])
 
 
 def states8(g, m, v, m_scale, v_scale, beta1, beta2, step, seed, first, scale=1.0):
-    """The new 8-bit states and the values that the step uses: m, v in 32-bit operations, each rounded by itself."""
+    """The new 8-bit states (to_codes of m and of v's root), and m and v, in 64 bits."""
     n = g.numel()
-    f = lambda x: torch.tensor(x, dtype=torch.float64).float()
-    each = lambda s: s.repeat_interleave(256)[:n]
-    g = g.float() * f(scale)
-    m = m.float() * each(m_scale)
-    v = v.float() * each(v_scale)
-    v = v * v
-    m = f(beta1) * m + f(1 - beta1) * g
-    v = f(beta2) * v + f(1 - beta2) * (g * g)
+    each = lambda s: s.double().repeat_interleave(256)[:n]
+    g = g.double() * scale
+    m, v = m.double() * each(m_scale), (v.double() * each(v_scale)) ** 2
+    m, v = beta1 * m + (1 - beta1) * g, beta2 * v + (1 - beta2) * g * g
     um, uv = dither(step, seed, first, n)
-    cm, sm = to_codes(m, um, False)
-    cv, sv = to_codes(v.double().sqrt().float(), uv, True)      # (a root in 64 bits, rounded, is the 32-bit one; torch's is off by a unit at times)
-    return cm, cv, sm, sv, m, v
+    return to_codes(m, um, False), to_codes(v.sqrt(), uv, True), m, v
