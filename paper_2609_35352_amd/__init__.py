@@ -767,16 +767,6 @@ def _shared(t, name, dtype, dev):
     return _packed(t, name, dtype, (1,), dev)
 
 
-def _write(t, name, dtype, shape, dev, packed, written):
-    """(address, row stride) of an output, which is noted as written; (0, 0) for None."""
-    if t is None:
-        return 0, 0
-    written.append(t)
-    if packed:
-        return _packed(t, name, dtype, shape, dev), 0
-    return t.data_ptr(), _rows(t, name, dtype, shape, dev)[0]
-
-
 def layer_norm(x, weight, bias, y, eps: float = 1e-5, residual=None, total=None, mean=None, rstd=None, stream=None) -> None:
     """fiona_layer_norm: y [n][d] = the norm of x [n][d], or of x + residual, which total receives; weight, bias [d] (x's
     type or float32, or None: one and zero); mean, rstd float32 [n].  y or total may be x or residual."""
@@ -785,22 +775,24 @@ def layer_norm(x, weight, bias, y, eps: float = 1e-5, residual=None, total=None,
         raise ValueError("x must have shape [n][width]")
     code = _type_code(dt)
     n, d = shape
-    f32, written = _INT["f32"], []
+    f32 = _INT["f32"]
     w = weight if weight is not None else bias
     wt = dt if w is None or w.dtype is dt else f32
-    xs = _rows(x, "x", dt, shape, dev)
-    rp, rs = (residual.data_ptr(), _rows(residual, "residual", dt, shape, dev)[0]) if residual is not None else (0, 0)
-    wp = _packed(weight, "weight", wt, (d,), dev) if weight is not None else 0
-    bp = _packed(bias, "bias", wt, (d,), dev) if bias is not None else 0
-    yp, ys = _write(y, "y", dt, shape, dev, False, written)
-    tp, ts = _write(total, "total", dt, shape, dev, False, written)
-    mp, _ = _write(mean, "mean", f32, (n,), dev, True, written)
-    qp, _ = _write(rstd, "rstd", f32, (n,), dev, True, written)
-    args = _NORM_ARGS.pack(n, d, code, code if wt is dt else 0, eps, x.data_ptr(), rp, wp, bp, yp, tp, mp, qp, xs[0], rs, ys, ts)
-    rc = _lm_lib().fiona_layer_norm(args, _stream_of(stream, dev))
+    xs, ys = _rows(x, "x", dt, shape, dev), _rows(y, "y", dt, shape, dev)
+    rp = rs = tp = ts = 0
+    if residual is not None:
+        rp, rs = residual.data_ptr(), _rows(residual, "residual", dt, shape, dev)[0]
+    if total is not None:
+        tp, ts = total.data_ptr(), _rows(total, "total", dt, shape, dev)[0]
+    args = _NORM_ARGS.pack(n, d, code, code if wt is dt else 0, eps, x.data_ptr(), rp,
+                           _packed(weight, "weight", wt, (d,), dev) if weight is not None else 0,
+                           _packed(bias, "bias", wt, (d,), dev) if bias is not None else 0, y.data_ptr(), tp,
+                           _packed(mean, "mean", f32, (n,), dev) if mean is not None else 0,
+                           _packed(rstd, "rstd", f32, (n,), dev) if rstd is not None else 0, xs[0], rs, ys[0], ts)
+    rc = lib().fiona_layer_norm(args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_layer_norm")
-    _modified[0](written)
+    _modified[0]([t for t in (y, total, mean, rstd) if t is not None])
 
 
 class _Handle:
@@ -844,20 +836,21 @@ class LayerNorm(_Handle):
 def layer_norm_backward(ln: LayerNorm, dy, x, weight, mean, rstd, dx_base, dx, dweight=None, dbias=None, stream=None) -> None:
     """fiona_layer_norm_backward: dx [n][d] = dx_base (or None: zero) plus the gradient through the norm of x (layer_norm's
     total, where it had a residual) from dy [n][d]; dweight, dbias [d].  dx may be dx_base, dy or x."""
-    n, dev, dt, wt, f32, written = x.shape[0], x.get_device(), ln.dtype, ln.weight_dtype, _INT["f32"], []
+    n, dev, dt, wt, f32 = x.shape[0], x.get_device(), ln.dtype, ln.weight_dtype, _INT["f32"]
     shape, row = (n, ln.width), (ln.width,)
-    gs, xs = _rows(dy, "dy", dt, shape, dev), _rows(x, "x", dt, shape, dev)
-    wp = _packed(weight, "weight", wt, row, dev) if weight is not None else 0
-    bp, bs = (dx_base.data_ptr(), _rows(dx_base, "dx_base", dt, shape, dev)[0]) if dx_base is not None else (0, 0)
-    dp, ds = _write(dx, "dx", dt, shape, dev, False, written)
-    args = _NORM_BACKWARD_ARGS.pack(n, dy.data_ptr(), x.data_ptr(), wp, _packed(mean, "mean", f32, (n,), dev),
-                                    _packed(rstd, "rstd", f32, (n,), dev), bp, dp,
-                                    _write(dweight, "dweight", wt, row, dev, True, written)[0],
-                                    _write(dbias, "dbias", wt, row, dev, True, written)[0], gs[0], xs[0], bs, ds)
+    gs, xs, ds = _rows(dy, "dy", dt, shape, dev), _rows(x, "x", dt, shape, dev), _rows(dx, "dx", dt, shape, dev)
+    bp = bs = 0
+    if dx_base is not None:
+        bp, bs = dx_base.data_ptr(), _rows(dx_base, "dx_base", dt, shape, dev)[0]
+    args = _NORM_BACKWARD_ARGS.pack(n, dy.data_ptr(), x.data_ptr(),
+                                    _packed(weight, "weight", wt, row, dev) if weight is not None else 0,
+                                    _packed(mean, "mean", f32, (n,), dev), _packed(rstd, "rstd", f32, (n,), dev), bp, dx.data_ptr(),
+                                    _packed(dweight, "dweight", wt, row, dev) if dweight is not None else 0,
+                                    _packed(dbias, "dbias", wt, row, dev) if dbias is not None else 0, gs[0], xs[0], bs, ds[0])
     rc = lib().fiona_layer_norm_backward(ln.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_layer_norm_backward")
-    _modified[0](written)
+    _modified[0]([t for t in (dx, dweight, dbias) if t is not None])
 
 
 class TokenLoss(_Handle):
@@ -876,20 +869,21 @@ def preference_loss(tl: TokenLoss, logits, targets, offsets, reference, loss, lo
     """fiona_preference_loss: logits [n_tok][vocab], targets int32 [n_tok] (outside the vocabulary: not counted), offsets int32
     [2 n_pair + 1], reference float32 [2 n_pair] -> loss float32 [n_pair], logps float32 [2 n_pair] and dlogits
     [n_tok][vocab] (None: not wanted; it may be logits).  weights float32 [n_pair]: default 1 / n_pair."""
-    n, p, dev, i32, f32, written = logits.shape[0], loss.shape[0], logits.get_device(), _INT[4], _INT["f32"], []
+    n, p, dev, i32, f32 = logits.shape[0], loss.shape[0], logits.get_device(), _INT[4], _INT["f32"]
     shape = (n, tl.vocab)
     zs = _rows(logits, "logits", tl.dtype, shape, dev)
-    dp, ds = _write(dlogits, "dlogits", tl.dtype, shape, dev, False, written)
+    dp = ds = 0
+    if dlogits is not None:
+        dp, ds = dlogits.data_ptr(), _rows(dlogits, "dlogits", tl.dtype, shape, dev)[0]
     args = _PREFERENCE_ARGS.pack(n, p, beta, label_smoothing, logits.data_ptr(), dp, zs[0], ds,
                                  _packed(targets, "targets", i32, (n,), dev), _packed(offsets, "offsets", i32, (2 * p + 1,), dev),
                                  _packed(reference, "reference", f32, (2 * p,), dev),
                                  _packed(weights, "weights", f32, (p,), dev) if weights is not None else 0,
-                                 _write(loss, "loss", f32, (p,), dev, True, written)[0],
-                                 _write(logps, "logps", f32, (2 * p,), dev, True, written)[0])
+                                 _packed(loss, "loss", f32, (p,), dev), _packed(logps, "logps", f32, (2 * p,), dev))
     rc = lib().fiona_preference_loss(tl.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_preference_loss")
-    _modified[0](written)
+    _modified[0]((loss, logps) if dlogits is None else (loss, logps, dlogits))
 
 
 def policy_loss(tl: TokenLoss, logits, targets, old, advantages, loss, logps, dlogits=None, reference=None,
@@ -897,21 +891,22 @@ def policy_loss(tl: TokenLoss, logits, targets, old, advantages, loss, logps, dl
     """fiona_policy_loss: logits [n_tok][vocab], targets int32 [n_tok] (outside the vocabulary: not counted), old, advantages
     and, with kl > 0, reference float32 [n_tok] -> loss, logps float32 [n_tok] and dlogits [n_tok][vocab] (None: not
     wanted; it may be logits).  weights float32 [n_tok]: default 1 / n_tok."""
-    n, dev, f32, written = logits.shape[0], logits.get_device(), _INT["f32"], []
+    n, dev, f32 = logits.shape[0], logits.get_device(), _INT["f32"]
     shape, each = (n, tl.vocab), (n,)
     zs = _rows(logits, "logits", tl.dtype, shape, dev)
-    dp, ds = _write(dlogits, "dlogits", tl.dtype, shape, dev, False, written)
+    dp = ds = 0
+    if dlogits is not None:
+        dp, ds = dlogits.data_ptr(), _rows(dlogits, "dlogits", tl.dtype, shape, dev)[0]
     args = _POLICY_ARGS.pack(n, clip_low, clip_high, kl, logits.data_ptr(), dp, zs[0], ds,
                              _packed(targets, "targets", _INT[4], each, dev), _packed(old, "old", f32, each, dev),
                              _packed(advantages, "advantages", f32, each, dev),
                              _packed(reference, "reference", f32, each, dev) if reference is not None else 0,
                              _packed(weights, "weights", f32, each, dev) if weights is not None else 0,
-                             _write(loss, "loss", f32, each, dev, True, written)[0],
-                             _write(logps, "logps", f32, each, dev, True, written)[0])
+                             _packed(loss, "loss", f32, each, dev), _packed(logps, "logps", f32, each, dev))
     rc = lib().fiona_policy_loss(tl.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_policy_loss")
-    _modified[0](written)
+    _modified[0]((loss, logps) if dlogits is None else (loss, logps, dlogits))
 
 
 class AdamW(_Handle):
