@@ -37,8 +37,10 @@ int check_logits(const fiona_token_loss *H, uint32_t n, const void *logits, cons
 }
 
 // Parts of each of n rows of `pieces` pieces: enough workgroups to fill the GPU, none
-// below 256 pieces (one for each of its threads).
-constexpr uint32_t kWorkgroups = 1024;
+// below 256 pieces (one for each of its threads).  1024 / 2048 / 4096 / 8192 workgroups,
+// parts and gradient, us: 1392 tokens of 50021 in binary16 80 / 74 / 73 / 87, 885 of
+// 32768 in bfloat16 28 / 30 / 32 / 44, 7955 of 32768 225 / 226 / 224 / 235.
+constexpr uint32_t kWorkgroups = 2048;
 uint32_t splits_of(uint32_t n, uint32_t pieces) {
   n = std::max(1u, n);
   return std::max(1u, std::min({(kWorkgroups + n - 1) / n, (pieces + 255) / 256, fiona::kLossSplits}));
@@ -84,6 +86,14 @@ void launch_grad(const fiona::TokenParams &P, const fiona::PolicyParams &Q, hipS
   });
 }
 
+// Whether each row's policy loss is one workgroup's: rows of up to 64 KiB, or enough
+// of the longer ones (one workgroup reads and writes 256 KiB in 17 us).  us of two
+// launches, parts and gradient, without the gap between them / of whole rows, in
+// bfloat16: 2 x 16000 7.2 / 4.9, 64 x 32768 8.9 / 7.6, 16 x 64000 7.6 / 10.4, 64 x 64000
+// 11.8 / 11.1, 64 x 131072 12.8 / 18.2, 100 x 131072 22.8 / 19.4, 200 x 131072 30.2 /
+// 24.7, 3000 x 131072 411 / 290.
+bool whole_rows(uint32_t n, uint32_t pieces) { return pieces <= 4096 || (pieces <= 1024 * 16 && n >= pieces / 192); }
+
 // The policy loss with whole rows in registers.
 template <typename T>
 void launch_rows(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint32_t pieces, hipStream_t stream) {
@@ -94,7 +104,6 @@ void launch_rows(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint
   else if (pieces <= 1024 * 8) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 8>), grid, dim3(1024), 0, stream, P, Q);
   else hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 16>), grid, dim3(1024), 0, stream, P, Q);
 }
-constexpr uint32_t kRowPieces = 1024 * 16;
 
 }  // namespace
 
@@ -190,7 +199,7 @@ int fiona_policy_loss(const fiona_token_loss *H, const fiona_policy_args *args, 
   with_type(H->desc.type, [&](auto t) {
     using T = decltype(t);
     const uint32_t pieces = pieces_of(H->desc);
-    if (A.dlogits && pieces <= kRowPieces && P.vocab >= fiona::kLaneElems<T>) {
+    if (A.dlogits && whole_rows(A.n_tok, pieces) && P.vocab >= fiona::kLaneElems<T>) {
       launch_rows<T>(P, Q, pieces, stream);
       return;
     }

@@ -98,14 +98,14 @@ __device__ __forceinline__ void gather(const float (&x)[N], float &m, float &s) 
 
 // Four pieces of a row, 256 of them apart, for a lane whose first one starts at `at`.
 // Steps that end before the row does (`whole`, the same in the workgroup) need no checks.
-template <typename T, bool NARROW>
-__device__ __forceinline__ void read_step(const T *row, uint32_t at, uint32_t n, bool whole, u4 (&v)[4]) {
+template <typename T, bool NARROW, int U>
+__device__ __forceinline__ void read_step(const T *row, uint32_t at, uint32_t n, bool whole, u4 (&v)[U]) {
   if (whole) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = load_shared(row + at + u * 256 * kLaneElems<T>);
+    for (int u = 0; u < U; ++u) v[u] = load_shared(row + at + u * 256 * kLaneElems<T>);
   } else {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = read_piece<T, NARROW>(row, at + u * 256 * kLaneElems<T>, n);
+    for (int u = 0; u < U; ++u) v[u] = read_piece<T, NARROW>(row, at + u * 256 * kLaneElems<T>, n);
   }
 }
 
@@ -120,7 +120,7 @@ __device__ __forceinline__ float log_sum(float m, float s) { return (m == -INFIN
 // A workgroup to a part of a token's row.
 template <typename T, bool NARROW>
 __global__ void __launch_bounds__(256) token_stats_kernel(TokenParams P) {
-  constexpr int E = kLaneElems<T>, U = 4;
+  constexpr int E = kLaneElems<T>, U = 2;
   const uint32_t t = blockIdx.x, split = blockIdx.y;
   const int32_t y = P.targets[t];
   if (split == 0 && threadIdx.x == 0) P.coef[t] = 0;          // (of a token in no sequence)
@@ -166,30 +166,32 @@ __global__ void __launch_bounds__(1024) pair_kernel(TokenParams P, PairParams Q,
   const uint32_t lane = threadIdx.x % lanes;
   __shared__ double sh[2][16];
   const uint32_t p = blockIdx.x;
-  double sum[2];
-  int32_t first[2], last[2];
+  int32_t end[3];      // sequence k: from end[k] to end[k + 1]
+#pragma unroll
+  for (int k = 0; k < 3; ++k) end[k] = min(max(Q.offsets[2 * p + k], 0), (int32_t)P.n_tok);
+  const int32_t from = min(end[0], end[1]), to = max(end[1], end[2]);
+  auto sequence = [&](int32_t t) { return t >= end[0] && t < end[1] ? 0 : t >= end[1] && t < end[2] ? 1 : -1; };
+  double sum[2] = {0, 0};
+  for (int32_t t = from + (int32_t)(threadIdx.x / lanes); t < to; t += 1024 / lanes) {
+    const int k = sequence(t);
+    float m = -INFINITY, s = 0;
+    if (lane < P.splits) {
+      const float2 part = P.part[(uint64_t)t * P.splits + lane];
+      m = part.x, s = part.y;
+    }
+    const float zt = P.at_target[t];
+    const bool live = k >= 0 && counts(P.targets[t], P.vocab);     // (what the others' parts hold is not used)
+    float top = m;
+    for (uint32_t i = 1; i < lanes; i *= 2) top = fmaxf(top, __shfl_xor(top, i));
+    s *= __builtin_amdgcn_exp2f((m - (top == -INFINITY ? 0.f : top)) * kLossLog2e);
+    for (uint32_t i = 1; i < lanes; i *= 2) s += __shfl_xor(s, i);
+    const float lse = log_sum(top, s);
+    if (lane || !live) continue;
+    P.lse[t] = lse;
+    sum[0] += k ? 0. : zt - lse, sum[1] += k ? zt - lse : 0.;
+  }
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    first[k] = min(max(Q.offsets[2 * p + k], 0), (int32_t)P.n_tok);
-    last[k] = min(max(Q.offsets[2 * p + k + 1], 0), (int32_t)P.n_tok);
-    sum[k] = 0;
-    for (int32_t t = first[k] + (int32_t)(threadIdx.x / lanes); t < last[k]; t += 1024 / lanes) {
-      if (!counts(P.targets[t], P.vocab)) continue;
-      float m = -INFINITY, s = 0;
-      if (lane < P.splits) {
-        const float2 part = P.part[(uint64_t)t * P.splits + lane];
-        m = part.x, s = part.y;
-      }
-      const float zt = P.at_target[t];
-      float top = m;
-      for (uint32_t i = 1; i < lanes; i *= 2) top = fmaxf(top, __shfl_xor(top, i));
-      s *= __builtin_amdgcn_exp2f((m - (top == -INFINITY ? 0.f : top)) * kLossLog2e);
-      for (uint32_t i = 1; i < lanes; i *= 2) s += __shfl_xor(s, i);
-      const float lse = log_sum(top, s);
-      if (lane) continue;
-      P.lse[t] = lse;
-      sum[k] += zt - lse;
-    }
     for (int i = 32; i; i >>= 1) sum[k] += __shfl_xor(sum[k], i);
     if (threadIdx.x % 64 == 0) sh[k][threadIdx.x / 64] = sum[k];
   }
@@ -201,10 +203,10 @@ __global__ void __launch_bounds__(1024) pair_kernel(TokenParams P, PairParams Q,
   const double w = Q.weights ? Q.weights[p] : 1. / Q.n_pair, e = Q.smoothing, x = exp(-fabs(h)), big = 1 / (1 + x), small = x / (1 + x);
   const double up = h >= 0 ? big : small, down = h >= 0 ? small : big;      // sigmoid(h), sigmoid(-h)
   const float g = w == 0 ? 0.f : (float)(w * Q.beta * (e * up - (1 - e) * down));
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
-    for (int32_t t = first[k] + (int32_t)threadIdx.x; t < last[k]; t += 1024)
-      if (counts(P.targets[t], P.vocab)) P.coef[t] = k ? -g : g;
+  for (int32_t t = from + (int32_t)threadIdx.x; t < to; t += 1024) {
+    const int k = sequence(t);
+    if (k >= 0 && counts(P.targets[t], P.vocab)) P.coef[t] = k ? -g : g;
+  }
   if (threadIdx.x) return;
   // -log sigmoid(h) = log(1 + exp(-|h|)) + max(-h, 0)
   const double loss = log1p(x) + (h < 0 ? (1 - e) * -h : e > 0 && h > 0 ? e * h : 0.);
@@ -232,7 +234,7 @@ __device__ __forceinline__ u4 gradient_of(u4 v, uint32_t at, uint32_t n, int32_t
 // well, from the parts of its row.
 template <typename T, bool NARROW, bool POLICY>
 __global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyParams Q, uint32_t slice) {
-  constexpr int E = kLaneElems<T>, U = 4;
+  constexpr int E = kLaneElems<T>, U = 2;
   // From the last token on: its logits were read last.
   const uint32_t t = P.n_tok - 1 - blockIdx.x, split = blockIdx.y, end = min((split + 1) * slice * E, P.vocab);
   const int32_t y = P.targets[t];
