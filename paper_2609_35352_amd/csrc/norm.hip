@@ -68,8 +68,14 @@ void with_grad_shape(uint32_t q, F f) {
   else if constexpr (wide) f(Shape<8, 4>{});
 }
 
-// Parts of the rows' sums.
+// Parts of the rows' sums: a workgroup's each.  512 / 1024, us with their sum: 8192 rows
+// of 4096 in bfloat16 55 / 60, 4096 of 8192 60 / 75, 2048 of 768 in 32 bits 13.2 / 17.7,
+// 8192 of 1376 in binary16 30 / 27.
 constexpr uint32_t kMostParts = 512;
+// Where a lane holds one piece of a row, many rows go two at a time, for the bytes in
+// flight (one / two at a time, us: 16384 of 1376 in bfloat16 48.3 / 40.7, 8192 of 2048
+// 26.8 / 27.4, 1531 of 1373 9.9 / 10.7, 300 of 2048 6.1 / 6.8).
+constexpr uint32_t kTwoRows = 4096;
 constexpr uint32_t pitch_of(uint32_t d) { return (d + 3) / 4 * 4; }
 bool by_columns(uint32_t type, uint32_t d) { return d < 16 / type_size(type) || d > kMostSums; }
 uint32_t parts_of(uint32_t type, uint32_t d, uint32_t n) {
@@ -183,7 +189,14 @@ int fiona_layer_norm_backward(const fiona_norm *norm, const fiona_norm_backward_
     } else if (sums && !columns) {
       with_grad_shape<T>(q, [&](auto s) {
         constexpr int WAVES = decltype(s)::kWaves, NV = decltype(s)::kPieces;
-        hipLaunchKernelGGL((fiona::norm_grads_kernel<T, W, WAVES, NV>), dim3(parts), dim3(fiona::kNormThreads<WAVES>), 0, stream, P);
+        const dim3 grid(parts), threads(fiona::kNormThreads<WAVES>);
+        if constexpr (NV == 1) {
+          if (A.n >= kTwoRows) {
+            hipLaunchKernelGGL((fiona::norm_grads_kernel<T, W, WAVES, NV, 2>), grid, threads, 0, stream, P);
+            return;
+          }
+        }
+        hipLaunchKernelGGL((fiona::norm_grads_kernel<T, W, WAVES, NV, 1>), grid, threads, 0, stream, P);
       });
     } else if (A.n) {
       with_shape<T>(q, [&](auto s) {

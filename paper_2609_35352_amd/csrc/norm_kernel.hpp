@@ -32,20 +32,26 @@ struct NormGradParams {
 template <int WAVES>
 constexpr int kNormThreads = WAVES > 4 ? 64 * WAVES : 256;
 
-// Sums of two values over a group; `slot` alternates from call to call, so that one
+// Sums of N values over a group; `slot` alternates from call to call, so that one
 // barrier is enough.
-template <int WAVES>
-__device__ __forceinline__ void group_sum(float &a, float &b, uint32_t slot) {
-  a = wave_sum(a), b = wave_sum(b);
+template <int WAVES, int N>
+__device__ __forceinline__ void group_sum(float (&x)[N], uint32_t slot) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
   if constexpr (WAVES > 1) {
-    __shared__ float2 part[2][kNormThreads<WAVES> / 64];
+    __shared__ float part[2][kNormThreads<WAVES> / 64][N];
     const uint32_t w = wave_index();
-    if (threadIdx.x % 64 == 0) part[slot][w] = {a, b};
+    if (threadIdx.x % 64 == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) part[slot][w][i] = x[i];
     __syncthreads();
     const uint32_t first = w / WAVES * WAVES;
-    a = b = 0;
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) a += part[slot][first + i].x, b += part[slot][first + i].y;
+    for (int i = 0; i < N; ++i) x[i] = 0;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] += part[slot][first + k][i];
   }
 }
 
@@ -83,7 +89,7 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_kernel(NormParams P)
 #pragma unroll
     for (int k = 0; k < NV; ++k) add[k] = load_once(piece_at(r, (k * 64 * WAVES + lane) * E, d));
   }
-  float s[NV][E], sum = 0, none = 0;
+  float s[NV][E], sum[1] = {0}, square[1] = {0};
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const uint32_t at = (k * 64 * WAVES + lane) * E;
@@ -98,22 +104,21 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_kernel(NormParams P)
       unpack<T>(raw[k], s[k]);           // (what the backward pass finds is what is normalised)
     }
 #pragma unroll
-    for (int j = 0; j < E; ++j) sum += s[k][j];
+    for (int j = 0; j < E; ++j) sum[0] += s[k][j];
   }
-  group_sum<WAVES>(sum, none, 0);
-  const float mean = sum / d;
-  float square = 0;
+  group_sum<WAVES>(sum, 0);
+  const float mean = sum[0] / d;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const uint32_t at = (k * 64 * WAVES + lane) * E;
 #pragma unroll
     for (int j = 0; j < E; ++j) {
       s[k][j] -= mean;
-      square += at + j < d ? s[k][j] * s[k][j] : 0.f;
+      square[0] += at + j < d ? s[k][j] * s[k][j] : 0.f;
     }
   }
-  group_sum<WAVES>(square, none, 1);
-  const float rstd = 1 / sqrtf(square / d + P.eps);
+  group_sum<WAVES>(square, 1);
+  const float rstd = 1 / sqrtf(square[0] / d + P.eps);
   if (!live) return;
   T *y = (T *)P.y + t * P.y_row, *total = (T *)P.total + (P.total ? t * P.total_row : 0);
 #pragma unroll
@@ -177,7 +182,7 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grad_kernel(NormGrad
     if (P.dx_base) rb[k] = load_once(piece_at(base, at, d));
   }
   const float mean = P.mean[t], rstd = P.rstd[t];
-  float s1 = 0, s2 = 0;
+  float sum[2] = {0, 0};
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const uint32_t at = (k * 64 * WAVES + lane) * E;
@@ -185,10 +190,10 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grad_kernel(NormGrad
     load_weights<T, W>(P.weight, at, d, 1.f, w);
     unpack_grad<T>(rx[k], rg[k], at, d, mean, rstd, w, u, xh);
 #pragma unroll
-    for (int j = 0; j < E; ++j) s1 += u[j], s2 += u[j] * xh[j];
+    for (int j = 0; j < E; ++j) sum[0] += u[j], sum[1] += u[j] * xh[j];
   }
-  group_sum<WAVES>(s1, s2, 0);
-  s1 /= d, s2 /= d;
+  group_sum<WAVES>(sum, 0);
+  const float s1 = sum[0] / d, s2 = sum[1] / d;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const uint32_t at = (k * 64 * WAVES + lane) * E;
@@ -199,29 +204,32 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grad_kernel(NormGrad
   }
 }
 
-// dx of every gridDim-th group's row, and this workgroup's part of the weights'
+// dx of R rows at a time of every gridDim-th, and this workgroup's part of the weights'
 // gradients, which its lanes add up in registers over those rows.
-template <typename T, typename W, int WAVES, int NV>
+template <typename T, typename W, int WAVES, int NV, int R>
 __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grads_kernel(NormGradParams P) {
   constexpr int E = kLaneElems<T>, GROUPS = kNormThreads<WAVES> / 64 / WAVES;
   const uint32_t lane = threadIdx.x % (64 * WAVES), group = wave_index() / WAVES, d = P.d;
   const float per = 1.f / d;
   const uint64_t step = (uint64_t)gridDim.x * GROUPS;
-  // The next row is on its way while one is computed (a group without a row at the
-  // end goes along with the last one).
-  u4 rx[NV], rg[NV], rb[NV];
-  float mean = 0, rstd = 0;
-  auto load = [&](uint64_t t) {
-    t = t < P.n ? t : P.n - 1;
-    const T *x = (const T *)P.x + t * P.x_row, *dy = (const T *)P.dy + t * P.dy_row;
-    const T *base = (const T *)P.dx_base + (P.dx_base ? t * P.dx_base_row : 0);
+  // The next rows are on their way while these are computed (where none is left the
+  // last one is taken along).
+  u4 rx[R][NV], rg[R][NV], rb[R][NV];
+  float mean[R], rstd[R];
+  auto load = [&](uint64_t first) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const uint32_t at = (k * 64 * WAVES + lane) * E;
-      rx[k] = load_once(piece_at(x, at, d)), rg[k] = load_once(piece_at(dy, at, d));
-      if (P.dx_base) rb[k] = load_once(piece_at(base, at, d));
+    for (int i = 0; i < R; ++i) {
+      const uint64_t t = first + i * step < P.n ? first + i * step : P.n - 1;
+      const T *x = (const T *)P.x + t * P.x_row, *dy = (const T *)P.dy + t * P.dy_row;
+      const T *base = (const T *)P.dx_base + (P.dx_base ? t * P.dx_base_row : 0);
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const uint32_t at = (k * 64 * WAVES + lane) * E;
+        rx[i][k] = load_once(piece_at(x, at, d)), rg[i][k] = load_once(piece_at(dy, at, d));
+        if (P.dx_base) rb[i][k] = load_once(piece_at(base, at, d));
+      }
+      mean[i] = P.mean[t], rstd[i] = P.rstd[t];
     }
-    mean = P.mean[t], rstd = P.rstd[t];
   };
   uint64_t first = (uint64_t)blockIdx.x * GROUPS;
   if (first < P.n) load(first + group);
@@ -232,35 +240,46 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grads_kernel(NormGra
 #pragma unroll
     for (int j = 0; j < E; ++j) dw[k][j] = db[k][j] = 0;
   }
-  for (uint32_t slot = 0; first < P.n; first += step, slot ^= 1) {
-    const bool live = first + group < P.n;
+  for (uint32_t slot = 0; first < P.n; first += R * step, slot ^= 1) {
     const uint64_t t = first + group;
-    const float m = mean, r = rstd;
-    float s1 = 0, s2 = 0;
-    float xh[NV][E], g[NV][E];
-    u4 add[NV];
+    float xh[R][NV][E], g[R][NV][E], m[R], r[R], sum[2 * R];
+    u4 add[R][NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const uint32_t at = (k * 64 * WAVES + lane) * E;
-      unpack<T>(piece_fix<T>(rx[k], at, d), xh[k]);
-      unpack<T>(piece_fix<T>(rg[k], at, d), g[k]);
-      add[k] = rb[k];
-    }
-    if (first + step < P.n) load(t + step);
+    for (int i = 0; i < R; ++i) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        xh[k][j] = (xh[k][j] - m) * r;
-        if (live) dw[k][j] += g[k][j] * xh[k][j], db[k][j] += g[k][j];
-        g[k][j] *= w[k][j];
-        s1 += g[k][j], s2 += g[k][j] * xh[k][j];
+      for (int k = 0; k < NV; ++k) {
+        const uint32_t at = (k * 64 * WAVES + lane) * E;
+        unpack<T>(piece_fix<T>(rx[i][k], at, d), xh[i][k]);
+        unpack<T>(piece_fix<T>(rg[i][k], at, d), g[i][k]);
+        add[i][k] = rb[i][k];
       }
-    group_sum<WAVES>(s1, s2, slot);
-    if (!live) continue;
+      m[i] = mean[i], r[i] = rstd[i];
+    }
+    if (first + R * step < P.n) load(t + R * step);
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-      store_grad((T *)P.dx + t * P.dx_row, (k * 64 * WAVES + lane) * E, d, P.dx_base, add[k], r, s1 * per, s2 * per, g[k], xh[k]);
+    for (int i = 0; i < R; ++i) {
+      const bool live = t + i * step < P.n;
+      float s1 = 0, s2 = 0;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          xh[i][k][j] = (xh[i][k][j] - m[i]) * r[i];
+          if (live) dw[k][j] += g[i][k][j] * xh[i][k][j], db[k][j] += g[i][k][j];
+          g[i][k][j] *= w[k][j];
+          s1 += g[i][k][j], s2 += g[i][k][j] * xh[i][k][j];
+        }
+      sum[2 * i] = s1, sum[2 * i + 1] = s2;
+    }
+    group_sum<WAVES>(sum, slot);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (t + i * step >= P.n) continue;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        store_grad((T *)P.dx + (t + i * step) * P.dx_row, (k * 64 * WAVES + lane) * E, d, P.dx_base, add[i][k], r[i], sum[2 * i] * per,
+                   sum[2 * i + 1] * per, g[i][k], xh[i][k]);
+    }
   }
   // This workgroup's part: its groups' sums, through LDS.
   float *part = P.part + (uint64_t)blockIdx.x * 2 * P.pitch;
