@@ -762,7 +762,8 @@ int fiona_policy_loss(const fiona_token_loss *loss, const fiona_policy_args *arg
  *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *     p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
  *   param, grad  device, of the desc's type; param is written
- *   master       device, float32, or NULL.  With it p is the master, and param its value rounded
+ *   master       device, float32, or NULL.  With it p is the master, and param its value rounded;
+ *                without, what a step changes by less than half a unit of a 16-bit param is lost
  *   m, v         device: float32 (state_bits 32), or (8) e4m3 values c of blocks of
  *                FIONA_ADAMW_BLOCK elements, counted from the tensor's first, that stand
  *                for m = c m_scale and sqrt(v) = c v_scale of their block
@@ -801,7 +802,7 @@ typedef struct fiona_adamw_tensor {
 
 typedef struct fiona_adamw_desc {
   uint32_t type, state_bits, n_tensor, seed;
-  double beta1, beta2, eps;              /* betas in [0, 1), eps > 0 */
+  double beta1, beta2, eps;              /* betas in [0, 1), eps a normal float32 > 0 */
   const fiona_adamw_tensor *tensors;     /* host, [n_tensor] */
 } fiona_adamw_desc;
 

@@ -910,8 +910,8 @@ def policy_loss(tl: TokenLoss, logits, targets, old, advantages, loss, logps, dl
 
 
 class AdamW(_Handle):
-    """An optimiser over many tensors (fiona_adamw_create), which it keeps: lists of contiguous tensors of the same shape at
-    the same place.  params, grads: float32, float16 or bfloat16; masters: float32, beside 16-bit parameters; m, v: float32,
+    """An optimiser over many tensors (fiona_adamw_create), whose memory it keeps: lists of contiguous tensors of the same
+    shape at the same place.  params, grads: float32, float16 or bfloat16; masters: float32, beside 16-bit parameters; m, v: float32,
     or float8_e4m3fn with m_scales, v_scales float32 [ceil(n / 256)] (v then holds the root).  weight_decay: one for all or
     a list.  Parameters may require a gradient: a step is not recorded."""
 
@@ -923,7 +923,9 @@ class AdamW(_Handle):
 
         _lm_lib()
         lists = {"params": params, "grads": grads, "m": m, "v": v, "masters": masters, "m_scales": m_scales, "v_scales": v_scales}
-        lists = {k: list(t) for k, t in lists.items() if t is not None}
+        # (aliases: their memory stays, whatever becomes of the tensors given)
+        lists = {k: [x if x is None or x.requires_grad and k != "params" else x.detach() for x in t]
+                 for k, t in lists.items() if t is not None}
         n = len(lists["params"])
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
         for name, t in list(lists.items()) + [("weight_decay", decay)]:
@@ -944,14 +946,12 @@ class AdamW(_Handle):
             at = []
             for name, dtype, want in kinds:
                 t = lists[name][i] if name in lists else None
-                if t is not None and name == "params":
-                    t = t.detach()
                 at.append(_packed(t, "%s[%d]" % (name, i), dtype, want, self.device) if t is not None else 0)
             packed.append(_ADAMW_TENSOR.pack(*at, count, decay[i]))
         table = ctypes.create_string_buffer(b"".join(packed), max(1, n * _ADAMW_TENSOR.size))
         if n:
             _stream_of(None, self.device)      # (the current device is the tensors')
-        self._create("fiona_adamw_create", _ADAMW_DESC.pack(code, 8 if small else 32, n, int(seed), betas[0], betas[1], eps,
+        self._create("fiona_adamw_create", _ADAMW_DESC.pack(code, 8 if small else 32, n, int(seed) & 0xFFFFFFFF, betas[0], betas[1], eps,
                                                             ctypes.addressof(table)))
         self._tensors = lists
         # What a step writes, tensors that share a version counter once.

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -125,7 +126,7 @@ int fiona_adamw_create(const fiona_adamw_desc *desc, fiona_adamw **out) {
   if (!desc) return FIONA_ERR_ARG;
   const fiona_adamw_desc &D = *desc;
   if (!known_type(D.type) || (D.state_bits != 8 && D.state_bits != 32)) return FIONA_ERR_UNSUPPORTED;
-  if (!(D.beta1 >= 0) || !(D.beta1 < 1) || !(D.beta2 >= 0) || !(D.beta2 < 1) || !((float)D.eps > 0) || !std::isfinite(D.eps) ||
+  if (!(D.beta1 >= 0) || !(D.beta1 < 1) || !(D.beta2 >= 0) || !(D.beta2 < 1) || !((float)D.eps >= FLT_MIN) || !std::isfinite((float)D.eps) ||
       (D.n_tensor && !D.tensors))
     return FIONA_ERR_ARG;
   fiona_adamw *H = new (std::nothrow) fiona_adamw;

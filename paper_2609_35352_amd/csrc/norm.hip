@@ -54,8 +54,8 @@ void with_shape(uint32_t q, F f) {
 
 // The same in the backward pass with the weights' gradients, where a lane holds at most
 // 16 elements: with their sums, weights and the next row that is a hundred registers
-// (32 elements, rows of 16384, spilled: 413 us for 2048 of them, 353 in 32 bits; a pass
-// over columns takes 38 beside 55 for dx).
+// (32 elements, rows of 16384, spilled: 413 us for 2048 of them in bfloat16, 353 in 32
+// bits; a pass over columns takes 29 and 48 beside 55 and 92 for dx).
 constexpr uint32_t kMostSums = 8192;
 template <typename T, typename F>
 void with_grad_shape(uint32_t q, F f) {
@@ -181,9 +181,11 @@ int fiona_layer_norm_backward(const fiona_norm *norm, const fiona_norm_backward_
     using T = decltype(t);
     using W = decltype(v);
     constexpr uint32_t E = fiona::kLaneElems<T>;
-    if (sums && columns)    // (before dx, which may be dy or x)
-      hipLaunchKernelGGL(fiona::norm_column_kernel<T>, dim3((D.width + 255) / 256, parts), dim3(256), 0, stream, P);
     const uint32_t q = (D.width + E - 1) / E;
+    if (sums && D.width < E)    // (before dx, which may be dy or x)
+      hipLaunchKernelGGL(fiona::norm_narrow_column_kernel<T>, dim3(parts), dim3(64), 0, stream, P);
+    else if (sums && columns)
+      hipLaunchKernelGGL(fiona::norm_column_kernel<T>, dim3((q + 255) / 256, parts), dim3(256), 0, stream, P);
     if (D.width < E) {
       if (A.n) hipLaunchKernelGGL((fiona::norm_narrow_grad_kernel<T, W>), dim3((A.n + 255) / 256), dim3(256), 0, stream, P);
     } else if (sums && !columns) {

@@ -77,10 +77,8 @@ template <typename T, typename W, int WAVES, int NV>
 __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_kernel(NormParams P) {
   constexpr int E = kLaneElems<T>, GROUPS = kNormThreads<WAVES> / 64 / WAVES;
   const uint32_t lane = threadIdx.x % (64 * WAVES), d = P.d;
-  uint64_t t = (uint64_t)blockIdx.x * GROUPS + wave_index() / WAVES;
-  const bool live = t < P.n;
-  if (WAVES == 1 && !live) return;
-  if (!live) t = P.n - 1;
+  const uint64_t t = (uint64_t)blockIdx.x * GROUPS + wave_index() / WAVES;
+  if (t >= P.n) return;      // (groups of one wavefront, which meet at no barrier)
   const T *x = (const T *)P.x + t * P.x_row, *r = (const T *)P.residual + (P.residual ? t * P.residual_row : 0);
   u4 raw[NV], add[NV];
 #pragma unroll
@@ -119,7 +117,6 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_kernel(NormParams P)
   }
   group_sum<WAVES>(square, 1);
   const float rstd = 1 / sqrtf(square[0] / d + P.eps);
-  if (!live) return;
   T *y = (T *)P.y + t * P.y_row, *total = (T *)P.total + (P.total ? t * P.total_row : 0);
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
@@ -170,8 +167,8 @@ template <typename T, typename W, int WAVES, int NV>
 __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grad_kernel(NormGradParams P) {
   constexpr int E = kLaneElems<T>, GROUPS = kNormThreads<WAVES> / 64 / WAVES;
   const uint32_t lane = threadIdx.x % (64 * WAVES), d = P.d;
-  uint64_t t = (uint64_t)blockIdx.x * GROUPS + wave_index() / WAVES;
-  if (t >= P.n) return;      // (groups of one wavefront: the others fill their workgroup)
+  const uint64_t t = (uint64_t)blockIdx.x * GROUPS + wave_index() / WAVES;
+  if (t >= P.n) return;
   const T *x = (const T *)P.x + t * P.x_row, *dy = (const T *)P.dy + t * P.dy_row;
   const T *base = (const T *)P.dx_base + (P.dx_base ? t * P.dx_base_row : 0);
   u4 rx[NV], rg[NV], rb[NV];
@@ -335,19 +332,56 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(NormGradParams P) {
   if (out && c < P.d) out[c] = (W)s;
 }
 
-// Rows shorter than a piece, or too long for their sums to stay in registers: a part of
-// the weights' gradients for 256 columns, a thread to a column.
+// Rows too long for their sums to stay in registers beside them: a part of the weights'
+// gradients alone, a thread to a piece of columns, four rows of it in flight.
 template <typename T>
 __global__ void __launch_bounds__(256) norm_column_kernel(NormGradParams P) {
-  const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+  constexpr int E = kLaneElems<T>, U = 4;
+  const uint32_t at = (blockIdx.x * 256 + threadIdx.x) * E, d = P.d;
+  if (at >= d) return;
+  float dw[E], db[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) dw[j] = db[j] = 0;
+  for (uint64_t first = blockIdx.y; first < P.n; first += U * gridDim.y) {
+    u4 rx[U], rg[U];
+    float mean[U], rstd[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint64_t t = first + u * gridDim.y < P.n ? first + u * gridDim.y : first;
+      rx[u] = load_shared(piece_at((const T *)P.x + t * P.x_row, at, d)), rg[u] = load_shared(piece_at((const T *)P.dy + t * P.dy_row, at, d));
+      mean[u] = P.mean[t], rstd[u] = P.rstd[t];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (first + u * gridDim.y >= P.n) continue;
+      float x[E], g[E];
+      unpack<T>(piece_fix<T>(rx[u], at, d), x);
+      unpack<T>(piece_fix<T>(rg[u], at, d), g);
+#pragma unroll
+      for (int j = 0; j < E; ++j) dw[j] += g[j] * ((x[j] - mean[u]) * rstd[u]), db[j] += g[j];
+    }
+  }
+  float *part = P.part + (uint64_t)blockIdx.y * 2 * P.pitch + at;
+#pragma unroll
+  for (int j = 0; j < E; j += 4) {
+    if (at + j >= d) continue;      // (the pitch is in whole steps of 4)
+    *(f4 *)(part + j) = (f4){dw[j], dw[j + 1], dw[j + 2], dw[j + 3]};
+    *(f4 *)(part + P.pitch + j) = (f4){db[j], db[j + 1], db[j + 2], db[j + 3]};
+  }
+}
+
+// Rows shorter than a piece: a thread to a column.
+template <typename T>
+__global__ void __launch_bounds__(64) norm_narrow_column_kernel(NormGradParams P) {
+  const uint32_t i = threadIdx.x;
   if (i >= P.d) return;
   float dw = 0, db = 0;
-  for (uint64_t t = blockIdx.y; t < P.n; t += gridDim.y) {
+  for (uint64_t t = blockIdx.x; t < P.n; t += gridDim.x) {
     const float dy = (float)((const T *)P.dy)[t * P.dy_row + i];
     dw += dy * (((float)((const T *)P.x)[t * P.x_row + i] - P.mean[t]) * P.rstd[t]);
     db += dy;
   }
-  float *part = P.part + (uint64_t)blockIdx.y * 2 * P.pitch;
+  float *part = P.part + (uint64_t)blockIdx.x * 2 * P.pitch;
   part[i] = dw, part[P.pitch + i] = db;
 }
 

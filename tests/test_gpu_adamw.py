@@ -106,7 +106,7 @@ def test_step(dtype, master, bits, shift):
 @pytest.mark.parametrize("bits", [32, 8])
 def test_first_steps_scale_and_decay(bits):
     dev = _dev()
-    for step_no, scale, betas, decay, eps in ((1, 0.25, (0.9, 0.999), 0.0, 1e-8), (1000000, 3.0, (0.95, 0.99), 0.3, 1e-3), (2, 1.0, (0.5, 0.5), 0.1, 1e-6)):
+    for step_no, scale, betas, decay, eps in ((4, 1.0, (0.0, 0.0), 0.1, 1e-6), (1, 0.25, (0.9, 0.999), 0.0, 1e-8), (1000000, 3.0, (0.95, 0.99), 0.3, 1e-3), (2, 1.0, (0.5, 0.5), 0.1, 1e-6)):
         c = _tensors([700, 256, 3000], F32, False, bits, seed=step_no % 97)
         t = _move(c, dev)
         opt = fiona.AdamW(**t, betas=betas, eps=eps, weight_decay=decay)
