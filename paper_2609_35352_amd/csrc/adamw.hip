@@ -22,8 +22,6 @@ struct fiona_adamw {
 
 namespace {
 
-constexpr uint64_t kWorkgroups = 2048;
-
 struct Piece {
   uint64_t at, end;
   bool written;
@@ -41,27 +39,16 @@ bool pieces_overlap(std::vector<Piece> &pieces) {
   return false;
 }
 
-// Elements of a chunk for n in all: whole steps of a workgroup's wavefronts, few enough
-// to go round the GPU, but not below one block to a wavefront.
-uint64_t chunk_of(uint64_t n) {
-  const uint64_t most = fiona::kChunkBlocks * FIONA_ADAMW_BLOCK, least = 4 * FIONA_ADAMW_BLOCK, want = n / kWorkgroups;
-  return std::max(least, std::min(most, want / least * least));
-}
-
-int check_tensors(const fiona_adamw_desc &D, uint64_t &chunk, uint64_t &chunks) {
+int check_tensors(const fiona_adamw_desc &D, uint64_t &chunks) {
   const uint64_t e = type_size(D.type);
   const bool small = D.state_bits == 8;
   std::vector<Piece> pieces;
-  uint64_t total = 0;
-  for (uint32_t i = 0; i < D.n_tensor; ++i) {
-    if (D.tensors[i].n >= (uint64_t)1 << 40) return FIONA_ERR_UNSUPPORTED;
-    total += D.tensors[i].n;
-  }
-  chunk = chunk_of(total), chunks = 0;
+  chunks = 0;
   for (uint32_t i = 0; i < D.n_tensor; ++i) {
     const fiona_adamw_tensor &T = D.tensors[i];
     if (!(T.weight_decay >= 0) || !std::isfinite(T.weight_decay)) return FIONA_ERR_ARG;
     if (!T.n) continue;
+    if (T.n >= (uint64_t)1 << 40) return FIONA_ERR_UNSUPPORTED;
     if (!T.param || !T.grad || !T.m || !T.v || (T.m_scale != nullptr) != small || (T.v_scale != nullptr) != small)
       return FIONA_ERR_ARG;
     if (T.master && D.type == FIONA_F32) return FIONA_ERR_ARG;
@@ -74,19 +61,19 @@ int check_tensors(const fiona_adamw_desc &D, uint64_t &chunk, uint64_t &chunks) 
     };
     add(T.param, T.n * e, true), add(T.grad, T.n * e, false), add(T.master, T.n * 4, true);
     add(T.m, T.n * s, true), add(T.v, T.n * s, true), add(T.m_scale, blocks * 4, true), add(T.v_scale, blocks * 4, true);
-    chunks += (T.n + chunk - 1) / chunk;
+    chunks += (T.n + fiona::kChunk - 1) / fiona::kChunk;
   }
   if (chunks >= 1u << 24) return FIONA_ERR_UNSUPPORTED;   // (times 256 threads: below 2^32)
   return pieces_overlap(pieces) ? FIONA_ERR_ALIAS : FIONA_OK;
 }
 
 int make(const fiona_adamw_desc &D, fiona_adamw *H) {
-  uint64_t step = 0, n_chunk = 0;
-  const int rc = check_tensors(D, step, n_chunk);
+  uint64_t n_chunk = 0;
+  const int rc = check_tensors(D, n_chunk);
   if (rc != FIONA_OK) return rc;
   std::vector<fiona::AdamwChunk> chunks;
   chunks.reserve(n_chunk);
-  const uint64_t e = type_size(D.type), s = D.state_bits == 8 ? 1 : 4;
+  const uint64_t e = type_size(D.type), s = D.state_bits == 8 ? 1 : 4, step = fiona::kChunk;
   uint64_t first = 0;
   for (uint32_t i = 0; i < D.n_tensor; ++i) {
     const fiona_adamw_tensor &T = D.tensors[i];

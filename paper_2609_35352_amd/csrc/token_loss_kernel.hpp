@@ -3,7 +3,23 @@
 // A row's log sum of exponentials in parts, as a softmax over a long axis: a part with
 // elements J has m_J = max z_j and s_J = sum exp(z_j - m_J), and two parts join as
 // m = max(m_1, m_2), s = sum_i s_i exp(m_i - m).  Exponentials are to base 2, of the
-// difference of two logits, taken before it is scaled.
+// difference of two logits, taken before it is scaled (a scaled maximum, rounded, would be
+// off by 2^-24 of itself).
+//
+// The policy loss of a token depends on its own row alone: where there are enough rows, or
+// short ones, a workgroup holds one in its registers, packed, and reads it once.  The
+// preference loss needs every row of a pair before the first of their gradients: parts,
+// then pairs, then gradients, in three launches, and rows read twice.  Long rows that are
+// few are split over workgroups in either.
+//
+// What bounds them: memory, and the vector units close behind (an exponential takes four
+// issue slots; parts of bfloat16 rows keep them 55% busy).  Measured: 2700 rows of 131072
+// in bfloat16 read and written once (1.49 GB with 300 rows of zeros) 278 us, 5.4 TB/s; 7955
+// rows of 32768 74 us for the parts (419 MB, 5.7 TB/s), 6 for the pairs, 151 for the
+// gradients (419 MB again and 521 MB written, 6.2 TB/s: the rows read last are the first
+// again, some of them still in the memory-side cache; read past the caches in both passes
+// 66 and 165).  24 rows of 50021 in 32 bits: 4.0 and 4.6 us, each one launch and its chain
+// of loads.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
