@@ -954,9 +954,14 @@ class AdamW(_Handle):
         self._create("fiona_adamw_create", _ADAMW_DESC.pack(code, 8 if small else 32, n, int(seed) & 0xFFFFFFFF, betas[0], betas[1], eps,
                                                             ctypes.addressof(table)))
         self._tensors = lists
-        # What a step writes, tensors that share a version counter once.
-        self._written = list({id(b): b for t in (lists[k] for k in lists if k != "grads") for x in t if x is not None
-                              for b in (x if x._base is None else x._base,)}.values())
+        # What a step writes, tensors that share a version counter (views of one) once.
+        self._written = list({id(b): b for b in (_root(x) for k in lists if k != "grads" for x in lists[k] if x is not None)}.values())
+
+
+def _root(t):
+    while t._base is not None:
+        t = t._base
+    return t
 
 
 def adamw_step(opt: AdamW, lr, step, grad_scale=None, stream=None) -> None:

@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grads_kernel(NormGra
                    sum[2 * i + 1] * per, g[i][k], xh[i][k]);
     }
   }
-  // This workgroup's part: its groups' sums, through LDS.
+  // This workgroup's part, or with no other the gradients: its groups' sums, through LDS.
   float *part = P.part + (uint64_t)blockIdx.x * 2 * P.pitch;
   if constexpr (GROUPS > 1) {
     __shared__ f4 sh[GROUPS][2][64 * WAVES * NV * E / 4];
@@ -310,7 +310,12 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grads_kernel(NormGra
       float a = 0, b = 0;
 #pragma unroll
       for (int q = 0; q < GROUPS; ++q) a += ((const float *)sh[q][0])[i], b += ((const float *)sh[q][1])[i];
-      part[i] = a, part[P.pitch + i] = b;
+      if (P.parts > 1) {
+        part[i] = a, part[P.pitch + i] = b;
+      } else {
+        if (P.dweight) ((W *)P.dweight)[i] = (W)a;
+        if (P.dbias) ((W *)P.dbias)[i] = (W)b;
+      }
     }
   } else {
 #pragma unroll
@@ -319,8 +324,17 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grads_kernel(NormGra
       for (int j = 0; j < E; j += 4) {
         const uint32_t at = (k * 64 * WAVES + lane) * E + j;
         if (at >= d) continue;      // (the pitch is in whole steps of 4)
-        *(f4 *)(part + at) = (f4){dw[k][j], dw[k][j + 1], dw[k][j + 2], dw[k][j + 3]};
-        *(f4 *)(part + P.pitch + at) = (f4){db[k][j], db[k][j + 1], db[k][j + 2], db[k][j + 3]};
+        if (P.parts > 1) {
+          *(f4 *)(part + at) = (f4){dw[k][j], dw[k][j + 1], dw[k][j + 2], dw[k][j + 3]};
+          *(f4 *)(part + P.pitch + at) = (f4){db[k][j], db[k][j + 1], db[k][j + 2], db[k][j + 3]};
+          continue;
+        }
+#pragma unroll
+        for (int i = j; i < j + 4; ++i) {
+          if (at + i - j >= d) continue;
+          if (P.dweight) ((W *)P.dweight)[at + i - j] = (W)dw[k][i];
+          if (P.dbias) ((W *)P.dbias)[at + i - j] = (W)db[k][i];
+        }
       }
   }
 }

@@ -91,7 +91,8 @@ void launch_grad(const fiona::TokenParams &P, const fiona::PolicyParams &Q, hipS
 // launches, parts and gradient, without the gap between them / of whole rows, in
 // bfloat16: 2 x 16000 7.2 / 4.9, 64 x 32768 8.9 / 7.6, 16 x 64000 7.6 / 10.4, 64 x 64000
 // 11.8 / 11.1, 64 x 131072 12.8 / 18.2, 100 x 131072 22.8 / 19.4, 200 x 131072 30.2 /
-// 24.7, 3000 x 131072 411 / 290.
+// 24.7, 3000 x 131072 411 / 290.  (Rows of 24 pieces a lane spill: 1500 x 78213 in 32 bits 233 /
+// 233, 1500 x 190000 in bfloat16 284 / 302.)
 bool whole_rows(uint32_t n, uint32_t pieces) { return pieces <= 4096 || (pieces <= 1024 * 16 && n >= pieces / 192); }
 
 // The policy loss with whole rows in registers.
