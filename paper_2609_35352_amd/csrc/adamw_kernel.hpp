@@ -49,12 +49,18 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
 
 // y in [0, 448] to one of the two neighbouring e4m3 values: up where what it is above
 // the lower one, in steps between them, and a dither in (0, 1) make one together.
-// one_and: the dither and one, as 24 bits hold it.  Exponents stay those of the value's
-// binade, from 2^-6 (the smallest normal value) on.
-__device__ __forceinline__ float to_code(float y, float one_and) {
+// Exponents stay those of the value's binade, from 2^-6 (the smallest normal value) on.
+__device__ __forceinline__ float to_code(float y, float dither) {
   const uint32_t e = __builtin_bit_cast(uint32_t, y) & 0x7F800000u, u = e > (121u << 23) ? e : 121u << 23;
   const float step = __builtin_bit_cast(float, u - (3u << 23)), per = __builtin_bit_cast(float, (257u << 23) - u);
-  return __builtin_fmaf(__builtin_floorf(__builtin_fmaf(y, per, one_and)), step, -step);
+  return __builtin_floorf(__builtin_fmaf(y, per, dither)) * step;      // (both products are exact)
+}
+
+// x^1/2 as rounded, from the hardware's x^-1/2 (a unit off at most) and one correction;
+// half the instructions of the compiler's.  Below 2^-126 less than the root, but above zero.
+__device__ __forceinline__ float root_of(float x) {
+  const float y = __builtin_amdgcn_rsqf(fmaxf(x, 0x1p-126f)), r = x * y;
+  return __builtin_fmaf(__builtin_fmaf(-r, r, x), 0.5f * y, r);
 }
 
 // Four consecutive elements of T, at any address that they may stand at.
@@ -153,18 +159,34 @@ __device__ __forceinline__ Four<T> four_of(const float (&x)[4]) {
   return f;
 }
 
-// A block's values as codes, and its scale.  A value that is no number gets the code
-// for that; an infinity makes the scale one, and with it the block.
+// The largest magnitudes of a block's m, in lanes 0 to 31, and of its roots, in lanes 32
+// to 63: from the 16 lanes of a row on one register carries both.
+__device__ __forceinline__ float block_tops(const float (&m)[4], const float (&r)[4]) {
+  auto row = [](float x) {
+    x = fmaxf(x, dpp<0xB1>(x));
+    x = fmaxf(x, dpp<0x4E>(x));
+    x = fmaxf(x, dpp<0x141>(x));
+    return fmaxf(x, dpp<0x140>(x));
+  };
+  const float a = row(fmaxf(fmaxf(__builtin_fabsf(m[0]), __builtin_fabsf(m[1])), fmaxf(__builtin_fabsf(m[2]), __builtin_fabsf(m[3]))));
+  const float b = row(fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3])));
+  const auto h = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), false, false);
+  const float x = fmaxf(__builtin_bit_cast(float, (uint32_t)h[0]), __builtin_bit_cast(float, (uint32_t)h[1]));
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto q = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)q[0]), __builtin_bit_cast(float, (uint32_t)q[1]));
+}
+
+// Values as codes, per: 448 over the block's largest magnitude (zero where there is none).
+// A value that is no number gets the code for that; an infinity makes per zero and the
+// scale one, and with it the block.
 template <bool ROOTS>
-__device__ __forceinline__ float block_codes(float (&x)[4], const float (&one_and)[4]) {
-  const float t = wave_max(fmaxf(fmaxf(__builtin_fabsf(x[0]), __builtin_fabsf(x[1])), fmaxf(__builtin_fabsf(x[2]), __builtin_fabsf(x[3]))));
-  const float most = t < 0x1p-100f ? 0.f : t, per = most > 0 ? 448.f * __builtin_amdgcn_rcpf(most) : 0.f;
+__device__ __forceinline__ void codes_of(float (&x)[4], const float (&dither)[4], float per) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float y = __builtin_fabsf(x[j]) * per, c = to_code(y > 448.f ? 448.f : y, one_and[j]);
-    x[j] = ROOTS ? x[j] > 0 && most > 0 ? fmaxf(c, 0x1p-9f) : c : __builtin_copysignf(c, x[j]);
+    const float y = __builtin_fabsf(x[j]) * per, c = to_code(__builtin_elementwise_minimum(y, 448.f), dither[j]);
+    x[j] = ROOTS ? x[j] * per > 0 ? fmaxf(c, 0x1p-9f) : c : __builtin_copysignf(c, x[j]);
   }
-  return most * (1 / 448.f);
 }
 
 // A workgroup to a chunk, a wavefront to a block, four elements to a lane.  (Four blocks
@@ -202,24 +224,34 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams P) {
   for (int j = 0; j < 4; ++j) {
     const float gj = g[j] * gs;
     if (SMALL) m[j] *= sm, v[j] *= sv, v[j] *= v[j];
-    m[j] = __builtin_fmaf(P.b1, m[j], P.a1 * gj);
-    v[j] = __builtin_fmaf(P.a2 * gj, gj, P.b2 * v[j]);
-    const float r = __builtin_amdgcn_sqrtf(v[j]);
+    // Each of the states' operations is rounded by itself, so that they are the same wherever
+    // the same operations are done in 32 bits.
+    float r;
+    {
+#pragma clang fp contract(off)
+      m[j] = P.b1 * m[j] + P.a1 * gj;
+      v[j] = P.b2 * v[j] + P.a2 * (gj * gj);
+      r = SMALL ? root_of(v[j]) : __builtin_amdgcn_sqrtf(v[j]);
+    }
     x[j] = x[j] * keep - lr * (m[j] * c1 * __builtin_amdgcn_rcpf(r * c2 + P.eps));
     if (sizeof(T) == 2) asm volatile("" : "+v"(x[j]));   // (param is this value rounded, not its last product's binary16 form)
     if (SMALL) {
       v[j] = r;
       const uint32_t h = mix((C.first + i + j) ^ key);
-      // one + (16 bits + 1/2) / 2^16, the bits below the leading one's seven places up
-      um[j] = __builtin_bit_cast(float, (h & 0xFFFFu) << 7 | 0x3F800040u);
-      uv[j] = __builtin_bit_cast(float, (h >> 9 & 0x7FFF80u) | 0x3F800040u);
+      // (16 bits + 1/2) / 2^16: one and that, the bits below the leading one's seven places up, less one
+      um[j] = __builtin_bit_cast(float, (h & 0xFFFFu) << 7 | 0x3F800040u) - 1.f;
+      uv[j] = __builtin_bit_cast(float, (h >> 9 & 0x7FFF80u) | 0x3F800040u) - 1.f;
     }
   }
   if (C.master) store_four(C.master, i, whole, valid, four_of<float>(x));
   store_four(C.param, i, whole, valid, four_of<T>(x));
   if constexpr (SMALL) {
-    const float tm = block_codes<false>(m, um), tv = block_codes<true>(v, uv);
-    if (lane == 0) C.m_scale[b] = tm, C.v_scale[b] = tv;
+    const float t = block_tops(m, v), most = t < 0x1p-100f ? 0.f : t, rcp = __builtin_amdgcn_rcpf(most);
+    const float per = most > 0 ? 448.f * __builtin_fmaf(__builtin_fmaf(-most, rcp, 1.f), rcp, rcp) : 0.f;
+    if (lane % 32 == 0) (lane ? C.v_scale : C.m_scale)[b] = most * (1 / 448.f);
+    auto at = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, per), l)); };
+    codes_of<false>(m, um, at(0));
+    codes_of<true>(v, uv, at(32));
   }
   store_four(C.m, i, whole, valid, four_of<S>(m));
   store_four(C.v, i, whole, valid, four_of<S>(v));
