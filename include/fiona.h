@@ -770,7 +770,7 @@ int fiona_policy_loss(const fiona_token_loss *loss, const fiona_policy_args *arg
  *   m_scale, v_scale  device, float32, one to a block (a last short one as well); NULL with 32 bits
  *   lr, step, grad_scale  device, one float32, int32 (from 1 on; less counts as 1) and float32 (NULL:
  *                1): read when the step runs, so that a captured one follows them
- * 8-bit states: the new m and v are used in 32 bits, then rounded to one of the two
+ * 8-bit states: the new m and v, from operations in 32 bits each rounded by itself, are used, then rounded to one of the two
  * neighbouring values, up with the probability that keeps their mean (rounded to
  * nearest, beta2 v would stay v for ever); sqrt(v) > 0 is never rounded to zero.  A
  * block's scale is its largest magnitude / 448 (zero, as its values, below 2^-100; v below 2^-126 counts

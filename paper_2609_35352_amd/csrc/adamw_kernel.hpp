@@ -7,8 +7,8 @@
 // with the probability of what it is above the lower, which keeps its mean.
 //
 // What bounds it: memory, 28 bytes an element with 32-bit states, 16 with 8-bit ones beside
-// masters (38 million elements: 171 us, 6.3 TB/s, and 107 us, 5.7; a copy reaches 5.2);
-// with 8-bit states and neither masters nor 32-bit parameters (10 bytes, 101 us) the vector
+// masters (38 million elements: 171 us, 6.3 TB/s, and 103 us, 6.0; a copy reaches 5.2);
+// with 8-bit states and neither masters nor 32-bit parameters (10 bytes, 95 us) the vector
 // units: about 90 instructions an element, two 32-bit products of the dither's among them.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -159,6 +159,10 @@ __device__ __forceinline__ Four<T> four_of(const float (&x)[4]) {
   return f;
 }
 
+__device__ __forceinline__ float lane_value(float x, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+
 // The largest magnitudes of a block's m, in lanes 0 to 31, and of its roots, in lanes 32
 // to 63: from the 16 lanes of a row on one register carries both.
 __device__ __forceinline__ float block_tops(const float (&m)[4], const float (&r)[4]) {
@@ -190,8 +194,8 @@ __device__ __forceinline__ void codes_of(float (&x)[4], const float (&dither)[4]
 }
 
 // A workgroup to a chunk, a wavefront to a block, four elements to a lane.  (Four blocks
-// to a wavefront, all their loads first: 117 us instead of 107 for the 38 million elements
-// above, 190 instead of 171 with 32-bit states.)
+// to a wavefront, all their loads first: 10 us more for the 38 million elements above, 19
+// more with 32-bit states.)
 template <typename T, bool SMALL>
 __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams P) {
   using S = std::conditional_t<SMALL, uint8_t, float>;
@@ -212,8 +216,11 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams P) {
   if (SMALL) sm = C.m_scale[b], sv = C.v_scale[b];
   __builtin_amdgcn_sched_barrier(0);
   const int32_t step = *P.step < 1 ? 1 : *P.step;
-  // 1 - beta^t without the difference of two near numbers.
-  const float c1 = 1.f / -expm1f(step * P.log_b1), c2 = 1.f / sqrtf(-expm1f(step * P.log_b2)), lr = *P.lr;
+  // 1 / (1 - beta1^t) in the lower lanes, 1 / (1 - beta2^t)^1/2 in the upper ones, without
+  // the difference of two near numbers (both in every lane: a tenth more instructions).
+  const bool low = lane < 32;
+  const float left = -expm1f(step * (low ? P.log_b1 : P.log_b2)), c = low ? __builtin_amdgcn_rcpf(left) : __builtin_amdgcn_rsqf(left);
+  const float c1 = lane_value(c, 0), c2 = lane_value(c, 32), lr = *P.lr;
   const float gs = P.grad_scale ? *P.grad_scale : 1.f, keep = 1.f - lr * C.decay;
   const uint32_t key = mix((uint32_t)step * 0x9E3779B1u + P.seed);
   float g[4], m[4], v[4], x[4], um[4], uv[4];
@@ -249,9 +256,8 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams P) {
     const float t = block_tops(m, v), most = t < 0x1p-100f ? 0.f : t, rcp = __builtin_amdgcn_rcpf(most);
     const float per = most > 0 ? 448.f * __builtin_fmaf(__builtin_fmaf(-most, rcp, 1.f), rcp, rcp) : 0.f;
     if (lane % 32 == 0) (lane ? C.v_scale : C.m_scale)[b] = most * (1 / 448.f);
-    auto at = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, per), l)); };
-    codes_of<false>(m, um, at(0));
-    codes_of<true>(v, uv, at(32));
+    codes_of<false>(m, um, lane_value(per, 0));
+    codes_of<true>(v, uv, lane_value(per, 32));
   }
   store_four(C.m, i, whole, valid, four_of<S>(m));
   store_four(C.v, i, whole, valid, four_of<S>(v));
