@@ -655,7 +655,7 @@ int fiona_layer_norm(const fiona_norm_args *args, hipStream_t stream);
  *   dweight, dbias      device, [width], of the weight's type, overwritten (zeros with n 0);
  *                       NULL: not wanted
  * fiona_norm_create: the workspace (the parts of dweight and dbias) for up to
- * max_rows rows.  Asynchronous on stream; at most two kernel launches, allocates nothing.
+ * max_rows rows.  Asynchronous on stream; at most three kernel launches, allocates nothing.
  * The workspace is shared by the handle's calls: one handle must not be used by
  * two streams, or in two graphs that run, at the same time.  Errors: as above, and
  * FIONA_ERR_NOMEM from fiona_norm_create.
@@ -768,22 +768,24 @@ int fiona_policy_loss(const fiona_token_loss *loss, const fiona_policy_args *arg
  *                FIONA_ADAMW_BLOCK elements, counted from the tensor's first, that stand
  *                for m = c m_scale and sqrt(v) = c v_scale of their block
  *   m_scale, v_scale  device, float32, one to a block (a last short one as well); NULL with 32 bits
+ *   weight_decay  at least zero, finite in 32 bits
  *   lr, step, grad_scale  device, one float32, int32 (from 1 on; less counts as 1) and float32 (NULL:
  *                1): read when the step runs, so that a captured one follows them
  * 8-bit states: the new m and v, from operations in 32 bits each rounded by itself, are used, then rounded to one of the two
  * neighbouring values, up with the probability that keeps their mean (rounded to
  * nearest, beta2 v would stay v for ever); sqrt(v) > 0 is never rounded to zero.  A
- * block's scale is its largest magnitude / 448 (zero, as its values, below 2^-100; v below 2^-126 counts
- * as zero).  The dither of
+ * block's scale is its largest magnitude / 448 (zero, as its values, below 2^-100; of v below 2^-126 less
+ * than the root is taken).  The dither of
  * element i is 16 bits for m (low) and 16 for v (high) of mix(i ^ mix(step 0x9E3779B1 + seed)) in
  * 32-bit arithmetic, i counting from the first tensor on, every tensor from a multiple of the block;
  *     mix(x): x ^= x >> 16; x *= 0xA3D8B167; x ^= x >> 15; x *= 0xC94F6E2B; x ^= x >> 16.
- * A gradient that is no number makes its element's states and parameter so, an infinite one with 8 bits
- * the states of its block.
+ * A gradient that is no number makes its element's states and parameter so.  With 8 bits one whose square
+ * passes float32's range does the same to v and the parameter, and an infinite one to m of its block.
  *
  * fiona_adamw_create keeps the tensors' addresses, not the tensors: they have to
  * live, where they are, as long as the handle is used.  What is written must not
- * overlap anything else of any tensor (FIONA_ERR_ALIAS).
+ * overlap anything else of any tensor (FIONA_ERR_ALIAS).  Limit: fewer than 2^24 pieces
+ * of 1024 elements, a tensor's last one counted whole (FIONA_ERR_UNSUPPORTED).
  * fiona_adamw_step: asynchronous on stream; one kernel launch, allocates nothing.
  * Errors: FIONA_ERR_ARG, FIONA_ERR_UNSUPPORTED, FIONA_ERR_ALIGN, FIONA_ERR_ALIAS,
  * FIONA_ERR_NOMEM, FIONA_ERR_HIP.

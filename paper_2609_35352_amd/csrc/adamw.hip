@@ -46,7 +46,7 @@ int check_tensors(const fiona_adamw_desc &D, uint64_t &chunks) {
   chunks = 0;
   for (uint32_t i = 0; i < D.n_tensor; ++i) {
     const fiona_adamw_tensor &T = D.tensors[i];
-    if (!(T.weight_decay >= 0) || !std::isfinite(T.weight_decay)) return FIONA_ERR_ARG;
+    if (!(T.weight_decay >= 0) || !std::isfinite((float)T.weight_decay)) return FIONA_ERR_ARG;
     if (!T.n) continue;
     if (T.n >= (uint64_t)1 << 40) return FIONA_ERR_UNSUPPORTED;
     if (!T.param || !T.grad || !T.m || !T.v || (T.m_scale != nullptr) != small || (T.v_scale != nullptr) != small)

@@ -182,8 +182,8 @@ __device__ __forceinline__ float block_tops(const float (&m)[4], const float (&r
 }
 
 // Values as codes, per: 448 over the block's largest magnitude (zero where there is none).
-// A value that is no number gets the code for that; an infinity makes per zero and the
-// scale one, and with it the block.
+// A value that is no number gets the code for that; an infinity makes per no number and
+// the scale infinite, and every code of the block the one for no number.
 template <bool ROOTS>
 __device__ __forceinline__ void codes_of(float (&x)[4], const float (&dither)[4], float per) {
 #pragma unroll

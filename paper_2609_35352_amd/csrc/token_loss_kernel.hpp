@@ -112,7 +112,7 @@ __device__ __forceinline__ void gather(const float (&x)[N], float &m, float &s) 
   m = top;
 }
 
-// Four pieces of a row, 256 of them apart, for a lane whose first one starts at `at`.
+// U pieces of a row, 256 of them apart, for a lane whose first one starts at `at`.
 // Steps that end before the row does (`whole`, the same in the workgroup) need no checks.
 template <typename T, bool NARROW, int U>
 __device__ __forceinline__ void read_step(const T *row, uint32_t at, uint32_t n, bool whole, u4 (&v)[U]) {

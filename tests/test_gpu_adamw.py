@@ -198,6 +198,44 @@ def test_a_gradient_that_is_no_number(bits):
         assert bool(torch.isnan(t["v"][0].float()[300]))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), 1e20])
+def test_infinite_gradients_and_squares_stay_with_their_block(value, bits, dtype):
+    """Other blocks are bit for bit those of a step without them, and so are the block's other parameters, masters and v."""
+    dev = _dev()
+    c = _tensors([256 * 3 + 40], dtype, dtype is BF16, bits, seed=9)
+    c["grads"][0][300] = 0
+    for k in ("m", "v"):                     # (not the block's largest without it)
+        c[k][0].view(torch.uint8 if bits == 8 else F32)[300] = 0
+    runs = []
+    for bad in (False, True):
+        t = _move(c, dev)
+        if bad:
+            t["grads"][0][300] = value
+        fiona.adamw_step(fiona.AdamW(**t, weight_decay=0.05), *_scalars(dev))
+        torch.cuda.synchronize()
+        runs.append({k: x[0].float().cpu() for k, x in t.items()})
+    plain, got = runs
+    block, outside = slice(256, 512), [i for i in range(808) if not 256 <= i < 512]
+    for k in ("params", "m", "v") + (("masters",) if dtype is BF16 else ()):
+        assert torch.equal(got[k][outside], plain[k][outside]), k
+        if k in ("params", "masters"):
+            same = plain[k][block].clone()
+            same[44] = got[k][300]
+            assert torch.equal(got[k][block].nan_to_num(7.0), same.nan_to_num(7.0)), k
+    finite = value == 1e20
+    if bits == 32:
+        assert torch.isinf(got["v"][300]) and bool(torch.isfinite(got["m"][300])) == finite
+        assert torch.isnan(got["params"][300]) != finite           # inf / inf, or a finite m over an infinite root
+        return
+    assert torch.isnan(got["v"][300]) and torch.isnan(got["params"][300])
+    assert torch.equal(torch.cat([got["v"][256:300], got["v"][301:512]]), torch.cat([plain["v"][256:300], plain["v"][301:512]]))
+    assert int(torch.isnan(got["m"][block]).sum()) == (0 if finite else 256)
+    for k in ("m_scales", "v_scales"):
+        assert torch.equal(got[k][[0, 2, 3]], plain[k][[0, 2, 3]]), k
+
+
 def test_several_steps_other_stream_and_graph_replay():
     dev = _dev()
     for bits in (32, 8):

@@ -128,6 +128,8 @@ int main(void) {
   EXPECT(FIONA_ERR_ALIAS, fiona_adamw_create(&ad, &opt));
   t[1] = tensor(1, 300), t[1].weight_decay = -1;
   EXPECT(FIONA_ERR_ARG, fiona_adamw_create(&ad, &opt));
+  t[1] = tensor(1, 300), t[1].weight_decay = 1e300;          /* infinite in 32 bits */
+  EXPECT(FIONA_ERR_ARG, fiona_adamw_create(&ad, &opt));
   t[1] = tensor(1, (uint64_t)1 << 50);
   EXPECT(FIONA_ERR_UNSUPPORTED, fiona_adamw_create(&ad, &opt));
   t[1] = tensor(1, 300);
