@@ -68,27 +68,39 @@ void with_grad_shape(uint32_t q, F f) {
   else if constexpr (wide) f(Shape<8, 4>{});
 }
 
-// Parts of the rows' sums: a workgroup's each.  512 / 1024, us with their sum: 8192 rows
-// of 4096 in bfloat16 55 / 60, 4096 of 8192 60 / 75, 2048 of 768 in 32 bits 13.2 / 17.7,
-// 8192 of 1376 in binary16 30 / 27.
+// Parts of the rows' sums: a workgroup's each, as many as are resident at once (rows of
+// several wavefronts take all registers of a compute unit with eight; 512 / 1024 parts of one
+// wavefront's rows, us with their sum: 2048 of 768 in 32 bits 13.2 / 17.7; 256 / 512 parts of the
+// others': 8192 rows of 4096 in bfloat16 50.6 / 53.9, 4096 of 8192 50.9 / 57.7, 600 of 8192
+// in binary16 16.4 / 23.2).
 constexpr uint32_t kMostParts = 512;
+uint32_t most_parts(uint32_t waves) { return waves == 1 ? kMostParts : 256; }
 // Where a lane holds one piece of a row, many rows go two at a time, for the bytes in
-// flight (one / two at a time, us: 16384 of 1376 in bfloat16 48.3 / 40.7, 8192 of 2048
-// 26.8 / 27.4, 1531 of 1373 9.9 / 10.7, 300 of 2048 6.1 / 6.8).
+// flight (one / two at a time, us, with one group to a workgroup: 16384 of 1376 in bfloat16
+// 48.3 / 40.7, 8192 of 2048 26.8 / 27.4, 1531 of 1373 9.9 / 10.7, 300 of 2048 6.1 / 6.8).
 constexpr uint32_t kTwoRows = 4096;
+// The wavefronts of a row's group there.
+uint32_t grad_waves(uint32_t type, uint32_t d) {
+  uint32_t waves = 0;
+  with_type(type, [&](auto t) {
+    constexpr uint32_t E = fiona::kLaneElems<decltype(t)>;
+    with_grad_shape<decltype(t)>((d + E - 1) / E, [&](auto s) { waves = decltype(s)::kWaves; });
+  });
+  return waves;
+}
 constexpr uint32_t pitch_of(uint32_t d) { return (d + 3) / 4 * 4; }
 bool by_columns(uint32_t type, uint32_t d) { return d < 16 / type_size(type) || d > kMostSums; }
 // Rows that one workgroup goes through, so that no parts are left to add up: four for each
 // of four groups (us on the GPU, one launch / two without the gap between them, which takes
-// the host 2 us more: 5 rows of 768 in bfloat16 4.4 / 6.4, 16 6.2 / 6.4, 32 9.9 / 7.2; two
-// rows of one group's 4096 7.5 / 6.5).
-uint32_t few_rows(uint32_t type, uint32_t d) {
-  const uint32_t e = 16 / type_size(type), q = (d + e - 1) / e;
-  return q <= (type == FIONA_F32 ? 256u : 128u) ? 16 : 1;
-}
+// the host 2 us more: 5 rows of 768 in bfloat16 4.4 / 6.4, 16 6.2 / 6.4, 32 9.9 / 7.2).
+// Of other rows one to a group.
+uint32_t few_rows(uint32_t waves) { return waves == 1 ? 16 : 1; }
 uint32_t parts_of(uint32_t type, uint32_t d, uint32_t n) {
   if (by_columns(type, d)) return std::max(1u, std::min(d > kMostSums ? 64 : kMostParts, (n + 15) / 16));
-  return n <= few_rows(type, d) ? 1 : std::min(kMostParts, n);
+  const uint32_t waves = grad_waves(type, d);
+  if (n <= few_rows(waves)) return 1;
+  const uint32_t groups = waves == 1 ? fiona::kGradGroups<1> : waves == 4 ? fiona::kGradGroups<4> : 1;
+  return std::min(most_parts(waves), (n + groups - 1) / groups);
 }
 
 }  // namespace
@@ -199,7 +211,7 @@ int fiona_layer_norm_backward(const fiona_norm *norm, const fiona_norm_backward_
     } else if (sums && !columns) {
       with_grad_shape<T>(q, [&](auto s) {
         constexpr int WAVES = decltype(s)::kWaves, NV = decltype(s)::kPieces;
-        const dim3 grid(parts), threads(fiona::kNormThreads<WAVES>);
+        const dim3 grid(parts), threads(64 * WAVES * fiona::kGradGroups<WAVES>);
         if constexpr (NV == 1) {
           if (A.n >= kTwoRows) {
             hipLaunchKernelGGL((fiona::norm_grads_kernel<T, W, WAVES, NV, 2>), grid, threads, 0, stream, P);

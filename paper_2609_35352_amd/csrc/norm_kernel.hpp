@@ -6,14 +6,14 @@
 // the result come from registers.  In the backward pass
 //     dx = rstd (u - mean u - xh mean(u xh)),  u = weight dy,  xh = (x - mean) rstd
 // takes one pair of sums over the row, and dweight = sum dy xh, dbias = sum dy one pair
-// over the rows for every column: each workgroup goes through every gridDim-th row with
-// its columns' sums in registers and leaves one part of them, and a second launch adds
-// the parts up, both in a fixed order.
+// over the rows for every column: each group of a workgroup goes through its share of the
+// rows with its columns' sums in registers, the workgroup leaves one part of them, and a
+// second launch adds the parts up, all in a fixed order.
 //
 // What bounds them: memory, at 10 to 15 operations for 4 to 16 bytes.  Measured: 16384
 // rows of 4096 in bfloat16 with a residual (537 MB) 90 us, 6.0 TB/s where a copy reaches
-// 5.2 (reads alone 7.0); its gradients for 8192 rows (269 MB, and 17 MB of parts each
-// way) 51 us and 4.7 for the parts' sum, 5.6 TB/s; a step of 8 rows of 768 4.3 us, one
+// 5.2 (reads alone 7.0); its gradients for 8192 rows (269 MB, and 8 MB of parts each
+// way) 46 us and 4.6 for the parts' sum, 6.0 TB/s; a step of 8 rows of 768 4.3 us, one
 // launch and two dependent loads.  Rows read with the weights asked for before the sums
 // instead of after them: 3.1 instead of 3.6 us for one row of 4096, 51 instead of 43 for
 // 16384 of 1373 (fewer wavefronts fit).
@@ -46,15 +46,21 @@ struct NormGradParams {
 // Workgroups: four wavefronts, or the sixteen of one group.
 template <int WAVES>
 constexpr int kNormThreads = WAVES > 4 ? 64 * WAVES : 256;
+// With the weights' gradients: groups of a workgroup, whose sums become one part (two
+// groups of four wavefronts, 256 parts / one, 512, us with the parts' sum: 8192 rows of 4096
+// in bfloat16 50.6 / 53.9, 8192 of 2048 30.4 / 33.5, 1531 of 1373 11.9 / 14.0; four groups of them
+// spill, and double the time of two rows at a time).
+template <int WAVES>
+constexpr int kGradGroups = WAVES == 1 ? 4 : WAVES == 4 ? 2 : 1;
 
 // Sums of N values over a group; `slot` alternates from call to call, so that one
 // barrier is enough.
-template <int WAVES, int N>
+template <int WAVES, int N, int THREADS = kNormThreads<WAVES>>
 __device__ __forceinline__ void group_sum(float (&x)[N], uint32_t slot) {
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
   if constexpr (WAVES > 1) {
-    __shared__ float part[2][kNormThreads<WAVES> / 64][N];
+    __shared__ float part[2][THREADS / 64][N];
     const uint32_t w = wave_index();
     if (threadIdx.x % 64 == 0)
 #pragma unroll
@@ -219,8 +225,8 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grad_kernel(NormGrad
 // dx of R rows at a time of every gridDim-th, and this workgroup's part of the weights'
 // gradients, which its lanes add up in registers over those rows.
 template <typename T, typename W, int WAVES, int NV, int R>
-__global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grads_kernel(NormGradParams P) {
-  constexpr int E = kLaneElems<T>, GROUPS = kNormThreads<WAVES> / 64 / WAVES;
+__global__ void __launch_bounds__(64 * WAVES * kGradGroups<WAVES>) norm_grads_kernel(NormGradParams P) {
+  constexpr int E = kLaneElems<T>, GROUPS = kGradGroups<WAVES>;
   const uint32_t lane = threadIdx.x % (64 * WAVES), group = wave_index() / WAVES, d = P.d;
   const float per = 1.f / d;
   const uint64_t step = (uint64_t)gridDim.x * GROUPS;
@@ -283,7 +289,7 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grads_kernel(NormGra
         }
       sum[2 * i] = s1, sum[2 * i + 1] = s2;
     }
-    group_sum<WAVES>(sum, slot);
+    group_sum<WAVES, 2 * R, 64 * WAVES * GROUPS>(sum, slot);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       if (t + i * step >= P.n) continue;
@@ -294,49 +300,51 @@ __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grads_kernel(NormGra
     }
   }
   // This workgroup's part, or with no other the gradients: its groups' sums, through LDS.
-  float *part = P.part + (uint64_t)blockIdx.x * 2 * P.pitch;
   if constexpr (GROUPS > 1) {
-    __shared__ f4 sh[GROUPS][2][64 * WAVES * NV * E / 4];
+    __shared__ f4 sh[GROUPS - 1][2][64 * WAVES * NV * E / 4];
+    if (group) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < E; j += 4) {
+          const uint32_t at = (k * E + j) / 4 * 64 * WAVES + lane;
+          sh[group - 1][0][at] = (f4){dw[k][j], dw[k][j + 1], dw[k][j + 2], dw[k][j + 3]};
+          sh[group - 1][1][at] = (f4){db[k][j], db[k][j + 1], db[k][j + 2], db[k][j + 3]};
+        }
+    }
+    __syncthreads();
+    if (group) return;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-      for (int j = 0; j < E; j += 4) {
-        const uint32_t at = ((k * 64 * WAVES + lane) * E + j) / 4;
-        sh[group][0][at] = (f4){dw[k][j], dw[k][j + 1], dw[k][j + 2], dw[k][j + 3]};
-        sh[group][1][at] = (f4){db[k][j], db[k][j + 1], db[k][j + 2], db[k][j + 3]};
-      }
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < d; i += kNormThreads<WAVES>) {
-      float a = 0, b = 0;
+      for (int j = 0; j < E; j += 4)
 #pragma unroll
-      for (int q = 0; q < GROUPS; ++q) a += ((const float *)sh[q][0])[i], b += ((const float *)sh[q][1])[i];
+        for (int q = 0; q < GROUPS - 1; ++q) {
+          const uint32_t at = (k * E + j) / 4 * 64 * WAVES + lane;
+          const f4 a = sh[q][0][at], b = sh[q][1][at];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) dw[k][j + i] += a[i], db[k][j + i] += b[i];
+        }
+  }
+  float *part = P.part + (uint64_t)blockIdx.x * 2 * P.pitch;
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int j = 0; j < E; j += 4) {
+      const uint32_t at = (k * 64 * WAVES + lane) * E + j;
+      if (at >= d) continue;      // (the pitch is in whole steps of 4)
       if (P.parts > 1) {
-        part[i] = a, part[P.pitch + i] = b;
-      } else {
-        if (P.dweight) ((W *)P.dweight)[i] = (W)a;
-        if (P.dbias) ((W *)P.dbias)[i] = (W)b;
+        *(f4 *)(part + at) = (f4){dw[k][j], dw[k][j + 1], dw[k][j + 2], dw[k][j + 3]};
+        *(f4 *)(part + P.pitch + at) = (f4){db[k][j], db[k][j + 1], db[k][j + 2], db[k][j + 3]};
+        continue;
+      }
+#pragma unroll
+      for (int i = j; i < j + 4; ++i) {
+        if (at + i - j >= d) continue;
+        if (P.dweight) ((W *)P.dweight)[at + i - j] = (W)dw[k][i];
+        if (P.dbias) ((W *)P.dbias)[at + i - j] = (W)db[k][i];
       }
     }
-  } else {
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-      for (int j = 0; j < E; j += 4) {
-        const uint32_t at = (k * 64 * WAVES + lane) * E + j;
-        if (at >= d) continue;      // (the pitch is in whole steps of 4)
-        if (P.parts > 1) {
-          *(f4 *)(part + at) = (f4){dw[k][j], dw[k][j + 1], dw[k][j + 2], dw[k][j + 3]};
-          *(f4 *)(part + P.pitch + at) = (f4){db[k][j], db[k][j + 1], db[k][j + 2], db[k][j + 3]};
-          continue;
-        }
-#pragma unroll
-        for (int i = j; i < j + 4; ++i) {
-          if (at + i - j >= d) continue;
-          if (P.dweight) ((W *)P.dweight)[at + i - j] = (W)dw[k][i];
-          if (P.dbias) ((W *)P.dbias)[at + i - j] = (W)db[k][i];
-        }
-      }
-  }
 }
 
 // The parts of dweight and dbias added up, 64 columns to a workgroup, its

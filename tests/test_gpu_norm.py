@@ -99,6 +99,15 @@ def test_backward(n, d, dtype, wt):
     _check_backward(c, _backward(c, dev, sums=False))
 
 
+@pytest.mark.parametrize("dtype,n,d", [(F16, 2, 1373), (F16, 3, 1373), (F16, 1025, 1373), (BF16, 4099, 1100), (F16, 513, 4096), (BF16, 300, 8190),
+                                       (F32, 4, 2500), (F32, 770, 1030), (F32, 300, 4099), (F32, 18, 999), (F32, 2051, 771), (BF16, 4101, 509)])
+def test_backward_of_more_rows_than_groups(dtype, n, d):
+    """Rows that fill one workgroup's groups, leave one of them a row short, or come again after every group's first."""
+    dev = _dev()
+    c = _inputs(n, d, dtype, F32, seed=n + d)
+    _check_backward(c, _backward(c, dev))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_a_mean_far_from_zero(dtype):
     """Deviations of one part in 300: the square's mean less the mean's square would lose them in 32 bits."""
