@@ -46,9 +46,20 @@ uint32_t splits_of(uint32_t n, uint32_t pieces) {
   return std::max(1u, std::min({(kWorkgroups + n - 1) / n, (pieces + 255) / 256, fiona::kLossSplits}));
 }
 
-uint32_t pieces_of(const fiona_token_loss_desc &D) {
+// Elements of a line of memory less one where some row of logits starts off the 16 bytes,
+// rows are long and there are many, so that it counts (us, gradients and their parts or
+// whole rows, from the rows' first elements / from their lines: 6300 rows of 30011 in bfloat16 380 /
+// 322, of 9001 in binary16 111 / 101, of 4001 43.0 / 42.0 (in 32 bits 86 / 80), of 2003 31.8 / 35.7; 3000 whole rows of
+// 50016 in binary16 124 / 129, 8000 of 4001 in bfloat16 32.5 / 35.2, 1500 of 125001 178 / 155,
+// 2000 of 50021 in 32 bits 159 / 148, 24 of them 8.5 / 9.2, 300 of 50001 in bfloat16 19.7 / 19.6).
+constexpr uint64_t kLine = 128, kSkewedRow = 12288, kSkewedRows = 32 << 20;
+uint32_t skew_of(const fiona_token_loss_desc &D, const void *logits, uint64_t logits_row, uint32_t n) {
+  const uint64_t e = type_size(D.type), off = (uint64_t)logits | (n > 1 ? logits_row * e : 0), row = D.vocab * e;
+  return off % 16 && row >= kSkewedRow && n * row >= kSkewedRows ? kLine / e - 1 : 0;
+}
+uint32_t pieces_of(const fiona_token_loss_desc &D, uint32_t skew) {
   const uint32_t e = 16 / type_size(D.type);
-  return (D.vocab + e - 1) / e;
+  return (D.vocab + skew + e - 1) / e;
 }
 
 fiona::TokenParams params(const fiona_token_loss *H, uint32_t n, const void *logits, void *dlogits, const int32_t *targets,
@@ -58,31 +69,34 @@ fiona::TokenParams params(const fiona_token_loss *H, uint32_t n, const void *log
   P.n_tok = n, P.vocab = H->desc.vocab;
   P.part = (float2 *)H->ws, P.at_target = (float *)(P.part + H->part_cap);
   P.lse = P.at_target + H->desc.max_tokens, P.coef = P.lse + H->desc.max_tokens;
-  const uint32_t pieces = pieces_of(H->desc);
+  P.skew = skew_of(H->desc, logits, logits_row, n);
+  const uint32_t pieces = pieces_of(H->desc, P.skew);
   P.slice = (pieces + splits_of(n, pieces) - 1) / splits_of(n, pieces);
   P.splits = (pieces + P.slice - 1) / P.slice;
   return P;
 }
 
-// Calls f with whether rows are shorter than a piece.
+// Calls f with whether rows are shorter than a piece, and whether they are skewed.
 template <typename T, typename F>
-void with_width(uint32_t vocab, F f) {
-  if (vocab < fiona::kLaneElems<T>) f(std::true_type{});
-  else f(std::false_type{});
+void with_rows(const fiona::TokenParams &P, F f) {
+  if (P.vocab < fiona::kLaneElems<T>) f(std::true_type{}, std::false_type{});
+  else if (P.skew) f(std::false_type{}, std::true_type{});
+  else f(std::false_type{}, std::false_type{});
 }
 
 template <typename T>
 void launch_stats(const fiona::TokenParams &P, hipStream_t stream) {
-  with_width<T>(P.vocab, [&](auto narrow) {
-    hipLaunchKernelGGL((fiona::token_stats_kernel<T, decltype(narrow)::value>), dim3(P.n_tok, P.splits), dim3(256), 0, stream, P);
+  with_rows<T>(P, [&](auto narrow, auto skewed) {
+    hipLaunchKernelGGL((fiona::token_stats_kernel<T, decltype(narrow)::value, decltype(skewed)::value>), dim3(P.n_tok, P.splits), dim3(256),
+                       0, stream, P);
   });
 }
 
 template <typename T, bool POLICY>
 void launch_grad(const fiona::TokenParams &P, const fiona::PolicyParams &Q, hipStream_t stream) {
-  with_width<T>(P.vocab, [&](auto narrow) {
-    hipLaunchKernelGGL((fiona::token_grad_kernel<T, decltype(narrow)::value, POLICY>), dim3(P.n_tok, P.dz ? P.splits : 1), dim3(256), 0,
-                       stream, P, Q, P.slice);
+  with_rows<T>(P, [&](auto narrow, auto skewed) {
+    hipLaunchKernelGGL((fiona::token_grad_kernel<T, decltype(narrow)::value, decltype(skewed)::value, POLICY>),
+                       dim3(P.n_tok, P.dz ? P.splits : 1), dim3(256), 0, stream, P, Q, P.slice);
   });
 }
 
@@ -93,17 +107,23 @@ void launch_grad(const fiona::TokenParams &P, const fiona::PolicyParams &Q, hipS
 // 11.8 / 11.1, 64 x 131072 12.8 / 18.2, 100 x 131072 22.8 / 19.4, 200 x 131072 30.2 /
 // 24.7, 3000 x 131072 411 / 290.  (Rows of 24 pieces a lane spill: 1500 x 78213 in 32 bits 233 /
 // 233, 1500 x 190000 in bfloat16 284 / 302.)
-bool whole_rows(uint32_t n, uint32_t pieces) { return pieces <= 4096 || (pieces <= 1024 * 16 && n >= pieces / 192); }
+constexpr uint32_t kRowPieces = 1024 * 16;
+bool whole_rows(uint32_t n, uint32_t pieces) { return pieces <= 4096 || (pieces <= kRowPieces && n >= pieces / 192); }
 
 // The policy loss with whole rows in registers.
+template <typename T, bool SKEWED>
+void launch_shape(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint32_t pieces, hipStream_t stream) {
+  const dim3 grid(P.n_tok);
+  if (pieces <= 256 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 256, 4, SKEWED>), grid, dim3(256), 0, stream, P, Q);
+  else if (pieces <= 512 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 512, 4, SKEWED>), grid, dim3(512), 0, stream, P, Q);
+  else if (pieces <= 1024 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 4, SKEWED>), grid, dim3(1024), 0, stream, P, Q);
+  else if (pieces <= 1024 * 8) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 8, SKEWED>), grid, dim3(1024), 0, stream, P, Q);
+  else hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 16, SKEWED>), grid, dim3(1024), 0, stream, P, Q);
+}
 template <typename T>
 void launch_rows(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint32_t pieces, hipStream_t stream) {
-  const dim3 grid(P.n_tok);
-  if (pieces <= 256 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 256, 4>), grid, dim3(256), 0, stream, P, Q);
-  else if (pieces <= 512 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 512, 4>), grid, dim3(512), 0, stream, P, Q);
-  else if (pieces <= 1024 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 4>), grid, dim3(1024), 0, stream, P, Q);
-  else if (pieces <= 1024 * 8) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 8>), grid, dim3(1024), 0, stream, P, Q);
-  else hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 16>), grid, dim3(1024), 0, stream, P, Q);
+  if (P.skew) launch_shape<T, true>(P, Q, pieces, stream);
+  else launch_shape<T, false>(P, Q, pieces, stream);
 }
 
 }  // namespace
@@ -194,12 +214,15 @@ int fiona_policy_loss(const fiona_token_loss *H, const fiona_policy_args *args, 
   const uint32_t own[] = {1, 0, 0};
   if ((rc = check_alias(in, 6, out, 3, own)) != FIONA_OK) return rc;
   if (!on_device(H->device)) return FIONA_ERR_ARG;
-  const fiona::TokenParams P = params(H, A.n_tok, A.logits, A.dlogits, A.targets, A.logits_row, A.dlogits_row);
+  fiona::TokenParams P = params(H, A.n_tok, A.logits, A.dlogits, A.targets, A.logits_row, A.dlogits_row);
   const fiona::PolicyParams Q{A.old, A.advantages, A.kl > 0 ? A.reference : nullptr, A.weights, A.loss, A.logps,
                               A.clip_low, A.clip_high, A.kl};
   with_type(H->desc.type, [&](auto t) {
     using T = decltype(t);
-    const uint32_t pieces = pieces_of(H->desc);
+    uint32_t pieces = pieces_of(H->desc, P.skew);
+    if (pieces > kRowPieces && pieces_of(H->desc, 0) <= kRowPieces) {     // (rows that just fit: by less than lines)
+      while (pieces > kRowPieces) P.skew /= 2, pieces = pieces_of(H->desc, P.skew);
+    }
     if (A.dlogits && whole_rows(A.n_tok, pieces) && P.vocab >= fiona::kLaneElems<T>) {
       launch_rows<T>(P, Q, pieces, stream);
       return;

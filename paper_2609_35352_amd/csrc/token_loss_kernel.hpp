@@ -40,6 +40,7 @@ struct TokenParams {
   uint64_t z_row, dz_row;
   uint32_t n_tok, vocab;
   uint32_t splits, slice;         // parts of a row, and their pieces
+  uint32_t skew;                  // elements of a line less one (see before)
 };
 
 struct PairParams {
@@ -73,11 +74,21 @@ __device__ __forceinline__ float policy_of(const PolicyParams &Q, uint32_t n_tok
 
 __device__ __forceinline__ bool counts(int32_t target, uint32_t vocab) { return target >= 0 && (uint32_t)target < vocab; }
 
-// A lane's piece of a row of n elements.  NARROW: rows shorter than a piece.
+// Rows of SKEWED kernels start anywhere, their pieces at lines of memory: a row is worked on
+// as one that begins at the line of its first element, with up to skew elements before it that
+// are no part of it.  (A wavefront's 1024 bytes across the ends of lines leave two of them
+// half written, and at an odd element of 16 bits take longer to read.)
+template <typename T, bool SKEWED>
+__device__ __forceinline__ uint32_t before(const void *row, uint32_t skew) {
+  return SKEWED ? (uint32_t)((uint64_t)row / sizeof(T)) & skew : 0;
+}
+
+// A lane's piece of a row whose elements are those from `from` up to n.  NARROW: rows
+// shorter than a piece, from 0.
 template <typename T, bool NARROW>
-__device__ __forceinline__ u4 read_piece(const T *row, uint32_t at, uint32_t n) {
+__device__ __forceinline__ u4 read_piece(const T *row, uint32_t at, uint32_t from, uint32_t n) {
   if constexpr (!NARROW) {
-    return load_shared(piece_at(row, at, n));
+    return load_shared(row + max(at + kLaneElems<T> <= n ? at : n - kLaneElems<T>, from));
   } else {
     uint32_t w[4];
     load_row<T, kLaneElems<T>, false>(row, at ? 0 : (int)n, w);
@@ -85,17 +96,18 @@ __device__ __forceinline__ u4 read_piece(const T *row, uint32_t at, uint32_t n) 
   }
 }
 
-// The elements of such a piece, -inf from the row's end on.  whole: it is known to end before.
+// The elements of such a piece, -inf outside the row.  whole: it is known to lie inside.
 template <typename T, bool NARROW>
-__device__ __forceinline__ void logits_of(u4 v, uint32_t at, uint32_t n, float (&x)[kLaneElems<T>], bool whole = false) {
-  if (whole || at + kLaneElems<T> <= n) {
+__device__ __forceinline__ void logits_of(u4 v, uint32_t at, uint32_t from, uint32_t n, float (&x)[kLaneElems<T>], bool whole = false) {
+  if (whole || (at >= from && at + kLaneElems<T> <= n)) {
     unpack<T>(v, x);
     return;
   }
+  if (at < from) v = __builtin_bit_cast(u4, __builtin_bit_cast(unsigned __int128, v) << (min(from - at, kLaneElems<T> - 1) * 8 * sizeof(T)));
   unpack<T>(NARROW ? v : piece_fix<T>(v, at, n), x);
 #pragma unroll
   for (int j = 0; j < (int)kLaneElems<T>; ++j)
-    if (at + j >= n) x[j] = -INFINITY;
+    if (at + j < from || at + j >= n) x[j] = -INFINITY;
 }
 
 // Adds elements to a running maximum and sum of exponentials.
@@ -113,15 +125,15 @@ __device__ __forceinline__ void gather(const float (&x)[N], float &m, float &s) 
 }
 
 // U pieces of a row, 256 of them apart, for a lane whose first one starts at `at`.
-// Steps that end before the row does (`whole`, the same in the workgroup) need no checks.
+// Steps that lie inside the row (`whole`, the same in the wavefront) need no checks.
 template <typename T, bool NARROW, int U>
-__device__ __forceinline__ void read_step(const T *row, uint32_t at, uint32_t n, bool whole, u4 (&v)[U]) {
+__device__ __forceinline__ void read_step(const T *row, uint32_t at, uint32_t from, uint32_t n, bool whole, u4 (&v)[U]) {
   if (whole) {
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = load_shared(row + at + u * 256 * kLaneElems<T>);
   } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = read_piece<T, NARROW>(row, at + u * 256 * kLaneElems<T>, n);
+    for (int u = 0; u < U; ++u) v[u] = read_piece<T, NARROW>(row, at + u * 256 * kLaneElems<T>, from, n);
   }
 }
 
@@ -134,7 +146,7 @@ __device__ __forceinline__ void join_wave(float &m, float &s) {
 __device__ __forceinline__ float log_sum(float m, float s) { return (m == -INFINITY ? 0.f : m) + kLossLn2 * __builtin_amdgcn_logf(s); }
 
 // A workgroup to a part of a token's row.
-template <typename T, bool NARROW>
+template <typename T, bool NARROW, bool SKEWED>
 __global__ void __launch_bounds__(256) token_stats_kernel(TokenParams P) {
   constexpr int E = kLaneElems<T>, U = 2;
   const uint32_t t = blockIdx.x, split = blockIdx.y;
@@ -142,25 +154,28 @@ __global__ void __launch_bounds__(256) token_stats_kernel(TokenParams P) {
   if (split == 0 && threadIdx.x == 0) P.coef[t] = 0;          // (of a token in no sequence)
   if (!counts(y, P.vocab)) return;
   const T *z = (const T *)P.z + t * P.z_row;
+  const uint32_t from = before<T, SKEWED>(z, P.skew), n = P.vocab + from, w = wave_index();
+  z -= from;
   constexpr uint32_t STEP = U * 256 * E;
-  const uint32_t start = split * P.slice * E, end = min(start + P.slice * E, P.vocab);
+  const uint32_t start = split * P.slice * E, end = min(start + P.slice * E, n);
+  auto inside = [&](uint32_t base) { return base + STEP <= end && (!from || base || w); };
   u4 v[U];
-  read_step<T, NARROW>(z, start + threadIdx.x * E, P.vocab, start + STEP <= end, v);
+  read_step<T, NARROW>(z, start + threadIdx.x * E, from, n, inside(start), v);
   float zt = 0;
-  if (split == 0 && threadIdx.x == 0) zt = (float)z[y];
+  if (split == 0 && threadIdx.x == 0) zt = (float)z[from + y];
   float m = -INFINITY, s = 0;
   for (uint32_t base = start; base < end; base += STEP) {
     const uint32_t at = base + threadIdx.x * E;
-    const bool whole = base + STEP <= end;
+    const bool whole = inside(base);
     float x[U * E];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float e[E];
-      logits_of<T, NARROW>(v[u], at + u * 256 * E, end, e, whole);
+      logits_of<T, NARROW>(v[u], at + u * 256 * E, from, end, e, whole);
 #pragma unroll
       for (int j = 0; j < E; ++j) x[u * E + j] = e[j];
     }
-    if (base + STEP < end) read_step<T, NARROW>(z, at + STEP, P.vocab, base + 2 * STEP <= end, v);
+    if (base + STEP < end) read_step<T, NARROW>(z, at + STEP, from, n, inside(base + STEP), v);
     gather(x, m, s);
   }
   join_wave(m, s);
@@ -232,33 +247,48 @@ __global__ void __launch_bounds__(1024) pair_kernel(TokenParams P, PairParams Q,
 
 // c (onehot(y) - softmax(z)) of a lane's piece.
 template <typename T, bool NARROW>
-__device__ __forceinline__ u4 gradient_of(u4 v, uint32_t at, uint32_t n, int32_t y, float c, float lse, bool whole = false) {
+__device__ __forceinline__ u4 gradient_of(u4 v, uint32_t at, uint32_t from, uint32_t n, uint32_t y, float c, float lse, bool whole = false) {
   constexpr int E = kLaneElems<T>;
   float x[E];
-  logits_of<T, NARROW>(v, at, n, x, whole);
+  logits_of<T, NARROW>(v, at, from, n, x, whole);
 #pragma unroll
   for (int j = 0; j < E; ++j) x[j] = -c * __builtin_amdgcn_exp2f((x[j] - lse) * kLossLog2e);
-  if ((uint32_t)y - at < (uint32_t)E) {
+  if (y - at < (uint32_t)E) {
 #pragma unroll
     for (int j = 0; j < E; ++j)
-      if (at + j == (uint32_t)y) x[j] += c;
+      if (at + j == y) x[j] += c;
   }
   return pack<T>(x);
 }
 
+// A lane's piece of a row of the gradient stored.
+template <typename T>
+__device__ __forceinline__ void store_inside(T *row, uint32_t at, uint32_t from, uint32_t n, u4 v) {
+  if (at >= from) return store_piece(row, at, n, v);
+#pragma unroll
+  for (int j = 0; j < (int)kLaneElems<T>; ++j)
+    if (at + j >= from && at + j < n) {
+      if constexpr (sizeof(T) == 4) ((uint32_t *)row)[at + j] = v[j];
+      else ((uint16_t *)row)[at + j] = (uint16_t)(v[j / 2] >> (j % 2 * 16));
+    }
+}
+
 // A workgroup to a part of a token's row of the gradient.  POLICY: the token's loss as
 // well, from the parts of its row.
-template <typename T, bool NARROW, bool POLICY>
+template <typename T, bool NARROW, bool SKEWED, bool POLICY>
 __global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyParams Q, uint32_t slice) {
   constexpr int E = kLaneElems<T>, U = 2;
   // From the last token on: its logits were read last.
-  const uint32_t t = P.n_tok - 1 - blockIdx.x, split = blockIdx.y, end = min((split + 1) * slice * E, P.vocab);
+  const uint32_t t = P.n_tok - 1 - blockIdx.x, split = blockIdx.y;
   const int32_t y = P.targets[t];
   const T *z = (const T *)P.z + t * P.z_row;
+  const uint32_t from = before<T, SKEWED>(z, P.skew), n = P.vocab + from, w = wave_index();
+  z -= from;
   constexpr uint32_t STEP = U * 256 * E;
-  const uint32_t start = split * slice * E;
+  const uint32_t start = split * slice * E, end = min(start + slice * E, n);
+  auto inside = [&](uint32_t base) { return base + STEP <= end && (!from || base || w); };
   u4 v[U];
-  auto load = [&](uint32_t base) { read_step<T, NARROW>(z, base + threadIdx.x * E, P.vocab, base + STEP <= end, v); };
+  auto load = [&](uint32_t base) { read_step<T, NARROW>(z, base + threadIdx.x * E, from, n, inside(base), v); };
   float c = 0, lse = 0;
   if constexpr (POLICY) {
     const bool live = counts(y, P.vocab);
@@ -279,9 +309,9 @@ __global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyPa
     c = P.coef[t], lse = P.lse[t];
     if (c != 0) load(start);
   }
-  T *dz = (T *)P.dz + t * P.dz_row;
+  T *dz = (T *)P.dz + t * P.dz_row - from;
   if (c == 0) {
-    for (uint32_t at = start + threadIdx.x * E; at < end; at += 256 * E) store_piece(dz, at, P.vocab, (u4){0, 0, 0, 0});
+    for (uint32_t at = start + threadIdx.x * E; at < end; at += 256 * E) store_inside(dz, at, from, n, (u4){0, 0, 0, 0});
     return;
   }
   for (uint32_t base = start; base < end; base += STEP) {
@@ -290,41 +320,47 @@ __global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyPa
     for (int u = 0; u < U; ++u) g[u] = v[u];
     if (base + STEP < end) load(base + STEP);
     const uint32_t at = base + threadIdx.x * E;
-    const bool whole = base + STEP <= end;
+    const bool whole = inside(base);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uint32_t i = at + u * 256 * E;
-      if (whole) __builtin_nontemporal_store(gradient_of<T, NARROW>(g[u], i, P.vocab, y, c, lse, true), (u4_any *)(dz + i));
-      else if (i < end) store_piece(dz, i, P.vocab, gradient_of<T, NARROW>(g[u], i, P.vocab, y, c, lse));
+      if (whole) __builtin_nontemporal_store(gradient_of<T, NARROW>(g[u], i, from, n, from + y, c, lse, true), (u4_any *)(dz + i));
+      else if (i < end) store_inside(dz, i, from, n, gradient_of<T, NARROW>(g[u], i, from, n, from + y, c, lse));
     }
   }
 }
 
 // The policy loss with a workgroup's registers holding the whole row: read once.
-template <typename T, int THREADS, int NV>
+template <typename T, int THREADS, int NV, bool SKEWED>
 __global__ void __launch_bounds__(THREADS) policy_row_kernel(TokenParams P, PolicyParams Q) {
   constexpr int E = kLaneElems<T>, WAVES = THREADS / 64;
   const uint32_t t = blockIdx.x;
   const int32_t y = P.targets[t];
-  T *dz = (T *)P.dz + t * P.dz_row;
+  const T *z = (const T *)P.z + t * P.z_row;
+  const uint32_t from = before<T, SKEWED>(z, P.skew), n = P.vocab + from, wave = wave_index();
+  z -= from;
+  T *dz = (T *)P.dz + t * P.dz_row - from;
   if (!counts(y, P.vocab)) {
     if (threadIdx.x == 0) Q.loss[t] = 0, Q.logps[t] = 0;
-    for (uint32_t at = threadIdx.x * E; at < P.vocab; at += THREADS * E) store_piece(dz, at, P.vocab, (u4){0, 0, 0, 0});
+    for (uint32_t at = threadIdx.x * E; at < n; at += THREADS * E) store_inside(dz, at, from, n, (u4){0, 0, 0, 0});
     return;
   }
-  const T *z = (const T *)P.z + t * P.z_row;
   u4 v[NV];
 #pragma unroll
-  for (int k = 0; k < NV; ++k) v[k] = load_once(piece_at(z, (k * THREADS + threadIdx.x) * E, P.vocab));
+  for (int k = 0; k < NV; ++k) {
+    const uint32_t at = (k * THREADS + threadIdx.x) * E;
+    v[k] = load_once(z + max(at + E <= n ? at : n - E, from));
+  }
+  auto inside = [&](int k) { return (k + 1) * THREADS * E <= n && (k || !from || wave); };
   // (by one thread, through LDS: where dlogits are the logits the element is overwritten after the barrier)
   __shared__ float at_target;
-  if (threadIdx.x == 0) at_target = (float)z[y];
+  if (threadIdx.x == 0) at_target = (float)z[from + y];
   float m = -INFINITY, s = 0;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    if (k * THREADS * E >= P.vocab) continue;
+    if (k * THREADS * E >= n) continue;
     float x[E];
-    logits_of<T, false>(v[k], (k * THREADS + threadIdx.x) * E, P.vocab, x, (k + 1) * THREADS * E <= P.vocab);
+    logits_of<T, false>(v[k], (k * THREADS + threadIdx.x) * E, from, n, x, inside(k));
     gather(x, m, s);
     // (only the packed row stays: its elements kept as 32-bit values for the second pass spilled, 599 us for 200)
     asm volatile("" : "+v"(v[k]));
@@ -341,18 +377,18 @@ __global__ void __launch_bounds__(THREADS) policy_row_kernel(TokenParams P, Poli
   const float c = policy_of(Q, P.n_tok, t, l, loss);
   if (c == 0) {
     if (threadIdx.x == 0) Q.loss[t] = loss, Q.logps[t] = l;
-    for (uint32_t at = threadIdx.x * E; at < P.vocab; at += THREADS * E) store_piece(dz, at, P.vocab, (u4){0, 0, 0, 0});
+    for (uint32_t at = threadIdx.x * E; at < n; at += THREADS * E) store_inside(dz, at, from, n, (u4){0, 0, 0, 0});
     return;
   }
   if (threadIdx.x == 0) Q.loss[t] = loss, Q.logps[t] = l;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const uint32_t at = (k * THREADS + threadIdx.x) * E;
-    if (k * THREADS * E >= P.vocab) continue;
-    const bool whole = (k + 1) * THREADS * E <= P.vocab;
-    const u4 g = gradient_of<T, false>(v[k], at, P.vocab, y, c, lse, whole);
+    if (k * THREADS * E >= n) continue;
+    const bool whole = inside(k);
+    const u4 g = gradient_of<T, false>(v[k], at, from, n, from + y, c, lse, whole);
     if (whole) __builtin_nontemporal_store(g, (u4_any *)(dz + at));
-    else store_piece(dz, at, P.vocab, g);
+    else store_inside(dz, at, from, n, g);
   }
 }
 

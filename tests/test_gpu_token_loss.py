@@ -278,6 +278,38 @@ def test_in_place(V, dtype):
     assert torch.equal(t["logits"], want[2]) and torch.equal(loss, want[0])
 
 
+@pytest.mark.parametrize("n,V,dtype", [(346, 50021, BF16), (132, 131071, F16), (1870, 9001, F16), (121, 140001, BF16), (1040, 8193, F32),
+                                       (2040, 8229, BF16)])
+def test_long_rows_from_their_lines(n, V, dtype):
+    """Logits of over 32 MiB whose rows start at every place of a line of memory; their gradients at others, and in place."""
+    dev = _dev()
+    half = (n - 3) // 2
+    for c, name, check in ((_pairs([half, n - 3 - half], V, dtype, seed=V), "preference_loss", _check_prefer),
+                           (_tokens(n, V, dtype, seed=V), "policy_loss", _check_policy)):
+        t = {k: v.to(dev) for k, v in c.items()}
+        h = fiona.TokenLoss(dtype, V, n, 1)
+
+        def run(z, dz):
+            if name == "preference_loss":
+                loss, logps = torch.empty(1, device=dev), torch.empty(2, device=dev)
+                fiona.preference_loss(h, z, t["targets"], t["offsets"], t["reference"], loss, logps, dz, weights=t["weights"])
+            else:
+                loss, logps = torch.empty(n, device=dev), torch.empty(n, device=dev)
+                fiona.policy_loss(h, z, t["targets"], t["old"], t["advantages"], loss, logps, dz, reference=t["reference"], kl=0.05,
+                                  weights=t["weights"])
+            return loss, logps, dz
+
+        gap = 4 if V % 2 else 3                          # (odd strides)
+        z_store, z = _spaced(c["logits"], dev, gap, 1)
+        store, dz = _spaced(c["logits"], dev, gap + 2, 3)
+        got = run(z, dz)
+        check(c, got)
+        again = run(z, z)
+        assert all(torch.equal(a, b) for a, b in zip(got, again))
+        dz.fill_(7.0), z.fill_(7.0)
+        assert bool((store == 7).all()) and bool((z_store == 7).all())
+
+
 def test_gradients_against_differences():
     """The sum of the losses, in 64 bits, at both ends of a small step of the logits."""
     dev = _dev()
