@@ -101,24 +101,35 @@ void launch_grad(const fiona::TokenParams &P, const fiona::PolicyParams &Q, hipS
 }
 
 // Whether each row's policy loss is one workgroup's: rows of up to 64 KiB, or enough
-// of the longer ones (one workgroup reads and writes 256 KiB in 17 us).  us of two
-// launches, parts and gradient, without the gap between them / of whole rows, in
-// bfloat16: 2 x 16000 7.2 / 4.9, 64 x 32768 8.9 / 7.6, 16 x 64000 7.6 / 10.4, 64 x 64000
-// 11.8 / 11.1, 64 x 131072 12.8 / 18.2, 100 x 131072 22.8 / 19.4, 200 x 131072 30.2 /
-// 24.7, 3000 x 131072 411 / 290.  (Rows of 24 pieces a lane spill: 1500 x 78213 in 32 bits 233 /
-// 233, 1500 x 190000 in bfloat16 284 / 302.)
-constexpr uint32_t kRowPieces = 1024 * 16;
+// of the longer ones (one workgroup reads and writes 256 KiB in 17 us), up to what the registers and
+// LDS of a compute unit hold.  us of two launches, parts and gradient, without the gap
+// between them / of whole rows, in bfloat16: 2 x 16000 7.2 / 4.9, 64 x 32768 8.9 / 7.6, 16 x
+// 64000 7.6 / 10.4, 64 x 64000 11.8 / 11.1, 64 x 131072 12.8 / 18.2, 100 x 131072 22.8 / 19.4,
+// 3000 x 131072 411 / 290, 100 x 151936 21.6 / 21.1, 2000 x 151936 352 / 237, and 1500 x 100000
+// in 32 bits 348 / 220.
+constexpr uint32_t kRowPieces = 1024 * 25;
 bool whole_rows(uint32_t n, uint32_t pieces) { return pieces <= 4096 || (pieces <= kRowPieces && n >= pieces / 192); }
 
-// The policy loss with whole rows in registers.
+// The policy loss with whole rows.  Where there are rows for every compute unit, of up to 512
+// threads, so that two or more workgroups share a unit and one reads while another writes,
+// and as many as a row needs (us of 1024 threads and half the pieces / of 512: 8000 rows of
+// 32000 in bfloat16 182 / 171, 3000 of 50000 123 / 115, 300 of them 21.3 / 19.0, 256 13.5 / 14.2, 4000
+// of 10001 in 32 bits 62.7 / 56.2, 2000 of 32000 90 / 92; of whole shapes / of threads as needed:
+// 8000 rows of 2000 in bfloat16 22.9 / 15.6, 3000 of 20000 56 / 48).
+template <typename T, int NV, int NL, bool SKEWED>
+void launch_row(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint32_t threads, hipStream_t stream) {
+  hipLaunchKernelGGL((fiona::policy_row_kernel<T, NV, NL, SKEWED>), dim3(P.n_tok), dim3(threads), 0, stream, P, Q, threads);
+}
 template <typename T, bool SKEWED>
 void launch_shape(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint32_t pieces, hipStream_t stream) {
-  const dim3 grid(P.n_tok);
-  if (pieces <= 256 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 256, 4, SKEWED>), grid, dim3(256), 0, stream, P, Q);
-  else if (pieces <= 512 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 512, 4, SKEWED>), grid, dim3(512), 0, stream, P, Q);
-  else if (pieces <= 1024 * 4) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 4, SKEWED>), grid, dim3(1024), 0, stream, P, Q);
-  else if (pieces <= 1024 * 8) hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 8, SKEWED>), grid, dim3(1024), 0, stream, P, Q);
-  else hipLaunchKernelGGL((fiona::policy_row_kernel<T, 1024, 16, SKEWED>), grid, dim3(1024), 0, stream, P, Q);
+  const bool many = P.n_tok > 256;
+  const uint32_t most = many ? 512 : 1024;
+  auto threads = [&](uint32_t nv) { return std::min(1024u, (pieces + 64 * nv - 1) / (64 * nv) * 64); };
+  if (pieces <= 4 * most) launch_row<T, 4, 0, SKEWED>(P, Q, threads(many ? 4 : 2), stream);
+  else if (pieces <= 8 * most) launch_row<T, 8, 0, SKEWED>(P, Q, many ? threads(8) : 1024, stream);
+  else if (pieces <= 16 * most) launch_row<T, 16, 0, SKEWED>(P, Q, threads(16), stream);
+  else if (pieces <= 16 * 1024) launch_row<T, 16, 0, SKEWED>(P, Q, 1024, stream);
+  else launch_row<T, 16, 9, SKEWED>(P, Q, 1024, stream);
 }
 template <typename T>
 void launch_rows(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint32_t pieces, hipStream_t stream) {

@@ -14,7 +14,8 @@
 //
 // What bounds them: memory, and the vector units close behind (an exponential takes four
 // issue slots; parts of bfloat16 rows keep them 55% busy).  Measured: 2700 rows of 131072
-// in bfloat16 read and written once (1.49 GB with 300 rows of zeros) 278 us, 5.4 TB/s; 7955
+// in bfloat16 read and written once (1.49 GB with 300 rows of zeros) 278 us, 5.4 TB/s, 8000 of
+// 32000 (1.02 GB) 172, 6.0; 7955
 // rows of 32768 74 us for the parts (419 MB, 5.7 TB/s), 6 for the pairs, 151 for the
 // gradients (419 MB again and 521 MB written, 6.2 TB/s: the rows read last are the first
 // again, some of them still in the memory-side cache; read past the caches in both passes
@@ -330,10 +331,13 @@ __global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyPa
   }
 }
 
-// The policy loss with a workgroup's registers holding the whole row: read once.
-template <typename T, int THREADS, int NV, bool SKEWED>
-__global__ void __launch_bounds__(THREADS) policy_row_kernel(TokenParams P, PolicyParams Q) {
-  constexpr int E = kLaneElems<T>, WAVES = THREADS / 64;
+// The policy loss with a workgroup holding the whole row: read once.  NV pieces to a lane
+// stay in registers, NL more of the longest rows in LDS (24 in registers spill: 302 us for
+// 1500 rows of 190000 in bfloat16, 284 in two launches).
+template <typename T, int NV, int NL, bool SKEWED>
+__global__ void __launch_bounds__(1024) policy_row_kernel(TokenParams P, PolicyParams Q, uint32_t threads) {
+  constexpr uint32_t E = kLaneElems<T>;
+  if (NL) threads = 1024;
   const uint32_t t = blockIdx.x;
   const int32_t y = P.targets[t];
   const T *z = (const T *)P.z + t * P.z_row;
@@ -342,53 +346,83 @@ __global__ void __launch_bounds__(THREADS) policy_row_kernel(TokenParams P, Poli
   T *dz = (T *)P.dz + t * P.dz_row - from;
   if (!counts(y, P.vocab)) {
     if (threadIdx.x == 0) Q.loss[t] = 0, Q.logps[t] = 0;
-    for (uint32_t at = threadIdx.x * E; at < n; at += THREADS * E) store_inside(dz, at, from, n, (u4){0, 0, 0, 0});
+    for (uint32_t at = threadIdx.x * E; at < n; at += threads * E) store_inside(dz, at, from, n, (u4){0, 0, 0, 0});
     return;
   }
-  u4 v[NV];
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const uint32_t at = (k * THREADS + threadIdx.x) * E;
-    v[k] = load_once(z + max(at + E <= n ? at : n - E, from));
-  }
-  auto inside = [&](int k) { return (k + 1) * THREADS * E <= n && (k || !from || wave); };
+  auto load = [&](uint32_t k) {
+    const uint32_t at = (k * threads + threadIdx.x) * E;
+    return load_once(z + max(at + E <= n ? at : n - E, from));
+  };
+  auto inside = [&](uint32_t k) { return (k + 1) * threads * E <= n && (k || !from || wave); };
   // (by one thread, through LDS: where dlogits are the logits the element is overwritten after the barrier)
   __shared__ float at_target;
   if (threadIdx.x == 0) at_target = (float)z[from + y];
   float m = -INFINITY, s = 0;
+  __shared__ u4 far[NL ? NL * 1024 : 1];
+  constexpr int U = 3;
+  if constexpr (NL > 0) {
+    static_assert(NL % U == 0);
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    if (k * THREADS * E >= n) continue;
+    for (int k = 0; k < NL; k += U) {
+      if ((NV + k) * threads * E >= n) continue;
+      u4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = load(NV + k + u);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        far[(k + u) * threads + threadIdx.x] = v[u];
+        float x[E];
+        logits_of<T, false>(v[u], ((NV + k + u) * threads + threadIdx.x) * E, from, n, x, inside(NV + k + u));
+        gather(x, m, s);
+      }
+    }
+  }
+  u4 v[NV];
+#pragma unroll
+  for (uint32_t k = 0; k < NV; ++k) v[k] = load(k);
+#pragma unroll
+  for (uint32_t k = 0; k < NV; ++k) {
+    if (k * threads * E >= n) continue;
     float x[E];
-    logits_of<T, false>(v[k], (k * THREADS + threadIdx.x) * E, from, n, x, inside(k));
+    logits_of<T, false>(v[k], (k * threads + threadIdx.x) * E, from, n, x, inside(k));
     gather(x, m, s);
     // (only the packed row stays: its elements kept as 32-bit values for the second pass spilled, 599 us for 200)
     asm volatile("" : "+v"(v[k]));
   }
-  __shared__ float2 part[WAVES];
+  __shared__ float2 part[16];
   join_wave(m, s);
   if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = {m, s};
   __syncthreads();
   const uint32_t lane = threadIdx.x % 64;
-  m = lane < WAVES ? part[lane].x : -INFINITY, s = lane < WAVES ? part[lane].y : 0.f;
+  m = lane < threads / 64 ? part[lane].x : -INFINITY, s = lane < threads / 64 ? part[lane].y : 0.f;
   join_wave(m, s);
   const float lse = log_sum(m, s), l = at_target - lse;
   float loss;
   const float c = policy_of(Q, P.n_tok, t, l, loss);
   if (c == 0) {
     if (threadIdx.x == 0) Q.loss[t] = loss, Q.logps[t] = l;
-    for (uint32_t at = threadIdx.x * E; at < n; at += THREADS * E) store_inside(dz, at, from, n, (u4){0, 0, 0, 0});
+    for (uint32_t at = threadIdx.x * E; at < n; at += threads * E) store_inside(dz, at, from, n, (u4){0, 0, 0, 0});
     return;
   }
   if (threadIdx.x == 0) Q.loss[t] = loss, Q.logps[t] = l;
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const uint32_t at = (k * THREADS + threadIdx.x) * E;
-    if (k * THREADS * E >= n) continue;
+  auto store = [&](uint32_t k, u4 v) {
+    const uint32_t at = (k * threads + threadIdx.x) * E;
     const bool whole = inside(k);
-    const u4 g = gradient_of<T, false>(v[k], at, from, n, from + y, c, lse, whole);
+    const u4 g = gradient_of<T, false>(v, at, from, n, from + y, c, lse, whole);
     if (whole) __builtin_nontemporal_store(g, (u4_any *)(dz + at));
     else store_inside(dz, at, from, n, g);
+  };
+#pragma unroll
+  for (uint32_t k = 0; k < NV; ++k) {
+    if (k * threads * E >= n) continue;
+    store(k, v[k]);
+  }
+  if constexpr (NL > 0) {
+#pragma unroll
+    for (int k = 0; k < NL; ++k) {
+      if ((NV + k) * threads * E >= n) continue;
+      store(NV + k, far[k * threads + threadIdx.x]);
+    }
   }
 }
 
