@@ -110,26 +110,31 @@ void launch_grad(const fiona::TokenParams &P, const fiona::PolicyParams &Q, hipS
 constexpr uint32_t kRowPieces = 1024 * 25;
 bool whole_rows(uint32_t n, uint32_t pieces) { return pieces <= 4096 || (pieces <= kRowPieces && n >= pieces / 192); }
 
-// The policy loss with whole rows.  Where there are rows for every compute unit, of up to 512
-// threads, so that two or more workgroups share a unit and one reads while another writes,
-// and as many as a row needs (us of 1024 threads and half the pieces / of 512: 8000 rows of
-// 32000 in bfloat16 182 / 171, 3000 of 50000 123 / 115, 300 of them 21.3 / 19.0, 256 13.5 / 14.2, 4000
-// of 10001 in 32 bits 62.7 / 56.2, 2000 of 32000 90 / 92; of whole shapes / of threads as needed:
-// 8000 rows of 2000 in bfloat16 22.9 / 15.6, 3000 of 20000 56 / 48).
-template <typename T, int NV, int NL, bool SKEWED>
+// The policy loss with whole rows.  Where there are more rows than compute units, shapes of
+// which two or more workgroups share a unit, so that one reads while another writes, and in
+// 16 bits even where that takes reading a quarter again (us of 1024 threads with the row in
+// registers / so: 8000 rows of 32000 in bfloat16, 512 threads, 182 / 171; in LDS as well 5000 of 50000
+// 205 / 177, 3000 of 70000 178 / 155, of 98000 238 / 229; reading again 2500 of 110000 in binary16 225 / 212,
+// 1500 of 125001 154 / 141, 3000 of 131072 285 / 284, but 1500 of 64000 in 32 bits 135 / 141).  256 rows
+// of 50000 take 13.5 / 14.2, and 300 21.3 / 19.6.  Threads as a row needs, not in whole shapes:
+// 8000 rows of 2000 22.9 / 15.6, 3000 of 20000 56 / 48.
+template <typename T, int NV, int NL, int NR, bool SKEWED>
 void launch_row(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint32_t threads, hipStream_t stream) {
-  hipLaunchKernelGGL((fiona::policy_row_kernel<T, NV, NL, SKEWED>), dim3(P.n_tok), dim3(threads), 0, stream, P, Q, threads);
+  hipLaunchKernelGGL((fiona::policy_row_kernel<T, NV, NL, NR, SKEWED>), dim3(P.n_tok), dim3(threads), 0, stream, P, Q, threads);
 }
 template <typename T, bool SKEWED>
 void launch_shape(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint32_t pieces, hipStream_t stream) {
   const bool many = P.n_tok > 256;
-  const uint32_t most = many ? 512 : 1024;
-  auto threads = [&](uint32_t nv) { return std::min(1024u, (pieces + 64 * nv - 1) / (64 * nv) * 64); };
-  if (pieces <= 4 * most) launch_row<T, 4, 0, SKEWED>(P, Q, threads(many ? 4 : 2), stream);
-  else if (pieces <= 8 * most) launch_row<T, 8, 0, SKEWED>(P, Q, many ? threads(8) : 1024, stream);
-  else if (pieces <= 16 * most) launch_row<T, 16, 0, SKEWED>(P, Q, threads(16), stream);
-  else if (pieces <= 16 * 1024) launch_row<T, 16, 0, SKEWED>(P, Q, 1024, stream);
-  else launch_row<T, 16, 9, SKEWED>(P, Q, 1024, stream);
+  auto threads = [&](uint32_t nv) { return (pieces + 64 * nv - 1) / (64 * nv) * 64; };
+  if (pieces <= 4 * 512) launch_row<T, 4, 0, 0, SKEWED>(P, Q, threads(many ? 4 : 2), stream);
+  else if (many && pieces <= 8 * 512) launch_row<T, 8, 0, 0, SKEWED>(P, Q, threads(8), stream);
+  else if (many && pieces <= 8 * 1024) launch_row<T, 4, 4, 0, SKEWED>(P, Q, 1024, stream);
+  else if (many && pieces <= 12 * 1024) launch_row<T, 8, 4, 0, SKEWED>(P, Q, 1024, stream);
+  else if (many && pieces <= 16 * 1024 && sizeof(T) == 2) launch_row<T, 8, 4, 4, SKEWED>(P, Q, 1024, stream);
+  else if (pieces <= 4 * 1024) launch_row<T, 4, 0, 0, SKEWED>(P, Q, 1024, stream);
+  else if (pieces <= 8 * 1024) launch_row<T, 8, 0, 0, SKEWED>(P, Q, 1024, stream);
+  else if (pieces <= 16 * 1024) launch_row<T, 16, 0, 0, SKEWED>(P, Q, 1024, stream);
+  else launch_row<T, 16, 9, 0, SKEWED>(P, Q, 1024, stream);
 }
 template <typename T>
 void launch_rows(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint32_t pieces, hipStream_t stream) {

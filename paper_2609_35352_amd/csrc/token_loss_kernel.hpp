@@ -332,10 +332,11 @@ __global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyPa
 }
 
 // The policy loss with a workgroup holding the whole row: read once.  NV pieces to a lane
-// stay in registers, NL more of the longest rows in LDS (24 in registers spill: 302 us for
-// 1500 rows of 190000 in bfloat16, 284 in two launches).
-template <typename T, int NV, int NL, bool SKEWED>
-__global__ void __launch_bounds__(1024) policy_row_kernel(TokenParams P, PolicyParams Q, uint32_t threads) {
+// stay in registers, NL more in LDS, and NR more of the longest rows are read again, from the
+// caches.  With NL, 1024 threads, and with 4 of them registers for two workgroups to a
+// compute unit.  (24 in registers spill: 302 us for 1500 rows of 190000 in bfloat16, 284 in two launches.)
+template <typename T, int NV, int NL, int NR, bool SKEWED>
+__global__ void __launch_bounds__(1024, NL == 4 ? 8 : 4) policy_row_kernel(TokenParams P, PolicyParams Q, uint32_t threads) {
   constexpr uint32_t E = kLaneElems<T>;
   if (NL) threads = 1024;
   const uint32_t t = blockIdx.x;
@@ -349,9 +350,9 @@ __global__ void __launch_bounds__(1024) policy_row_kernel(TokenParams P, PolicyP
     for (uint32_t at = threadIdx.x * E; at < n; at += threads * E) store_inside(dz, at, from, n, (u4){0, 0, 0, 0});
     return;
   }
-  auto load = [&](uint32_t k) {
+  auto place = [&](uint32_t k) {
     const uint32_t at = (k * threads + threadIdx.x) * E;
-    return load_once(z + max(at + E <= n ? at : n - E, from));
+    return z + max(at + E <= n ? at : n - E, from);
   };
   auto inside = [&](uint32_t k) { return (k + 1) * threads * E <= n && (k || !from || wave); };
   // (by one thread, through LDS: where dlogits are the logits the element is overwritten after the barrier)
@@ -359,18 +360,18 @@ __global__ void __launch_bounds__(1024) policy_row_kernel(TokenParams P, PolicyP
   if (threadIdx.x == 0) at_target = (float)z[from + y];
   float m = -INFINITY, s = 0;
   __shared__ u4 far[NL ? NL * 1024 : 1];
-  constexpr int U = 3;
+  constexpr int U = NL == 4 ? 4 : 3;
   if constexpr (NL > 0) {
-    static_assert(NL % U == 0);
+    static_assert(NL % U == 0 && NR % U == 0);
 #pragma unroll
-    for (int k = 0; k < NL; k += U) {
+    for (int k = 0; k < NL + NR; k += U) {
       if ((NV + k) * threads * E >= n) continue;
       u4 v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = load(NV + k + u);
+      for (int u = 0; u < U; ++u) v[u] = k < NL ? load_once(place(NV + k + u)) : load_shared(place(NV + k + u));
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        far[(k + u) * threads + threadIdx.x] = v[u];
+        if (k < NL) far[(k + u) * 1024 + threadIdx.x] = v[u];
         float x[E];
         logits_of<T, false>(v[u], ((NV + k + u) * threads + threadIdx.x) * E, from, n, x, inside(NV + k + u));
         gather(x, m, s);
@@ -379,7 +380,7 @@ __global__ void __launch_bounds__(1024) policy_row_kernel(TokenParams P, PolicyP
   }
   u4 v[NV];
 #pragma unroll
-  for (uint32_t k = 0; k < NV; ++k) v[k] = load(k);
+  for (uint32_t k = 0; k < NV; ++k) v[k] = load_once(place(k));
 #pragma unroll
   for (uint32_t k = 0; k < NV; ++k) {
     if (k * threads * E >= n) continue;
@@ -421,7 +422,19 @@ __global__ void __launch_bounds__(1024) policy_row_kernel(TokenParams P, PolicyP
 #pragma unroll
     for (int k = 0; k < NL; ++k) {
       if ((NV + k) * threads * E >= n) continue;
-      store(NV + k, far[k * threads + threadIdx.x]);
+      store(NV + k, far[k * 1024 + threadIdx.x]);
+    }
+#pragma unroll
+    for (int k = NL; k < NL + NR; k += U) {
+      if ((NV + k) * threads * E >= n) continue;
+      u4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = load_shared(place(NV + k + u));
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if ((NV + k + u) * threads * E >= n) continue;
+        store(NV + k + u, v[u]);
+      }
     }
   }
 }

@@ -136,7 +136,8 @@ def test_many_tokens():
 
 
 @pytest.mark.parametrize("n,V,dtype", [(300, 2000, F16), (300, 20000, F32), (270, 30000, BF16), (260, 50016, F16), (100, 70000, F32), (105, 152064, BF16),
-                                       (90, 131072, F16), (60, 65536, F32), (40, 50016, BF16)])
+                                       (90, 131072, F16), (60, 65536, F32), (40, 50016, BF16), (258, 70000, BF16), (257, 131072, F16), (259, 98301, BF16),
+                                       (258, 120001, BF16), (257, 33000, F32), (258, 64000, F32)])
 def test_policy_of_whole_rows(n, V, dtype):
     """Rows that a workgroup holds whole, in registers alone and partly in LDS, for more and fewer rows than compute units."""
     dev = _dev()
@@ -288,7 +289,7 @@ def test_in_place(V, dtype):
 
 
 @pytest.mark.parametrize("n,V,dtype", [(346, 50021, BF16), (132, 131071, F16), (1870, 9001, F16), (121, 140001, BF16), (1040, 8193, F32),
-                                       (2040, 8229, BF16), (135, 199999, F16)])
+                                       (2040, 8229, BF16), (135, 199999, F16), (262, 125001, BF16)])
 def test_long_rows_from_their_lines(n, V, dtype):
     """Logits of over 32 MiB whose rows start at every place of a line of memory; their gradients at others, and in place."""
     dev = _dev()
