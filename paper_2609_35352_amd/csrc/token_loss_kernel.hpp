@@ -14,7 +14,7 @@
 //
 // What bounds them: memory, and the vector units close behind (an exponential takes four
 // issue slots; parts of bfloat16 rows keep them 55% busy).  Measured: 2700 rows of 131072
-// in bfloat16 read and written once (1.49 GB with 300 rows of zeros) 278 us, 5.4 TB/s, 8000 of
+// in bfloat16 read and written once (1.49 GB with 300 rows of zeros) 281 us, 5.3 TB/s, 8000 of
 // 32000 (1.02 GB) 172, 6.0; 7955
 // rows of 32768 74 us for the parts (419 MB, 5.7 TB/s), 6 for the pairs, 151 for the
 // gradients (419 MB again and 521 MB written, 6.2 TB/s: the rows read last are the first
