@@ -130,11 +130,16 @@ void launch_shape(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uin
   else if (many && pieces <= 8 * 512) launch_row<T, 8, 0, 0, SKEWED>(P, Q, threads(8), stream);
   else if (many && pieces <= 8 * 1024) launch_row<T, 4, 4, 0, SKEWED>(P, Q, 1024, stream);
   else if (many && pieces <= 12 * 1024) launch_row<T, 8, 4, 0, SKEWED>(P, Q, 1024, stream);
-  else if (many && pieces <= 16 * 1024 && sizeof(T) == 2) launch_row<T, 8, 4, 4, SKEWED>(P, Q, 1024, stream);
   else if (pieces <= 4 * 1024) launch_row<T, 4, 0, 0, SKEWED>(P, Q, 1024, stream);
   else if (pieces <= 8 * 1024) launch_row<T, 8, 0, 0, SKEWED>(P, Q, 1024, stream);
-  else if (pieces <= 16 * 1024) launch_row<T, 16, 0, 0, SKEWED>(P, Q, 1024, stream);
-  else launch_row<T, 16, 9, 0, SKEWED>(P, Q, 1024, stream);
+  else if (pieces <= 16 * 1024) {
+    if constexpr (sizeof(T) == 2) {
+      if (many) return launch_row<T, 8, 4, 4, SKEWED>(P, Q, 1024, stream);
+    }
+    launch_row<T, 16, 0, 0, SKEWED>(P, Q, 1024, stream);
+  } else {
+    launch_row<T, 16, 9, 0, SKEWED>(P, Q, 1024, stream);
+  }
 }
 template <typename T>
 void launch_rows(const fiona::TokenParams &P, const fiona::PolicyParams &Q, uint32_t pieces, hipStream_t stream) {
