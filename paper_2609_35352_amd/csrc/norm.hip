@@ -76,8 +76,8 @@ void with_grad_shape(uint32_t q, F f) {
 constexpr uint32_t kMostParts = 512;
 uint32_t most_parts(uint32_t waves) { return waves == 1 ? kMostParts : 256; }
 // Where a lane holds one piece of a row, many rows go two at a time, for the bytes in
-// flight (one / two at a time, us, with one group to a workgroup: 16384 of 1376 in bfloat16
-// 48.3 / 40.7, 8192 of 2048 26.8 / 27.4, 1531 of 1373 9.9 / 10.7, 300 of 2048 6.1 / 6.8).
+// flight (one / two at a time, us without the parts' sum: 16384 of 1376 in bfloat16 47.6 / 39.9,
+// 8192 of 2048 25.8 / 26.0, 1531 of 1373 8.4 / 9.3, 1000 of 2048 7.7 / 8.1).
 constexpr uint32_t kTwoRows = 4096;
 // The wavefronts of a row's group there.
 uint32_t grad_waves(uint32_t type, uint32_t d) {
