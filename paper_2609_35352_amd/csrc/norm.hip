@@ -35,7 +35,9 @@ int check_types(uint32_t type, uint32_t weight_type, uint32_t width) {
   return width > FIONA_MAX_NORM_WIDTH ? FIONA_ERR_UNSUPPORTED : FIONA_OK;
 }
 
-// The wavefronts and pieces that hold rows of q pieces: f(waves, pieces a lane).
+// The wavefronts and pieces that hold rows of q pieces: f(waves, pieces a lane).  (Three
+// quarters of a shape where they hold the row, us: 16384 rows of 1280 in bfloat16 33.2 / 30.6, 8192
+// of 5120 64.3 / 58.2, 2048 of 20480 79 / 73.)
 template <int W, int NV>
 struct Shape {
   static constexpr int kWaves = W, kPieces = NV;
@@ -44,10 +46,13 @@ template <typename T, typename F>
 void with_shape(uint32_t q, F f) {
   if (q <= 64) f(Shape<1, 1>{});
   else if (q <= 128) f(Shape<1, 2>{});
+  else if (q <= 192) f(Shape<1, 3>{});
   else if (q <= 256) f(Shape<1, 4>{});
   else if (q <= 512) f(Shape<4, 2>{});
+  else if (q <= 768) f(Shape<4, 3>{});
   else if (q <= 1024) f(Shape<4, 4>{});
   else if (q <= 2048) f(Shape<16, 2>{});
+  else if (q <= 3 * 1024) f(Shape<16, 3>{});
   else if (q <= 4096) f(Shape<16, 4>{});
   else if constexpr (sizeof(T) == 4) f(Shape<16, 8>{});
 }
@@ -55,15 +60,20 @@ void with_shape(uint32_t q, F f) {
 // The same in the backward pass with the weights' gradients, where a lane holds at most
 // 16 elements: with their sums, weights and the next row that is a hundred registers
 // (32 elements, rows of 16384, spilled: 413 us for 2048 of them in bfloat16, 353 in 32
-// bits; a pass over columns takes 29 and 48 beside 55 and 92 for dx).
+// bits; a pass over columns takes 29 and 48 beside 55 and 92 for dx).  (Three quarters of
+// a shape, us without the parts' sum: 16384 rows of 1280 in bfloat16 38.4 / 33.5, of 2560 72 / 58, 8192 of 5120
+// 63.3 / 59.5, 2048 of 768 in 32 bits 9.3 / 8.5.)
 constexpr uint32_t kMostSums = 8192;
 template <typename T, typename F>
 void with_grad_shape(uint32_t q, F f) {
   constexpr bool wide = sizeof(T) == 4;
   if (q <= 64) f(Shape<1, 1>{});
   else if (q <= 128) f(Shape<1, 2>{});
+  else if (q <= 192) f(std::conditional_t<wide, Shape<1, 3>, Shape<3, 1>>{});
   else if (q <= 256) f(std::conditional_t<wide, Shape<1, 4>, Shape<4, 1>>{});
+  else if (q <= 384) f(Shape<3, 2>{});
   else if (q <= 512) f(Shape<4, 2>{});
+  else if (q <= 768) f(std::conditional_t<wide, Shape<4, 3>, Shape<6, 2>>{});
   else if (q <= 1024) f(std::conditional_t<wide, Shape<4, 4>, Shape<8, 2>>{});
   else if constexpr (wide) f(Shape<8, 4>{});
 }
@@ -79,14 +89,14 @@ uint32_t most_parts(uint32_t waves) { return waves == 1 ? kMostParts : 256; }
 // flight (one / two at a time, us without the parts' sum: 16384 of 1376 in bfloat16 47.6 / 39.9,
 // 8192 of 2048 25.8 / 26.0, 1531 of 1373 8.4 / 9.3, 1000 of 2048 7.7 / 8.1).
 constexpr uint32_t kTwoRows = 4096;
-// The wavefronts of a row's group there.
-uint32_t grad_waves(uint32_t type, uint32_t d) {
-  uint32_t waves = 0;
+// The wavefronts of a row's group there, and the groups of a workgroup.
+void grad_groups(uint32_t type, uint32_t d, uint32_t &waves, uint32_t &groups) {
   with_type(type, [&](auto t) {
     constexpr uint32_t E = fiona::kLaneElems<decltype(t)>;
-    with_grad_shape<decltype(t)>((d + E - 1) / E, [&](auto s) { waves = decltype(s)::kWaves; });
+    with_grad_shape<decltype(t)>((d + E - 1) / E, [&](auto s) {
+      waves = decltype(s)::kWaves, groups = fiona::kGradGroups<decltype(s)::kWaves>;
+    });
   });
-  return waves;
 }
 constexpr uint32_t pitch_of(uint32_t d) { return (d + 3) / 4 * 4; }
 bool by_columns(uint32_t type, uint32_t d) { return d < 16 / type_size(type) || d > kMostSums; }
@@ -97,10 +107,9 @@ bool by_columns(uint32_t type, uint32_t d) { return d < 16 / type_size(type) || 
 uint32_t few_rows(uint32_t waves) { return waves == 1 ? 16 : 1; }
 uint32_t parts_of(uint32_t type, uint32_t d, uint32_t n) {
   if (by_columns(type, d)) return std::max(1u, std::min(d > kMostSums ? 64 : kMostParts, (n + 15) / 16));
-  const uint32_t waves = grad_waves(type, d);
-  if (n <= few_rows(waves)) return 1;
-  const uint32_t groups = waves == 1 ? fiona::kGradGroups<1> : waves == 4 ? fiona::kGradGroups<4> : 1;
-  return std::min(most_parts(waves), (n + groups - 1) / groups);
+  uint32_t waves = 1, groups = 1;
+  grad_groups(type, d, waves, groups);
+  return n <= few_rows(waves) ? 1 : std::min(most_parts(waves), (n + groups - 1) / groups);
 }
 
 }  // namespace

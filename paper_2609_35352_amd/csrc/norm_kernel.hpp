@@ -46,12 +46,13 @@ struct NormGradParams {
 // Workgroups: four wavefronts, or the sixteen of one group.
 template <int WAVES>
 constexpr int kNormThreads = WAVES > 4 ? 64 * WAVES : 256;
-// With the weights' gradients: groups of a workgroup, whose sums become one part (two
-// groups of four wavefronts, 256 parts / one, 512, us with the parts' sum: 8192 rows of 4096
-// in bfloat16 50.6 / 53.9, 8192 of 2048 30.4 / 33.5, 1531 of 1373 11.9 / 14.0; four groups of them
-// spill, and double the time of two rows at a time).
+// With the weights' gradients: groups of a workgroup, whose sums become one part: 4 to 12
+// wavefronts (groups of four wavefronts, two in 256 parts / one in 512, us with the parts' sum: 8192
+// rows of 4096 in bfloat16 50.6 / 53.9, 8192 of 2048 30.4 / 33.5, 1531 of 1373 11.9 / 14.0; three spill,
+// 49 and up; of three, four / three / two, without that sum: 16384 rows of 2560 58.5 / 57.5 / 70, of 1280 33.9 /
+// 40 / 35; of six, two / one: 8192 of 6144 68.5 / 73).
 template <int WAVES>
-constexpr int kGradGroups = WAVES == 1 ? 4 : WAVES == 4 ? 2 : 1;
+constexpr int kGradGroups = WAVES == 1 || WAVES == 3 ? 4 : WAVES == 4 || WAVES == 6 ? 2 : 1;
 
 // Sums of N values over a group; `slot` alternates from call to call, so that one
 // barrier is enough.

@@ -76,7 +76,7 @@ def _check_backward(c, got, base=True, affine=True):
 
 
 SHAPES = [(1, 1), (3, 5), (1, 768), (8, 768), (33, 1000), (17, 1373), (5, 2048), (6, 4096), (3, 5000), (2, 8192), (3, 16384),
-          (2, 20011), (2, 32768), (300, 64), (1000, 7), (515, 257), (2049, 96)]
+          (2, 20011), (2, 32768), (5, 700), (3, 2500), (2, 9001), (300, 64), (1000, 7), (515, 257), (2049, 96)]
 TYPES = [(F32, F32), (F16, F16), (F16, F32), (BF16, BF16), (BF16, F32)]
 
 
@@ -100,7 +100,8 @@ def test_backward(n, d, dtype, wt):
 
 
 @pytest.mark.parametrize("dtype,n,d", [(F16, 2, 1373), (F16, 3, 1373), (F16, 1025, 1373), (BF16, 4099, 1100), (F16, 513, 4096), (BF16, 300, 8190),
-                                       (F32, 4, 2500), (F32, 770, 1030), (F32, 300, 4099), (F32, 18, 999), (F32, 2051, 771), (BF16, 4101, 509)])
+                                       (F32, 4, 2500), (F32, 770, 1030), (F32, 300, 4099), (F32, 18, 999), (F32, 2051, 771), (BF16, 4101, 509),
+                                       (BF16, 1026, 1500), (F16, 4110, 1100), (F16, 2051, 2500), (BF16, 3, 2001), (BF16, 515, 5001), (F32, 4, 1300), (F32, 1029, 1500)])
 def test_backward_of_more_rows_than_groups(dtype, n, d):
     """Rows that fill one workgroup's groups, leave one of them a row short, or come again after every group's first."""
     dev = _dev()
