@@ -17,7 +17,7 @@ using namespace fiona_host;
 struct fiona_token_loss {
   fiona_token_loss_desc desc{};
   int device = -1;
-  char *ws = nullptr;      // parts of rows, then [3][max_tokens]: logits, log sums, derivatives
+  char *ws = nullptr;      // parts of rows, then [4][max_tokens]: log sums (2), logits, derivatives
   uint64_t part_cap = 0;   // parts that fit
 };
 
@@ -67,8 +67,8 @@ fiona::TokenParams params(const fiona_token_loss *H, uint32_t n, const void *log
   fiona::TokenParams P{};
   P.z = logits, P.dz = dlogits, P.targets = targets, P.z_row = logits_row, P.dz_row = dlogits_row;
   P.n_tok = n, P.vocab = H->desc.vocab;
-  P.part = (float2 *)H->ws, P.at_target = (float *)(P.part + H->part_cap);
-  P.lse = P.at_target + H->desc.max_tokens, P.coef = P.lse + H->desc.max_tokens;
+  P.part = (float2 *)H->ws, P.lse = P.part + H->part_cap;
+  P.at_target = (float *)(P.lse + H->desc.max_tokens), P.coef = P.at_target + H->desc.max_tokens;
   P.skew = skew_of(H->desc, logits, logits_row, n);
   const uint32_t pieces = pieces_of(H->desc, P.skew);
   P.slice = (pieces + splits_of(n, pieces) - 1) / splits_of(n, pieces);
@@ -167,7 +167,7 @@ int fiona_token_loss_create(const fiona_token_loss_desc *desc, fiona_token_loss 
     return FIONA_ERR_HIP;
   }
   H->part_cap = (uint64_t)D.max_tokens + kWorkgroups;     // (n rounded-up quotients of kWorkgroups / n, or 64 of few rows)
-  if (hipMalloc((void **)&H->ws, H->part_cap * sizeof(float2) + (uint64_t)D.max_tokens * 3 * sizeof(float)) != hipSuccess) {
+  if (hipMalloc((void **)&H->ws, H->part_cap * sizeof(float2) + (uint64_t)D.max_tokens * 4 * sizeof(float)) != hipSuccess) {
     (void)hipGetLastError();
     delete H;
     return FIONA_ERR_NOMEM;

@@ -37,7 +37,8 @@ struct TokenParams {
   void *dz;
   const int32_t *targets;
   float2 *part;                   // [n_tok][splits]: maximum and sum of a part of a row
-  float *at_target, *lse, *coef;  // [n_tok]: the target's logit, log sum of exponentials, derivative of the loss
+  float2 *lse;                    // [n_tok]: log sum of exponentials (see log_sum)
+  float *at_target, *coef;        // [n_tok]: the target's logit, derivative of the loss
   uint64_t z_row, dz_row;
   uint32_t n_tok, vocab;
   uint32_t splits, slice;         // parts of a row, and their pieces
@@ -144,7 +145,10 @@ __device__ __forceinline__ void join_wave(float &m, float &s) {
   s = wave_sum(s * __builtin_amdgcn_exp2f((m - ms) * kLossLog2e));
   m = top;
 }
-__device__ __forceinline__ float log_sum(float m, float s) { return (m == -INFINITY ? 0.f : m) + kLossLn2 * __builtin_amdgcn_logf(s); }
+// A row's log sum of exponentials as its maximum and log2 of the sum, which are never added up: rounded to 32 bits
+// their sum would be off by 2^-24 of the maximum, and so would every log-probability and every exponent.
+__device__ __forceinline__ float2 log_sum(float m, float s) { return {m, __builtin_amdgcn_logf(s)}; }
+__device__ __forceinline__ float log_prob(float z, float2 lse) { return (z - lse.x) - kLossLn2 * lse.y; }
 
 // A workgroup to a part of a token's row.
 template <typename T, bool NARROW, bool SKEWED>
@@ -217,10 +221,11 @@ __global__ void __launch_bounds__(1024) pair_kernel(TokenParams P, PairParams Q,
     for (uint32_t i = 1; i < lanes; i *= 2) top = fmaxf(top, __shfl_xor(top, i));
     s *= __builtin_amdgcn_exp2f((m - (top == -INFINITY ? 0.f : top)) * kLossLog2e);
     for (uint32_t i = 1; i < lanes; i *= 2) s += __shfl_xor(s, i);
-    const float lse = log_sum(top, s);
+    const float2 lse = log_sum(top, s);
+    const float l = log_prob(zt, lse);
     if (lane || !live) continue;
     P.lse[t] = lse;
-    sum[0] += k ? 0. : zt - lse, sum[1] += k ? zt - lse : 0.;
+    sum[0] += k ? 0. : l, sum[1] += k ? l : 0.;
   }
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -248,12 +253,12 @@ __global__ void __launch_bounds__(1024) pair_kernel(TokenParams P, PairParams Q,
 
 // c (onehot(y) - softmax(z)) of a lane's piece.
 template <typename T, bool NARROW>
-__device__ __forceinline__ u4 gradient_of(u4 v, uint32_t at, uint32_t from, uint32_t n, uint32_t y, float c, float lse, bool whole = false) {
+__device__ __forceinline__ u4 gradient_of(u4 v, uint32_t at, uint32_t from, uint32_t n, uint32_t y, float c, float2 lse, bool whole = false) {
   constexpr int E = kLaneElems<T>;
   float x[E];
   logits_of<T, NARROW>(v, at, from, n, x, whole);
 #pragma unroll
-  for (int j = 0; j < E; ++j) x[j] = -c * __builtin_amdgcn_exp2f((x[j] - lse) * kLossLog2e);
+  for (int j = 0; j < E; ++j) x[j] = -c * __builtin_amdgcn_exp2f(__builtin_fmaf(x[j] - lse.x, kLossLog2e, -lse.y));
   if (y - at < (uint32_t)E) {
 #pragma unroll
     for (int j = 0; j < E; ++j)
@@ -290,7 +295,8 @@ __global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyPa
   auto inside = [&](uint32_t base) { return base + STEP <= end && (!from || base || w); };
   u4 v[U];
   auto load = [&](uint32_t base) { read_step<T, NARROW>(z, base + threadIdx.x * E, from, n, inside(base), v); };
-  float c = 0, lse = 0;
+  float c = 0;
+  float2 lse = {0, 0};
   if constexpr (POLICY) {
     const bool live = counts(y, P.vocab);
     float l = 0, loss = 0;
@@ -301,7 +307,7 @@ __global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyPa
       if (lane < P.splits) m = P.part[(uint64_t)t * P.splits + lane].x, s = P.part[(uint64_t)t * P.splits + lane].y;
       join_wave(m, s);
       lse = log_sum(m, s);
-      l = P.at_target[t] - lse;
+      l = log_prob(P.at_target[t], lse);
       c = policy_of(Q, P.n_tok, t, l, loss);
     }
     if (split == 0 && threadIdx.x == 0) Q.loss[t] = loss, Q.logps[t] = l;
@@ -397,7 +403,8 @@ __global__ void __launch_bounds__(1024, NL == 4 ? 8 : 4) policy_row_kernel(Token
   const uint32_t lane = threadIdx.x % 64;
   m = lane < threads / 64 ? part[lane].x : -INFINITY, s = lane < threads / 64 ? part[lane].y : 0.f;
   join_wave(m, s);
-  const float lse = log_sum(m, s), l = at_target - lse;
+  const float2 lse = log_sum(m, s);
+  const float l = log_prob(at_target, lse);
   float loss;
   const float c = policy_of(Q, P.n_tok, t, l, loss);
   if (c == 0) {
