@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <cfloat>
 #include <type_traits>
 
 #include "fiona.h"
@@ -221,7 +222,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams P) {
   const bool low = lane < 32;
   const float left = -expm1f(step * (low ? P.log_b1 : P.log_b2)), c = low ? __builtin_amdgcn_rcpf(left) : __builtin_amdgcn_rsqf(left);
   const float c1 = lane_value(c, 0), c2 = lane_value(c, 32), lr = *P.lr;
-  const float gs = P.grad_scale ? *P.grad_scale : 1.f, keep = 1.f - lr * C.decay;
+  const float gs = P.grad_scale ? *P.grad_scale : 1.f, decay = lr * C.decay, rate = lr * c1;
   const uint32_t key = mix((uint32_t)step * 0x9E3779B1u + P.seed);
   float g[4], m[4], v[4], x[4], um[4], uv[4];
   floats_of(rg, g), floats_of(rm, m), floats_of(rv, v);
@@ -240,7 +241,10 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams P) {
       v[j] = P.b2 * v[j] + P.a2 * (gj * gj);
       r = SMALL ? root_of(v[j]) : __builtin_amdgcn_sqrtf(v[j]);
     }
-    x[j] = x[j] * keep - lr * (m[j] * c1 * __builtin_amdgcn_rcpf(r * c2 + P.eps));
+    // Decay and update are rounded into x together: 1 - lr decay by itself is a multiple of 2^-24, none of the decay at
+    // lr 2e-6 and decay 0.01.  (An infinite x stays: its decay is that of the largest number.)
+    const float u = m[j] * __builtin_amdgcn_rcpf(r * c2 + P.eps);
+    x[j] -= __builtin_fmaf(rate, u, decay * __builtin_amdgcn_fmed3f(x[j], -FLT_MAX, FLT_MAX));
     if (sizeof(T) == 2) asm volatile("" : "+v"(x[j]));   // (param is this value rounded, not its last product's binary16 form)
     if (SMALL) {
       v[j] = r;
