@@ -64,6 +64,12 @@ __device__ __forceinline__ float root_of(float x) {
   return __builtin_fmaf(__builtin_fmaf(-r, r, x), 0.5f * y, r);
 }
 
+// x^1/2, a unit off at most, subnormal x included (the hardware's root takes those as zero).
+__device__ __forceinline__ float wide_root(float x) {
+  const bool low = x < 0x1p-100f;
+  return __builtin_amdgcn_sqrtf(low ? x * 0x1p32f : x) * (low ? 0x1p-16f : 1.f);
+}
+
 // Four consecutive elements of T, at any address that they may stand at.
 typedef uint32_t u1_any __attribute__((aligned(1)));
 template <typename T>
@@ -239,7 +245,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwParams P) {
 #pragma clang fp contract(off)
       m[j] = P.b1 * m[j] + P.a1 * gj;
       v[j] = P.b2 * v[j] + P.a2 * (gj * gj);
-      r = SMALL ? root_of(v[j]) : __builtin_amdgcn_sqrtf(v[j]);
+      r = SMALL ? root_of(v[j]) : wide_root(v[j]);
     }
     // Decay and update are rounded into x together: 1 - lr decay by itself is a multiple of 2^-24, none of the decay at
     // lr 2e-6 and decay 0.01.  (An infinite x stays: its decay is that of the largest number.)
