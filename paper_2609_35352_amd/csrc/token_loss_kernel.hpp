@@ -61,9 +61,10 @@ struct PolicyParams {
 
 // The policy loss of a token with log-probability l, and its derivative.
 __device__ __forceinline__ float policy_of(const PolicyParams &Q, uint32_t n_tok, uint32_t t, float l, float &loss) {
-  const float w = Q.weights ? Q.weights[t] : 1.f / n_tok, a = Q.advantages[t], r = expf(l - Q.old[t]);
+  const float w = Q.weights ? Q.weights[t] : 1.f / n_tok, a = Q.advantages[t], x = l - Q.old[t], r = expf(x);
   if (w == 0) return loss = 0;
-  const float open = r * a, held = fminf(fmaxf(r, 1 - Q.clip_low), 1 + Q.clip_high) * a;
+  // (a ratio beyond 2^128 is infinite here, but its product with no advantage is zero)
+  const float open = a == 0 && x < INFINITY ? 0.f : r * a, held = fminf(fmaxf(r, 1 - Q.clip_low), 1 + Q.clip_high) * a;
   const bool free = !(open > held);          // (also where r is no number)
   float c = free ? -open : 0.f, s = free ? -open : -held;
   if (Q.reference) {
