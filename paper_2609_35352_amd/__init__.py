@@ -924,6 +924,8 @@ class AdamW(_Handle):
         _lm_lib()
         lists = {"params": params, "grads": grads, "m": m, "v": v, "masters": masters, "m_scales": m_scales, "v_scales": v_scales}
         lists = {k: list(t) for k, t in lists.items() if t is not None}
+        # What a step writes, tensors that share a version counter (views of one) once.
+        roots = {id(b): b for b in (_root(x) for k in lists if k != "grads" for x in lists[k] if x is not None)}
         lists["params"] = [x.detach() for x in lists["params"]]
         n = len(lists["params"])
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
@@ -953,9 +955,8 @@ class AdamW(_Handle):
         self._create("fiona_adamw_create", _ADAMW_DESC.pack(code, 8 if small else 32, n, int(seed) & 0xFFFFFFFF, betas[0], betas[1], eps,
                                                             ctypes.addressof(table)))
         # Aliases: their memory stays, whatever becomes of the tensors given.
-        self._tensors = lists = {k: [x if x is None else x.detach() for x in t] for k, t in lists.items()}
-        # What a step writes, tensors that share a version counter (views of one) once.
-        self._written = list({id(b): b for b in (_root(x) for k in lists if k != "grads" for x in lists[k] if x is not None)}.values())
+        self._tensors = {k: [x if x is None else x.detach() for x in t] for k, t in lists.items()}
+        self._written = [b.detach() for b in roots.values()]
 
 
 def _root(t):
