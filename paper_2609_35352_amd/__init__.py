@@ -19,6 +19,7 @@ import ctypes
 import os
 import struct
 import threading
+import types
 
 import numpy as np
 
@@ -481,8 +482,8 @@ def hybrid_linear_static(plan: Plan, in_t, pt_t, sign_t, scale_t, out_t, stream=
 #
 # Tensors are float32, float16 or bfloat16 tensors of the current device whose last
 # axis is contiguous; the other axes may have any stride.  Nothing is recorded for
-# autograd: tensors that require a gradient are refused in grad mode, and what a call
-# writes counts as modified in place.
+# autograd: tensors that require a gradient are refused in grad mode, tensors with a
+# forward-mode tangent always, and what a call writes counts as modified in place.
 # ----------------------------------------------------------------------------
 
 # The header's structs, fields in order with native alignment; packed in one go, as a
@@ -503,7 +504,7 @@ _ADAMW_TENSOR = struct.Struct("@7PQd")
 _ADAMW_DESC = struct.Struct("@4I3dP")
 
 _DTYPES = {}   # torch dtype -> fiona_type
-_raw_stream, _device_now, _modified = [], [], []
+_raw_stream, _device_now, _modified, _forward = [], [], [], []
 _INT = {}      # bytes -> torch dtype, and "f32"
 
 
@@ -529,6 +530,8 @@ def _lm_lib():
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (without the stream object: 2 us a call)
         _raw_stream.append(raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream))
         _modified.append(torch.autograd.graph.increment_version)   # (a tensor or several)
+        fw = torch.autograd.forward_ad   # (without its level: every call asks)
+        _forward.append(fw if hasattr(fw, "_current_level") else types.SimpleNamespace(_current_level=0, unpack_dual=fw.unpack_dual))
         _device_now.append(getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device)
         _INT.update({4: torch.int32, 8: torch.int64, "f32": torch.float32})
         _DTYPES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})   # (last: who finds a type finds all else)
@@ -555,6 +558,16 @@ def _type_code(dtype) -> int:
     if code is None:
         raise ValueError("%s is not float32, float16 or bfloat16" % (dtype,))
     return code
+
+
+def _no_tangents(arguments):
+    """Refuses tensors that carry a forward-mode tangent, in grad mode and outside it: no call computes those of its results.
+    (Asked for where a dual level is open; nothing carries one elsewhere.)"""
+    import torch
+
+    for name, t in arguments.items():
+        if isinstance(t, torch.Tensor) and _forward[0].unpack_dual(t).tangent is not None:
+            raise ValueError("%s carries a tangent, which this call does not follow (its primal or detach() where that is meant)" % name)
 
 
 def _refuse(t, name, dtype, shape, dev, packed=False):
@@ -636,6 +649,8 @@ def kv_append(k, v, slots, k_cache, v_cache, positions=None, cos=None, sin=None,
         pp = _packed(positions, "positions", _INT[4], (n,), dev)
     args = _APPEND_ARGS.pack(n, H, code, rot, n_pos, 1 if interleaved else 0, k.data_ptr(), v.data_ptr(), qp, qop,
                              ks[0], ks[1], vs[0], vs[1], qs[0], qs[1], qos[0], qos[1], at, pp, cp, sp)
+    if _forward[0]._current_level >= 0:
+        _no_tangents(locals())
     rc = lib().fiona_kv_append(cache, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_kv_append")
@@ -685,6 +700,8 @@ def paged_attention(att: Attention, q, k_cache, v_cache, page_table, lengths, ou
     args = _ATTENTION_ARGS.pack(n, width, int(window), float(scale) if scale is not None else att.head_dim ** -0.5,
                                 float(softcap), q.data_ptr(), out.data_ptr(), lp, qs[0], qs[1], os_[0], os_[1],
                                 ts[0], page_table.data_ptr(), _packed(lengths, "lengths", _INT[4], (n,), dev))
+    if _forward[0]._current_level >= 0:
+        _no_tangents(locals())
     rc = lib().fiona_paged_attention(att.handle, cache, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_paged_attention")
@@ -739,6 +756,8 @@ def adapter_linear(ad: Adapters, x, ids, A, B, base, y, ranks=None, scaling=None
     bp, bs = (base.data_ptr(), _rows(base, "base", ad.dtype, shape, dev)[0]) if base is not None else (0, 0)
     ys = _rows(y, "y", ad.dtype, shape, dev)
     args = _ADAPTER_ARGS.pack(*head, bp, y.data_ptr(), bs, ys[0], 0, 0, 0, 0, 0, 0, 0, 0)
+    if _forward[0]._current_level >= 0:
+        _no_tangents(locals())
     rc = lib().fiona_adapter_linear(ad.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_adapter_linear")
@@ -756,6 +775,8 @@ def adapter_backward(ad: Adapters, x, ids, A, B, dy, dx_base, dx, dA, dB, ranks=
     args = _ADAPTER_ARGS.pack(*head, 0, 0, 0, 0, dy.data_ptr(), bp, dx.data_ptr(),
                               _packed(dA, "dA", dt, (ad.n_adapter, ad.max_rank, ad.d_in), dev),
                               _packed(dB, "dB", dt, (ad.n_adapter, ad.d_out, ad.max_rank), dev), gs[0], bs, xs[0])
+    if _forward[0]._current_level >= 0:
+        _no_tangents(locals())
     rc = lib().fiona_adapter_backward(ad.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_adapter_backward")
@@ -789,6 +810,8 @@ def layer_norm(x, weight, bias, y, eps: float = 1e-5, residual=None, total=None,
                            _packed(bias, "bias", wt, (d,), dev) if bias is not None else 0, y.data_ptr(), tp,
                            _packed(mean, "mean", f32, (n,), dev) if mean is not None else 0,
                            _packed(rstd, "rstd", f32, (n,), dev) if rstd is not None else 0, xs[0], rs, ys[0], ts)
+    if _forward[0]._current_level >= 0:
+        _no_tangents(locals())
     rc = lib().fiona_layer_norm(args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_layer_norm")
@@ -847,6 +870,8 @@ def layer_norm_backward(ln: LayerNorm, dy, x, weight, mean, rstd, dx_base, dx, d
                                     _packed(mean, "mean", f32, (n,), dev), _packed(rstd, "rstd", f32, (n,), dev), bp, dx.data_ptr(),
                                     _packed(dweight, "dweight", wt, row, dev) if dweight is not None else 0,
                                     _packed(dbias, "dbias", wt, row, dev) if dbias is not None else 0, gs[0], xs[0], bs, ds[0])
+    if _forward[0]._current_level >= 0:
+        _no_tangents(locals())
     rc = lib().fiona_layer_norm_backward(ln.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_layer_norm_backward")
@@ -880,6 +905,8 @@ def preference_loss(tl: TokenLoss, logits, targets, offsets, reference, loss, lo
                                  _packed(reference, "reference", f32, (2 * p,), dev),
                                  _packed(weights, "weights", f32, (p,), dev) if weights is not None else 0,
                                  _packed(loss, "loss", f32, (p,), dev), _packed(logps, "logps", f32, (2 * p,), dev))
+    if _forward[0]._current_level >= 0:
+        _no_tangents(locals())
     rc = lib().fiona_preference_loss(tl.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_preference_loss")
@@ -903,6 +930,8 @@ def policy_loss(tl: TokenLoss, logits, targets, old, advantages, loss, logps, dl
                              _packed(reference, "reference", f32, each, dev) if reference is not None else 0,
                              _packed(weights, "weights", f32, each, dev) if weights is not None else 0,
                              _packed(loss, "loss", f32, each, dev), _packed(logps, "logps", f32, each, dev))
+    if _forward[0]._current_level >= 0:
+        _no_tangents(locals())
     rc = lib().fiona_policy_loss(tl.handle, args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_policy_loss")
@@ -924,6 +953,8 @@ class AdamW(_Handle):
         _lm_lib()
         lists = {"params": params, "grads": grads, "m": m, "v": v, "masters": masters, "m_scales": m_scales, "v_scales": v_scales}
         lists = {k: list(t) for k, t in lists.items() if t is not None}
+        if _forward[0]._current_level >= 0:
+            _no_tangents({"%s[%d]" % (k, i): x for k, t in lists.items() for i, x in enumerate(t)})
         # What a step writes, tensors that share a version counter (views of one) once.
         roots = {id(b): b for b in (_root(x) for k in lists if k != "grads" for x in lists[k] if x is not None)}
         lists["params"] = [x.detach() for x in lists["params"]]
@@ -971,6 +1002,8 @@ def adamw_step(opt: AdamW, lr, step, grad_scale=None, stream=None) -> None:
     dev = lr.get_device() if opt.device is None else opt.device
     args = (_shared(lr, "lr", _INT["f32"], dev), _shared(step, "step", _INT[4], dev),
             _shared(grad_scale, "grad_scale", _INT["f32"], dev) if grad_scale is not None else 0)
+    if _forward[0]._current_level >= 0:
+        _no_tangents(locals())
     rc = lib().fiona_adamw_step(opt.handle, *args, _stream_of(stream, dev))
     if rc:
         raise FionaError(rc, "fiona_adamw_step")
