@@ -44,11 +44,10 @@ __device__ __forceinline__ u4 pack(const float (&x)[kLaneElems<T>]) {
 }
 
 // A lane's piece of a row of n elements, from element `at`: nothing from n on.
-template <typename T, bool ONCE = true>
+template <typename T>
 __device__ __forceinline__ void store_piece(T *row, uint32_t at, uint32_t n, u4 v) {
   if (at + kLaneElems<T> <= n) {
-    if (ONCE) __builtin_nontemporal_store(v, (u4_any *)(row + at));
-    else *(u4_any *)(row + at) = v;
+    __builtin_nontemporal_store(v, (u4_any *)(row + at));
   } else {
 #pragma unroll
     for (int j = 0; j < (int)kLaneElems<T>; ++j)

@@ -96,7 +96,7 @@ template <typename T, bool POLICY>
 void launch_grad(const fiona::TokenParams &P, const fiona::PolicyParams &Q, hipStream_t stream) {
   with_rows<T>(P, [&](auto narrow, auto skewed) {
     hipLaunchKernelGGL((fiona::token_grad_kernel<T, decltype(narrow)::value, decltype(skewed)::value, POLICY>),
-                       dim3(P.n_tok, P.dz ? P.splits : 1), dim3(256), 0, stream, P, Q, P.slice);
+                       dim3(P.n_tok, P.dz ? P.splits : 1), dim3(256), 0, stream, P, Q);
   });
 }
 

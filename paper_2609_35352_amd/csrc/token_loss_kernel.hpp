@@ -283,7 +283,7 @@ __device__ __forceinline__ void store_inside(T *row, uint32_t at, uint32_t from,
 // A workgroup to a part of a token's row of the gradient.  POLICY: the token's loss as
 // well, from the parts of its row.
 template <typename T, bool NARROW, bool SKEWED, bool POLICY>
-__global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyParams Q, uint32_t slice) {
+__global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyParams Q) {
   constexpr int E = kLaneElems<T>, U = 2;
   // From the last token on: its logits were read last.
   const uint32_t t = P.n_tok - 1 - blockIdx.x, split = blockIdx.y;
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(256) token_grad_kernel(TokenParams P, PolicyPa
   const uint32_t from = before<T, SKEWED>(z, P.skew), n = P.vocab + from, w = wave_index();
   z -= from;
   constexpr uint32_t STEP = U * 256 * E;
-  const uint32_t start = split * slice * E, end = min(start + slice * E, n);
+  const uint32_t start = split * P.slice * E, end = min(start + P.slice * E, n);
   auto inside = [&](uint32_t base) { return base + STEP <= end && (!from || base || w); };
   u4 v[U];
   auto load = [&](uint32_t base) { read_step<T, NARROW>(z, base + threadIdx.x * E, from, n, inside(base), v); };
