@@ -760,7 +760,8 @@ int fiona_policy_loss(const fiona_token_loss *loss, const fiona_policy_args *arg
  * fiona_adamw_step: one step over all tensors of a handle, each of n contiguous
  * elements.  With g the gradient (times *grad_scale), t = *step and lr = *lr,
  *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
- *     p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ *     p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),
+ * p rounded once a step (so that a decay far below 2^-24 p a step is applied in the mean)
  *   param, grad  device, of the desc's type; param is written
  *   master       device, float32, or NULL.  With it p is the master, and param its value rounded;
  *                without, what a step changes by less than half a unit of a 16-bit param is lost

@@ -7,9 +7,9 @@
 // with the probability of what it is above the lower, which keeps its mean.
 //
 // What bounds it: memory, 28 bytes an element with 32-bit states, 16 with 8-bit ones beside
-// masters (38 million elements: 171 us, 6.3 TB/s, and 103 us, 6.0; a copy reaches 5.2);
-// with 8-bit states and neither masters nor 32-bit parameters (10 bytes, 95 us) the vector
-// units: about 90 instructions an element, two 32-bit products of the dither's among them.
+// masters (38 million elements: 175 us, 6.1 TB/s, and 103 us, 6.0; a copy reaches 5.2);
+// with 8-bit states and neither masters nor 32-bit parameters (10 bytes, 97 us) the vector
+// units: nearly 100 instructions an element, two 32-bit products of the dither's among them.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

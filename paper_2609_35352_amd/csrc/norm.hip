@@ -37,7 +37,8 @@ int check_types(uint32_t type, uint32_t weight_type, uint32_t width) {
 
 // The wavefronts and pieces that hold rows of q pieces: f(waves, pieces a lane).  (Three
 // quarters of a shape where they hold the row, us: 16384 rows of 1280 in bfloat16 33.2 / 30.6, 8192
-// of 5120 64.3 / 58.2, 2048 of 20480 79 / 73.)
+// of 5120 64.3 / 58.2, 2048 of 20480 79 / 73.)  The widest shape of 32 bits spills 5 registers
+// forwards; for dx see norm_grad_kernel.
 template <int W, int NV>
 struct Shape {
   static constexpr int kWaves = W, kPieces = NV;

@@ -184,7 +184,9 @@ __device__ __forceinline__ void store_grad(T *dx, uint32_t at, uint32_t d, bool 
   store_piece(dx, at, d, pack<T>(v));
 }
 
-// dx alone, a group to a row, which stays packed between the sums and the result.
+// dx alone, a group to a row, read once.  (Where a lane holds 24 elements or fewer of it nothing
+// spills; over 24576 elements of 16 bits 24 to 38 of a lane's registers do, over 16384 of 32 bits
+// 153 of them: the elements unpacked for the sums are kept for the result.)
 template <typename T, typename W, int WAVES, int NV>
 __global__ void __launch_bounds__(kNormThreads<WAVES>) norm_grad_kernel(NormGradParams P) {
   constexpr int E = kLaneElems<T>, GROUPS = kNormThreads<WAVES> / 64 / WAVES;
